@@ -419,6 +419,104 @@ int mpq_latency_estimate(const double* layer_us, int n_layers, int n_widths, con
                          double* total_us_out);
 int mpq_model_size_bytes(const int64_t* parameters, const int* bits, int n_layers, double* bytes_out);
 
+/* ==== serving a quantized model ====================================================================
+ * The linear layer above takes one activation step per tensor, calibrated beforehand.  A served model
+ * quantizes every token by its own maximum instead, keeps keys and values in 8 bits, and its tensors
+ * come in 16 bits as often as in 32.  In these calls a maximum so small that inv_b would not be finite
+ * (below qmax_b / FLT_MAX, 4e-37) counts as 0.  Element types of those tensors: */
+enum mpq_type { MPQ_F32 = 0, MPQ_BF16 = 1, MPQ_F16 = 2 };
+
+/* ---- Eq. 1 with a step per token, calibration and quantizer in one read --------------------------
+ * For each row t: m = max_k |x[t][k]|, codes_out[t][k] = code of x[t][k] under m, scale_out[t] = scale_b(m)
+ * (code and scale_b as defined at the top; a row of zeros gives zeros).
+ * x          [M x K] of x_type, K contiguous, rows x_stride elements apart (x_stride >= K; any alignment
+ *            that an element may have).
+ * codes_out  int8 [M x K], dense, any alignment.  scale_out float[M].  bits 2..8.
+ * Errors: MPQ_ERR_NULL, MPQ_ERR_SHAPE (dims, stride, an unknown type), MPQ_ERR_BITS, MPQ_ERR_ALIGN.  M = 0 is
+ * a batch without tokens: nothing is launched. */
+int mpq_token_quant(const void* x, int x_type, int64_t M, int64_t K, int64_t x_stride, int bits,
+                    int8_t* codes_out, float* scale_out, void* stream);
+
+/* ---- the quantized linear layer with a step per token and per output channel ----------------------
+ * y_out[m][n] = act(fl32(fl32(float(acc[m][n]) * a_scale[m]) * w_scale[n or 0])) rounded once to y_type,
+ * acc as mpq_qgemm defines it, act one of mpq_act.  a_scale float[M] (4-byte aligned); y_out [M x N] of
+ * y_type, dense, aligned to an element.  M = 0: nothing is launched.  Other arguments and errors as
+ * mpq_qgemm_act; an unknown y_type is MPQ_ERR_SHAPE.  No workspace. */
+int mpq_qgemm_tokens(const int8_t* a_q, const void* w_q, int w_storage_bits, int64_t M, int64_t N, int64_t K,
+                     const float* a_scale, const float* w_scale, int w_gran, int act, int y_type, void* y_out,
+                     void* stream);
+
+/* ---- both in one call: a linear layer from its input to its output --------------------------------
+ * mpq_token_quant(x, bits) followed by mpq_qgemm_tokens: the same results bit for bit.
+ * Workspace: the codes and steps of the tokens, size from the query (M = 0: 0), 16-byte aligned. */
+size_t mpq_linear_tokens_workspace_bytes(int64_t M, int64_t K);
+int mpq_linear_tokens(const void* x, int x_type, int64_t M, int64_t N, int64_t K, int64_t x_stride, int bits,
+                      const void* w_q, int w_storage_bits, const float* w_scale, int w_gran, int act, int y_type,
+                      void* y_out, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- a key/value cache of quantized pages ------------------------------------------------------------
+ * Keys and values of every sequence lie on pages of `page` tokens; token p of sequence s is in place p mod page
+ * of page table[s][p / page].  A page holds, for each of `heads` heads, codes of Eq. 1 under ONE maximum per
+ * page and head, for keys and for values apart.  The bit-width is a choice like any tensor's: 2..8, one byte a code.
+ *
+ * mpq_kv_cache (HOST struct of DEVICE pointers):
+ *   k_codes   int8 [pages][heads][page][dim]             v_codes  int8 [pages][heads][page / 4][dim][4]: four tokens of
+ *             a channel side by side, the order in which the product with the probabilities reads them
+ *   k_absmax, v_absmax  float [pages][heads]             page: 16, 32, 64 or 128;  dim: a multiple of 16, at most 256
+ *   Codes 16-byte, maxima 4-byte aligned.  A new cache needs no initialisation.
+ * mpq_kv_batch (HOST struct): the sequences of a call.
+ *   starts    device int32 [seqs + 1]: rows starts[s] .. starts[s + 1] - 1 of the call's tensors are the LAST tokens of
+ *             sequence s, in order; rows that belong to no sequence are neither read nor written
+ *   kv_len    device int32 [seqs]: tokens of each sequence, those rows included
+ *   table     device int32 [seqs][table_pages]
+ *   rows      of the call's tensors;  max_new >= every starts[s + 1] - starts[s] and max_len >= every kv_len[s] (HOST
+ *             bounds that size the launches: rows past max_new of a sequence are not processed, max_len only
+ *             decides how the work is split)
+ *   Contents of device arrays are not checked on the host and never cause a fault: ranges are cut to rows and to the
+ *   table, and tokens on a page outside 0 .. pages - 1 count as absent.  A page may stand in several tables as long as
+ *   no call appends to it.
+ *
+ * mpq_kv_append: rows of k and v ([rows][heads][dim] of `type`, dim contiguous, strides in elements) go to their
+ *   places.  The page's maximum becomes m' = max(its maximum m, max |new|), or max |new| alone where the call writes the
+ *   page's first token; where it grows, codes already there are quantized again, code' = Eq. 1 of fl32(code *
+ *   scale_b(m)) under m'.  Appending the same rows twice is the same as once.
+ * mpq_kv_gather: the rows' values fl32(code * scale_b(m)) rounded to `type`, k_out and v_out [rows][heads][dim]
+ *   dense; rows of absent tokens become 0.  Either output may be NULL.
+ * mpq_kv_attention: for row i of a sequence's n rows, at position p = kv_len - n + i, and query head h (of q_heads, a
+ *   multiple of heads; it reads key head h / (q_heads / heads)):
+ *     out = sum_j P_j V_j,  P = softmax over the visible j of softmax_scale * (q . K_j),  K, V = code * m / qmax_b;
+ *   visible: j < kv_len and on a valid page; with `causal` also j <= p, and with window > 0 (causal only) j > p - window.
+ *   A row that sees nothing gives 0.  q, out [rows][q_heads][dim] of `type`, dim contiguous, strides in
+ *   elements.  Statistics and sums in fp32; fp32 tensors are multiplied as two 16-bit terms (about 22 bits).
+ *   Workspace from the query, 16-byte aligned (0 where one workgroup takes a sequence's keys).
+ * Errors (all three): MPQ_ERR_NULL, MPQ_ERR_SHAPE, MPQ_ERR_BITS, MPQ_ERR_ALIGN (codes, maxima, elements),
+ *   MPQ_ERR_WORKSPACE.  rows = 0 or seqs = 0: nothing is launched. */
+typedef struct mpq_kv_cache {
+  int8_t* k_codes;
+  int8_t* v_codes;
+  float* k_absmax;
+  float* v_absmax;
+  int64_t pages;
+  int heads, dim, page, bits;
+} mpq_kv_cache;
+typedef struct mpq_kv_batch {
+  const int32_t* starts;
+  const int32_t* kv_len;
+  const int32_t* table;
+  int64_t rows;
+  int64_t max_new, max_len;
+  int seqs, table_pages;
+} mpq_kv_batch;
+int mpq_kv_append(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, const void* k, int64_t k_token_stride,
+                  int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride, void* stream);
+int mpq_kv_gather(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, void* k_out, void* v_out,
+                  void* stream);
+size_t mpq_kv_attention_workspace_bytes(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int q_heads);
+int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, const void* q,
+                     int64_t q_token_stride, int64_t q_head_stride, int q_heads, float softmax_scale, int causal,
+                     int64_t window, void* out, int64_t out_token_stride, int64_t out_head_stride, void* ws,
+                     size_t ws_bytes, void* stream);
+
 /* ---- measurement aid (not part of the method) --------------------------------------------------
  * Launches a kernel that does nothing but issue the int8 matrix instructions of the GEMM kernels (16x16x64; one
  * workgroup of eight waves per CU, 32 x iters instructions per wave) on operand registers filled once from

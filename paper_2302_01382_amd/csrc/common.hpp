@@ -41,6 +41,11 @@ int qgemm_act_partials(const int8_t* a_q, const void* w_q, int w_storage_bits, i
                        const float* a_scale, const float* w_scale, int w_gran, int act, float* y_out,
                        float* absmax_out, float* part, int64_t room, int* parts, hipStream_t st);
 
+// defined in token_quant.hip: the argument checks of mpq_token_quant but for its outputs, and the launch
+int check_token_quant(const void* x, int x_type, int64_t M, int64_t K, int64_t x_stride, int bits);
+int launch_token_quant(const void* x, int x_type, int64_t M, int64_t K, int64_t x_stride, int bits, int8_t* codes, float* scale,
+                       hipStream_t st);
+
 // defined in hutchinson.hip: allows its kernels the LDS they need on the current device (mpq_init)
 int prepare_hutchinson();
 

@@ -1,0 +1,473 @@
+// kv_attention.hip -- attention over a cache of quantized pages.
+//
+// For a row q at position p of its sequence and a key head:  o = sum_j P_j V_j, P = softmax_j(c q . K_j) over the visible
+// tokens j, K_j = code * (m_k / qmax) and V_j likewise with ONE maximum per page and head.  So both products run on the
+// codes themselves, which fp16 holds exactly, and a page's maximum is a factor of its 16 tokens' logits (keys) or
+// probabilities (values).
+//
+// One pass over the tokens with the running maximum and sum of the softmax, in registers alone:
+//   S' = K q'     16 tokens x 16 rows:  a lane holds four tokens of one row (lane & 15)
+//   O' = V' P'    16 channels x 16 rows: the operand P' of v_mfma_f32_16x16x32_f16 wants, from that same lane, eight tokens of
+//                 that row -- four of each of two S' tiles, which is what it holds.  The other operand is then four tokens of
+//                 a channel from each of the two tiles: a dword of the cache's value order [page / 4][dim][4] each.
+// No LDS, no transposition; the order of k within a product is free.
+//
+// Precision: logits, maxima, sums and outputs are fp32.  q goes in as fp16 after a scaling by a power of two (its row's
+// largest entry to 2^14: bf16 and fp16 keep every bit down to 2^-28 of that entry), fp32 as two such terms (22 bits).
+// Probabilities, at most 1, go in as fp16 times 2^14 (rounded by 2^-11, like an fp16 output), for
+// fp32 as two terms.  Values' maxima differ from page to page: probabilities carry them relative to a power of two that is
+// at least the largest maximum so far, an exact rescaling whenever it grows.
+#include "kv.hpp"
+
+namespace mpq {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+
+// four codes -> fp16: the byte code + 128 as the low bits of 1024 + u, less 1152 (both exact)
+__device__ __forceinline__ void codes4(int w, f16x2& lo, f16x2& hi) {
+  const unsigned u = (unsigned)w ^ 0x80808080u;
+  const f16x2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+  lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off;
+  hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off;
+}
+__device__ __forceinline__ f16x8 codes8(int a, int b) {
+  f16x2 x, y, z, w;
+  codes4(a, x, y);
+  codes4(b, z, w);
+  return f16x8{x.x, x.y, y.x, y.y, z.x, z.y, w.x, w.y};
+}
+
+__device__ __forceinline__ float across(float v, int mask) { return __shfl_xor(v, mask, 64); }
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kPBits = 14;  // probabilities are multiplied by 2^14 before they are rounded to fp16
+
+struct AttnArgs {
+  mpq_kv_cache c;
+  mpq_kv_batch b;
+  const void* q;
+  int64_t q_ts, q_hs;
+  void* out;
+  int64_t o_ts, o_hs;
+  int q_heads, group, causal;
+  int64_t window;
+  float scale;        // softmax_scale
+  int64_t row_tiles;  // tiles of 16 (row, query head) pairs per sequence and key head
+  int splits;
+  float* part_o;      // splits > 1: [tile][split][16][dim], then
+  float* part_ml;     // [tile][split][16][2]
+};
+
+constexpr int kAttnWaves = 4;
+
+// What a workgroup's rows may see: tokens [lo, hi).
+struct Span {
+  int64_t lo, hi;
+};
+
+template <int T, int DH>
+struct AttnShape {
+  static constexpr int TERMS = T == MPQ_F32 ? 2 : 1;
+  static constexpr int TT = DH <= 2 ? 64 : 32;  // tokens per step
+  static constexpr int NS = TT / 16;
+  static constexpr int DP = DH * 64;
+};
+
+// grid: ((sequence * heads + head) * row_tiles + tile) * splits + split.  DH: dim in units of 64, rounded up.
+template <int T, int DH>
+__global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
+  using S = AttnShape<T, DH>;
+  using E = Elem<T>;
+  typedef typename E::type El;
+  constexpr int TERMS = S::TERMS, TT = S::TT, NS = S::NS, DP = S::DP, NW = kAttnWaves;
+  __shared__ float sm_m[NW][16], sm_l[NW][16];
+  __shared__ __attribute__((aligned(16))) float sm_o[NW / 2][16][DP + 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int r = lane & 15, quarter = lane >> 4;
+  int64_t g = block_index();
+  const int split = (int)(g % a.splits);
+  const int64_t slot = g;  // of the partial results
+  g /= a.splits;
+  const int64_t tile = g % a.row_tiles;
+  g /= a.row_tiles;
+  const int h = (int)(g % a.c.heads);
+  const int64_t s = g / a.c.heads;
+  if (s >= a.b.seqs) return;
+  const Sequence sq = sequence(a.b, a.c.page, (int)s);
+  const int64_t len = sq.len < sq.room ? sq.len : sq.room;
+  const int64_t nrows = (int64_t)sq.n * a.group;
+  if (tile * 16 >= nrows) return;
+  const int D = a.c.dim;
+
+  // this lane's row: its position, what it sees
+  const int64_t idx = tile * 16 + r;
+  const bool real = idx < nrows;
+  const int64_t i = real ? idx / a.group : 0;
+  const int qh = h * a.group + (int)(real ? idx % a.group : 0);
+  auto seen = [&](int64_t row, int64_t& lo, int64_t& hi) {
+    const int64_t p = sq.len - sq.n + row;
+    hi = a.causal && p + 1 < len ? p + 1 : len;
+    lo = a.window > 0 && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
+  };
+  int64_t lo, hi;
+  seen(i, lo, hi);
+  if (!real) hi = 0;
+  // of the whole tile: its first and last token row
+  Span span;
+  {
+    int64_t unused;
+    const int64_t last = tile * 16 + 15 < nrows ? tile * 16 + 15 : nrows - 1;
+    seen(tile * 16 / a.group, span.lo, unused);
+    seen(last / a.group, unused, span.hi);
+  }
+  if (span.hi < span.lo) span.hi = span.lo;
+  // tokens that every row of the tile sees need no mask
+  int64_t all_lo, all_hi;
+  {
+    int64_t unused;
+    const int64_t last = tile * 16 + 15 < nrows ? tile * 16 + 15 : nrows - 1;
+    seen(last / a.group, all_lo, unused);
+    seen(tile * 16 / a.group, unused, all_hi);
+  }
+
+  // q: lane (row, quarter) holds channels 64 c + 16 quarter .. + 15 for every c, as the keys come
+  f16x8 q[TERMS][2 * DH];
+  float row_scale;
+  {
+    const El* row = reinterpret_cast<const El*>(a.q) + (sq.row0 + i) * a.q_ts + (int64_t)qh * a.q_hs;
+    f32x8 v[2 * DH];
+    float m = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 2 * DH; ++c) {
+      const int d = (c >> 1) * 64 + quarter * 16 + (c & 1) * 8;
+      v[c] = real && d < D ? E::load8(row + d) : f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[c][e]));
+    }
+    m = fmaxf(m, across(m, 16));
+    m = fmaxf(m, across(m, 32));
+    const int e2 = kPBits - (m > 0.0f ? __builtin_amdgcn_frexp_expf(m) : 0);
+#pragma unroll
+    for (int c = 0; c < 2 * DH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = __builtin_ldexpf(v[c][e], e2);
+        const _Float16 top = (_Float16)x;
+        q[0][c][e] = top;
+        if (TERMS == 2) q[TERMS - 1][c][e] = (_Float16)(x - (float)top);
+      }
+    // logits in units of log 2
+    const float qmax = (float)((1 << (a.c.bits - 1)) - 1);
+    row_scale = __builtin_ldexpf(a.scale * kLog2e / qmax, -e2);
+  }
+
+  // this workgroup's tokens: whole steps, dealt out to the splits in one piece each and to the waves in turn
+  const int64_t first = span.lo / TT, steps = (span.hi + TT - 1) / TT - first;
+  const int64_t per = steps > 0 ? (steps + a.splits - 1) / a.splits : 0;
+  const int64_t t0 = first + split * per, t1 = first + ((split + 1) * per < steps ? (split + 1) * per : steps);
+  const int32_t* table = a.b.table + s * a.b.table_pages;
+  const int64_t page_bytes = (int64_t)a.c.page * D;
+  const int shift = 31 - __builtin_clz((unsigned)a.c.page);
+
+  float m_run = -__builtin_inff(), l_run = 0.0f;
+  int v_exp = -100000;  // O' is in units of 2^(v_exp - kPBits)
+  f32x4 o[DH][4];
+#pragma unroll
+  for (int c = 0; c < DH; ++c)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[c][k] = f32x4{0, 0, 0, 0};
+
+  for (int64_t t = t0 + wave; t < t1; t += NW) {
+    const int64_t base = t * TT;
+    const int8_t *kp[NS], *vp[NS];
+    float mk[NS], mv[NS];
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+      const int64_t tok = base + u * 16;
+      const bool in = tok < span.hi;
+      const int64_t id0 = in ? table[tok >> shift] : -1;
+      const bool ok = id0 >= 0 && id0 < a.c.pages;
+      const int64_t id = ok ? id0 : 0;
+      const int at = (int)(tok & (a.c.page - 1));
+      kp[u] = a.c.k_codes + (id * a.c.heads + h) * page_bytes + at * D;
+      vp[u] = a.c.v_codes + (id * a.c.heads + h) * page_bytes + at * D;
+      mk[u] = ok ? a.c.k_absmax[id * a.c.heads + h] : -1.0f;
+      mv[u] = ok ? a.c.v_absmax[id * a.c.heads + h] : 0.0f;
+      bad |= !ok;
+    }
+    // S': tokens 16 u + 4 quarter .. + 3 of the step, row r
+    f32x4 sc[NS];
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+      sc[u] = f32x4{0, 0, 0, 0};
+      v4i w[DH];
+#pragma unroll
+      for (int c = 0; c < DH; ++c) {
+        const int d = c * 64 + quarter * 16;
+        w[c] = d < D ? *reinterpret_cast<const v4i*>(kp[u] + r * D + d) : v4i{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int c = 0; c < DH; ++c) {
+        const f16x8 k0 = codes8(w[c].x, w[c].y), k1 = codes8(w[c].z, w[c].w);
+#pragma unroll
+        for (int x = 0; x < TERMS; ++x) {
+          sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[x][2 * c], sc[u], 0, 0, 0);
+          sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[x][2 * c + 1], sc[u], 0, 0, 0);
+        }
+      }
+    }
+    // logits, in scalars: where elements of the accumulator vectors themselves were overwritten under a lane's condition, the
+    // compiler (hipcc 7.2) spread the first one's value over the three others
+    float x[NS][4];
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+      const float f = row_scale * mk[u];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[u][e] = sc[u][e] * f;
+    }
+    if (bad || base < all_lo || base + TT > all_hi) {  // uniform
+      // the row's first and last visible token, counted from the lane's first of the step
+      const int64_t at = base + quarter * 4;
+      const int from = (int)(lo - at < -1 ? -1 : lo - at > TT ? TT : lo - at), to = (int)(hi - at < -TT ? -TT : hi - at > TT ? TT : hi - at);
+#pragma unroll
+      for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool out = (16 * u + e < from) | (16 * u + e >= to) | (mk[u] < 0.0f);
+          x[u][e] = out ? -__builtin_inff() : x[u][e];
+        }
+    }
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, x[u][e]);
+    top = fmaxf(top, across(top, 16));
+    top = fmaxf(top, across(top, 32));
+    int ve = v_exp;
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+      if (mv[u] > 0.0f) {
+        const int e = __builtin_amdgcn_frexp_expf(mv[u]);
+        ve = e > ve ? e : ve;
+      }
+    const float m_new = fmaxf(m_run, top);
+    const float m_use = m_new == -__builtin_inff() ? 0.0f : m_new;
+    if (ve != v_exp || __any(m_new > m_run)) {
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+      l_run *= alpha;
+      const float f = __builtin_ldexpf(alpha, v_exp - ve);
+#pragma unroll
+      for (int c = 0; c < DH; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[c][k] *= f;
+      v_exp = ve;
+      m_run = m_new;
+    }
+    f16x4 p[TERMS][NS];
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+      const float f = mv[u] > 0.0f ? __builtin_ldexpf(mv[u], kPBits - v_exp) : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float w = __builtin_amdgcn_exp2f(x[u][e] - m_use);
+        l_run += w;
+        const float y = w * f;
+        const _Float16 hi16 = (_Float16)y;
+        p[0][u][e] = hi16;
+        if (TERMS == 2) p[TERMS - 1][u][e] = (_Float16)(y - (float)hi16);
+      }
+    }
+    // O': channels 64 c + 4 (lane & 15) + k of the value operand
+#pragma unroll
+    for (int u = 0; u < NS; u += 2) {
+#pragma unroll
+      for (int c = 0; c < DH; ++c) {
+        const int d = c * 64 + r * 4;
+        const bool in = d < D;
+        const v4i w0 = in ? *reinterpret_cast<const v4i*>(vp[u] + (quarter * D + d) * 4) : v4i{0, 0, 0, 0};
+        const v4i w1 = in ? *reinterpret_cast<const v4i*>(vp[u + 1] + (quarter * D + d) * 4) : v4i{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const f16x8 v = codes8(w0[k], w1[k]);
+#pragma unroll
+          for (int term = 0; term < TERMS; ++term) {
+            const f16x8 pp = __builtin_shufflevector(p[term][u], p[term][u + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+            o[c][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pp, o[c][k], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+  // a row's sum over its four lanes; the waves' shares joined: a lane holds, of row r, channels
+  // 64 c + 16 quarter + 4 e + k in o[c][k][e]
+  l_run += across(l_run, 16);
+  l_run += across(l_run, 32);
+  if (quarter == 0) {
+    sm_m[wave][r] = m_run;
+    sm_l[wave][r] = l_run;
+  }
+  __syncthreads();
+  float m_all = sm_m[0][r];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) m_all = fmaxf(m_all, sm_m[w][r]);
+  const float m_use = m_all == -__builtin_inff() ? 0.0f : m_all;
+  const float mine = __builtin_amdgcn_exp2f(m_run - m_use);
+  const float qmax = (float)((1 << (a.c.bits - 1)) - 1);
+  const float f = l_run > 0.0f ? __builtin_ldexpf(mine, v_exp - kPBits) / qmax : 0.0f;
+#pragma unroll
+  for (int half = 1; half >= 0; --half) {  // the upper half of the waves leaves its share, the lower half adds its own
+    if (wave / (NW / 2) == half) {
+#pragma unroll
+      for (int c = 0; c < DH; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f32x4* to = reinterpret_cast<f32x4*>(&sm_o[wave % (NW / 2)][r][c * 64 + quarter * 16 + 4 * e]);
+          const f32x4 v = f32x4{o[c][0][e], o[c][1][e], o[c][2][e], o[c][3][e]} * f;
+          *to = half ? v : v + *to;
+        }
+    }
+    __syncthreads();
+  }
+  for (int x = threadIdx.x; x < 16 * (D >> 2); x += NW * 64) {
+    const int row = x / (D >> 2), d = (x % (D >> 2)) * 4;
+    float top = sm_m[0][row];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, sm_m[w][row]);
+    const float use = top == -__builtin_inff() ? 0.0f : top;
+    float l = 0.0f;
+    f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) l += sm_l[w][row] * __builtin_amdgcn_exp2f(sm_m[w][row] - use);
+#pragma unroll
+    for (int w = 0; w < NW / 2; ++w) v += *reinterpret_cast<const f32x4*>(&sm_o[w][row][d]);
+    if (a.splits > 1) {
+      *reinterpret_cast<f32x4*>(a.part_o + (slot * 16 + row) * D + d) = v;
+      if (d == 0) {
+        a.part_ml[(slot * 16 + row) * 2] = top;
+        a.part_ml[(slot * 16 + row) * 2 + 1] = l;
+      }
+      continue;
+    }
+    const int64_t at = tile * 16 + row;
+    if (at >= nrows) continue;
+    El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + at / a.group) * a.o_ts + (h * a.group + at % a.group) * a.o_hs + d;
+    E::store4(to, l > 0.0f ? v / l : f32x4{0, 0, 0, 0});
+  }
+}
+
+// Joins the splits of a tile of 16 rows.  grid: (sequence * heads + head) * row_tiles + tile.
+template <int T>
+__global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
+  using E = Elem<T>;
+  typedef typename E::type El;
+  int64_t g = block_index();
+  const int64_t slot = g * a.splits;
+  const int64_t tile = g % a.row_tiles;
+  g /= a.row_tiles;
+  const int h = (int)(g % a.c.heads);
+  const int64_t s = g / a.c.heads;
+  if (s >= a.b.seqs) return;
+  const Sequence sq = sequence(a.b, a.c.page, (int)s);
+  const int64_t nrows = (int64_t)sq.n * a.group;
+  const int D = a.c.dim;
+  for (int x = threadIdx.x; x < 16 * (D >> 2); x += kBlock) {
+    const int row = x / (D >> 2), d = (x % (D >> 2)) * 4;
+    const int64_t at = tile * 16 + row;
+    if (at >= nrows) continue;
+    float top = -__builtin_inff();
+    for (int i = 0; i < a.splits; ++i) top = fmaxf(top, a.part_ml[((slot + i) * 16 + row) * 2]);
+    const float use = top == -__builtin_inff() ? 0.0f : top;
+    float l = 0.0f;
+    f32x4 v = {0, 0, 0, 0};
+    for (int i = 0; i < a.splits; ++i) {
+      const float f = __builtin_amdgcn_exp2f(a.part_ml[((slot + i) * 16 + row) * 2] - use);
+      l += a.part_ml[((slot + i) * 16 + row) * 2 + 1] * f;
+      v += *reinterpret_cast<const f32x4*>(a.part_o + ((slot + i) * 16 + row) * D + d) * f;
+    }
+    El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + at / a.group) * a.o_ts + (h * a.group + at % a.group) * a.o_hs + d;
+    E::store4(to, l > 0.0f ? v / l : f32x4{0, 0, 0, 0});
+  }
+}
+
+// How a call is cut up.
+struct AttnPlan {
+  int64_t row_tiles, tiles;
+  int splits;
+  size_t ws_bytes;
+};
+static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int q_heads, AttnPlan& p) {
+  if (q_heads <= 0 || q_heads % c.heads) return MPQ_ERR_SHAPE;
+  const int64_t most = b.max_new < b.rows ? b.max_new : b.rows;
+  if (mul_overflows(most, q_heads)) return MPQ_ERR_SHAPE;
+  p.row_tiles = (most * (q_heads / c.heads) + 15) / 16;
+  if (mul_overflows(p.row_tiles, (int64_t)b.seqs * c.heads)) return MPQ_ERR_SHAPE;
+  p.tiles = p.row_tiles * b.seqs * c.heads;
+  p.splits = 1;
+  p.ws_bytes = 0;
+  if (p.tiles == 0) return MPQ_OK;
+  // about three workgroups per CU, none with less than 256 tokens (a step for each of its waves)
+  const int64_t len = b.max_len < (int64_t)b.table_pages * c.page ? b.max_len : (int64_t)b.table_pages * c.page;
+  const int64_t want = (3 * kNumCU + p.tiles - 1) / p.tiles, most_splits = (len + 255) / 256;
+  int64_t splits = want < most_splits ? want : most_splits;
+  p.splits = (int)(splits < 1 ? 1 : splits);
+  if (blocks_z(p.tiles * p.splits, kAttnWaves * 64) > 65535u) return MPQ_ERR_SHAPE;
+  p.ws_bytes = p.splits > 1 ? (size_t)p.tiles * p.splits * 16 * (c.dim + 2) * sizeof(float) : 0;
+  return MPQ_OK;
+}
+
+template <int T>
+static int launch_attention(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
+  const dim3 grid = wide_grid(p.tiles * p.splits, kAttnWaves * 64);
+  const int dh = (a.c.dim + 63) / 64;
+  if (dh == 1) kv_attention_k<T, 1><<<grid, kAttnWaves * 64, 0, st>>>(a);
+  else if (dh == 2) kv_attention_k<T, 2><<<grid, kAttnWaves * 64, 0, st>>>(a);
+  else kv_attention_k<T, 4><<<grid, kAttnWaves * 64, 0, st>>>(a);
+  const int rc = launch_status();
+  if (rc != MPQ_OK || p.splits == 1) return rc;
+  kv_attention_join_k<T><<<wide_grid(p.tiles, kBlock), kBlock, 0, st>>>(a);
+  return launch_status();
+}
+
+}  // namespace mpq
+
+using namespace mpq;
+
+extern "C" size_t mpq_kv_attention_workspace_bytes(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int q_heads) {
+  AttnPlan p;
+  if (check_kv(cache, batch, MPQ_F32) != MPQ_OK || plan_attention(*cache, *batch, q_heads, p) != MPQ_OK) return 0;
+  return p.ws_bytes;
+}
+
+extern "C" int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, const void* q,
+                                int64_t q_token_stride, int64_t q_head_stride, int q_heads, float softmax_scale, int causal,
+                                int64_t window, void* out, int64_t out_token_stride, int64_t out_head_stride, void* ws,
+                                size_t ws_bytes, void* stream) {
+  int rc = check_kv(cache, batch, type);
+  if (rc != MPQ_OK) return rc;
+  AttnPlan p;
+  rc = plan_attention(*cache, *batch, q_heads, p);
+  if (rc != MPQ_OK) return rc;
+  if (window < 0 || (window > 0 && !causal) || !(softmax_scale == softmax_scale) || __builtin_isinf(softmax_scale)) return MPQ_ERR_SHAPE;
+  if (q_token_stride < 0 || q_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0) return MPQ_ERR_SHAPE;
+  if (mul_overflows(batch->rows, q_token_stride) || mul_overflows(batch->rows, out_token_stride) || mul_overflows(q_heads, q_head_stride) ||
+      mul_overflows(q_heads, out_head_stride))
+    return MPQ_ERR_SHAPE;
+  const uintptr_t el = (uintptr_t)(type_size(type) - 1);
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & el) return MPQ_ERR_ALIGN;
+  if (p.tiles == 0) return MPQ_OK;
+  if (!q || !out) return MPQ_ERR_NULL;
+  if (p.ws_bytes > 0 && (!ws || ws_bytes < p.ws_bytes)) return MPQ_ERR_WORKSPACE;
+  if (p.ws_bytes > 0 && !aligned16(ws)) return MPQ_ERR_ALIGN;
+  AttnArgs a{*cache, *batch, q, q_token_stride, q_head_stride, out, out_token_stride, out_head_stride, q_heads, q_heads / cache->heads,
+             causal != 0, window, softmax_scale, p.row_tiles, p.splits, nullptr, nullptr};
+  if (p.splits > 1) {
+    a.part_o = reinterpret_cast<float*>(ws);
+    a.part_ml = a.part_o + (size_t)p.tiles * p.splits * 16 * cache->dim;
+  }
+  hipStream_t st = (hipStream_t)stream;
+  if (type == MPQ_F32) return launch_attention<MPQ_F32>(a, p, st);
+  if (type == MPQ_BF16) return launch_attention<MPQ_BF16>(a, p, st);
+  return launch_attention<MPQ_F16>(a, p, st);
+}

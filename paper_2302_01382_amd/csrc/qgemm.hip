@@ -165,10 +165,9 @@ struct AnyCfg {
   static constexpr int SUMS_OFF = 0;
 };
 template <int TS, bool W4, RowKind KIND, int EPI>
-__global__ __launch_bounds__(AnyCfg<TS>::NT, TS == 64 ? 4 : 2) void qgemm_any(
-    const int8_t* __restrict__ A, const void* __restrict__ Wv, int64_t M, int64_t N, int64_t K,
-    const float* __restrict__ a_scale, const float* __restrict__ w_scale, int w_per_row, float* __restrict__ Y,
-    int32_t* __restrict__ ACC, EpiArgs epi) {
+__device__ __forceinline__ void any_tile_of(const int8_t* __restrict__ A, const void* __restrict__ Wv, int64_t M, int64_t N, int64_t K,
+                                            const float* __restrict__ a_scale, const float* __restrict__ w_scale, int w_per_row,
+                                            float* __restrict__ Y, int32_t* __restrict__ ACC, const EpiArgs& epi) {
   using C = AnyCfg<TS>;
   using SA = AnyStage<C::NT, TS, 8, KIND>;
   using SB = AnyStage<C::NT, TS, W4 ? 4 : 8, KIND>;
@@ -176,6 +175,7 @@ __global__ __launch_bounds__(AnyCfg<TS>::NT, TS == 64 ? 4 : 2) void qgemm_any(
   __shared__ __attribute__((aligned(16))) int8_t lds_a[2][TS * kAnyBK];
   __shared__ __attribute__((aligned(16))) int8_t lds_b[2][TS * kAnyBK];
   __shared__ __attribute__((aligned(16))) float scales[TS];
+  __shared__ float rows[EPI >= 4 ? TS : 1];  // tokens: the A scales of the tile's rows
   __shared__ float sums[C::NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int wm = wave / C::WN, wn = wave % C::WN;
@@ -195,7 +195,11 @@ __global__ __launch_bounds__(AnyCfg<TS>::NT, TS == 64 ? 4 : 2) void qgemm_any(
     sb_.load(rb[u], u * BKB);
   }
   const bool want_y = EPI != 0 || Y != nullptr;
-  const float sa = f_from_bits(__builtin_amdgcn_readfirstlane(bits_from_f(want_y ? a_scale[0] : 0.0f)));
+  const float sa = f_from_bits(__builtin_amdgcn_readfirstlane(bits_from_f(want_y && EPI < 4 ? a_scale[0] : 0.0f)));
+  if (EPI >= 4 && (int)threadIdx.x < TS) {
+    const int64_t m = m0 + (int)threadIdx.x;
+    rows[threadIdx.x] = a_scale[m < M ? m : M - 1];
+  }
   if (want_y && (int)threadIdx.x < TS) {
     const int64_t n = n0 + (int)threadIdx.x;
     scales[threadIdx.x] = w_scale[w_per_row && n < N ? n : 0];
@@ -252,9 +256,24 @@ __global__ __launch_bounds__(AnyCfg<TS>::NT, TS == 64 ? 4 : 2) void qgemm_any(
   }
   acc_ready(acc);
   float sse = 0.0f, amax = 0.0f;
-  epilogue<C, W4, false, EPI>(acc, m0, n0, wm, wn, lane, reinterpret_cast<const char*>(scales), M, N, sa, want_y, q_inv, q_max, Y,
-                              ACC, epi, sse, amax);
+  epilogue<C, W4, false, EPI>(acc, m0, n0, wm, wn, lane, reinterpret_cast<const char*>(scales), reinterpret_cast<const char*>(rows),
+                              M, N, sa, want_y, q_inv, q_max, Y, ACC, epi, sse, amax);
   finish_sums<C, EPI>(reinterpret_cast<char*>(sums), wave, sse, amax, epi, (int64_t)blockIdx.y * gridDim.x + blockIdx.x);
+}
+template <int TS, bool W4, RowKind KIND, int EPI>
+__global__ __launch_bounds__(AnyCfg<TS>::NT, TS == 64 ? 4 : 2) void qgemm_any(
+    const int8_t* __restrict__ A, const void* __restrict__ Wv, int64_t M, int64_t N, int64_t K,
+    const float* __restrict__ a_scale, const float* __restrict__ w_scale, int w_per_row, float* __restrict__ Y,
+    int32_t* __restrict__ ACC, EpiArgs epi) {
+  any_tile_of<TS, W4, KIND, EPI>(A, Wv, M, N, K, a_scale, w_scale, w_per_row, Y, ACC, epi);
+}
+// EPI 4 and 5: a step per row of A
+template <int TS, bool W4, RowKind KIND, int EPI>
+__global__ __launch_bounds__(AnyCfg<TS>::NT, TS == 64 ? 4 : 2) void qgemm_tokens_any(
+    const int8_t* __restrict__ A, const void* __restrict__ Wv, int64_t M, int64_t N, int64_t K,
+    const float* __restrict__ a_scale, const float* __restrict__ w_scale, int w_per_row, float* __restrict__ Y,
+    int32_t* __restrict__ ACC, EpiArgs epi) {
+  any_tile_of<TS, W4, KIND, EPI>(A, Wv, M, N, K, a_scale, w_scale, w_per_row, Y, ACC, epi);
 }
 
 // sum of `count` per-workgroup partials, one workgroup, fixed order
@@ -361,7 +380,7 @@ static int check_qgemm_args(const int8_t* a_q, const void* w_q, int w_storage_bi
   if (w_storage_bits == 4 && (K & 1)) return MPQ_ERR_SHAPE;
   if (mul_overflows(M, N) || mul_overflows(M, K) || mul_overflows(N, K)) return MPQ_ERR_SHAPE;
   if (w_gran != MPQ_PER_TENSOR && w_gran != MPQ_PER_ROW) return MPQ_ERR_GRAN;
-  if (y_out && (reinterpret_cast<uintptr_t>(y_out) & 3u)) return MPQ_ERR_ALIGN;
+  if (y_out && (reinterpret_cast<uintptr_t>(y_out) & (epi_mode(epi) == 5 ? 1u : 3u))) return MPQ_ERR_ALIGN;
   if (y_ref && (reinterpret_cast<uintptr_t>(y_ref) & 3u)) return MPQ_ERR_ALIGN;
   if (acc_out && (reinterpret_cast<uintptr_t>(acc_out) & 3u)) return MPQ_ERR_ALIGN;
   const int64_t gx = (N + 127) / 128, gy = (M + 127) / 128;
@@ -386,8 +405,11 @@ static int run_qgemm(const int8_t* a_q, const void* w_q, int w_storage_bits, int
   const bool w4 = w_storage_bits == 4;
   // (the score keeps one partial per 64 x 64 tile at most: its workspace holds no more)
   const bool fast = fast_path(a_q, w_q, w4, M, N, K);
-  const int waves = epi.yref ? 0 : skinny_waves(M, N, K, fast && epi.amax);
-  const bool plain = !epi.yref && !epi.codes && !epi.act && !epi.amax;
+  const int mode = epi_mode(epi);
+  if (mode >= 4 && token_skinny(M, N, K))
+    return launch_token_skinny(w4, DmaArgs{a_q, w_q, M, N, K, a_scale, w_scale, per_row, y_out, acc_out, st, epi, n_partials, 1, 0, false});
+  const int waves = epi.yref || mode >= 4 ? 0 : skinny_waves(M, N, K, fast && epi.amax);
+  const bool plain = mode < 4 && !epi.yref && !epi.codes && !epi.act && !epi.amax;
   const SplitPlan sp = plain && fast ? plan_split(M, N, K) : SplitPlan{};
   const bool split = sp.split > 1 && ws && aligned16(ws) && ws_bytes >= (size_t)sp.split * (size_t)(M * N) * sizeof(int32_t);
   if (waves && !(split && split_beats_skinny(sp, M, K, w4)))
@@ -424,14 +446,18 @@ static int run_qgemm(const int8_t* a_q, const void* w_q, int w_storage_bits, int
   const int64_t w_row = w4 ? K >> 1 : K;
   const bool dword = ((K | w_row | (int64_t)reinterpret_cast<uintptr_t>(a_q) | (int64_t)reinterpret_cast<uintptr_t>(w_q)) & 3) == 0;
   const RowKind kind = w_row < 16 ? kRowsShort : dword ? kRowsDword : kRowsByte;
-  const int mode = epi.yref ? 1 : epi.codes ? 3 : (epi.act || epi.amax) ? 2 : 0;
 #define MPQ_ANY(TS_, W4_, KIND_, EPI_)                                                                                    \
   qgemm_any<TS_, W4_, KIND_, EPI_><<<grid, AnyCfg<TS_>::NT, 0, st>>>(a_q, w_q, M, N, K, a_scale, w_scale, per_row, y_out, \
                                                                      acc_out, epi)
-#define MPQ_ANY_EPI(TS_, W4_, KIND_)               \
-  (mode == 1   ? (void)MPQ_ANY(TS_, W4_, KIND_, 1) \
-   : mode == 2 ? (void)MPQ_ANY(TS_, W4_, KIND_, 2) \
-   : mode == 3 ? (void)MPQ_ANY(TS_, W4_, KIND_, 3) \
+#define MPQ_ANY_TOKENS(TS_, W4_, KIND_, EPI_)                                                                         \
+  qgemm_tokens_any<TS_, W4_, KIND_, EPI_><<<grid, AnyCfg<TS_>::NT, 0, st>>>(a_q, w_q, M, N, K, a_scale, w_scale, per_row, \
+                                                                            y_out, acc_out, epi)
+#define MPQ_ANY_EPI(TS_, W4_, KIND_)                      \
+  (mode == 1   ? (void)MPQ_ANY(TS_, W4_, KIND_, 1)        \
+   : mode == 2 ? (void)MPQ_ANY(TS_, W4_, KIND_, 2)        \
+   : mode == 3 ? (void)MPQ_ANY(TS_, W4_, KIND_, 3)        \
+   : mode == 4 ? (void)MPQ_ANY_TOKENS(TS_, W4_, KIND_, 4) \
+   : mode == 5 ? (void)MPQ_ANY_TOKENS(TS_, W4_, KIND_, 5) \
                : (void)MPQ_ANY(TS_, W4_, KIND_, 0))
 #define MPQ_ANY_KIND(TS_, W4_)                                      \
   (kind == kRowsShort   ? MPQ_ANY_EPI(TS_, W4_, kRowsShort)         \
@@ -446,6 +472,7 @@ static int run_qgemm(const int8_t* a_q, const void* w_q, int w_storage_bits, int
   }
 #undef MPQ_ANY_KIND
 #undef MPQ_ANY_EPI
+#undef MPQ_ANY_TOKENS
 #undef MPQ_ANY
   if (n_partials) *n_partials = gx * gy;
   return launch_status();
@@ -581,4 +608,59 @@ extern "C" int mpq_qgemm_score(const int8_t* a_q, const void* w_q, int w_storage
   if (rc != MPQ_OK) return rc;
   sum_partials_k<<<1, kBlock, 0, st>>>(partials, count, sse_out);
   return launch_status();
+}
+
+// The layer with a step per token: the tokens' epilogue on the same kernels.
+namespace mpq {
+static EpiArgs token_epi(int act, int y_type) {
+  EpiArgs epi{nullptr, nullptr, act, nullptr, nullptr, 0, nullptr};
+  epi.y_type = y_type;
+  return epi;
+}
+static int check_qgemm_tokens_args(const int8_t* a_q, const void* w_q, int w_storage_bits, int64_t M, int64_t N, int64_t K,
+                                   const float* a_scale, const float* w_scale, int w_gran, int act, int y_type, const void* y_out) {
+  if (act < MPQ_ACT_NONE || act > MPQ_ACT_GELU || !known_type(y_type) || M < 0) return MPQ_ERR_SHAPE;
+  if (M > 0 && !y_out) return MPQ_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(a_scale) & 3u || reinterpret_cast<uintptr_t>(w_scale) & 3u) return MPQ_ERR_ALIGN;
+  if (M == 0) {  // a batch without tokens: what can be said of the layer alone
+    static const int8_t some[16] = {};
+    a_q = some;
+    a_scale = w_scale;
+    y_out = some;
+  }
+  return check_qgemm_args(a_q, w_q, w_storage_bits, M ? M : 1, N, K, a_scale, w_scale, w_gran, reinterpret_cast<const float*>(y_out),
+                          nullptr, token_epi(act, y_type));
+}
+}  // namespace mpq
+
+extern "C" int mpq_qgemm_tokens(const int8_t* a_q, const void* w_q, int w_storage_bits, int64_t M, int64_t N, int64_t K,
+                                const float* a_scale, const float* w_scale, int w_gran, int act, int y_type, void* y_out,
+                                void* stream) {
+  const int rc = check_qgemm_tokens_args(a_q, w_q, w_storage_bits, M, N, K, a_scale, w_scale, w_gran, act, y_type, y_out);
+  if (rc != MPQ_OK || M == 0) return rc;
+  return run_qgemm(a_q, w_q, w_storage_bits, M, N, K, a_scale, w_scale, w_gran, reinterpret_cast<float*>(y_out), nullptr,
+                   token_epi(act, y_type), nullptr, (hipStream_t)stream);
+}
+
+// codes [M x K], then the steps from the next multiple of 16 on
+static size_t token_codes_bytes(int64_t M, int64_t K) { return ((size_t)(M * K) + 15) & ~(size_t)15; }
+extern "C" size_t mpq_linear_tokens_workspace_bytes(int64_t M, int64_t K) {
+  if (M <= 0 || K <= 0 || mul_overflows(M, K)) return 0;
+  return token_codes_bytes(M, K) + (size_t)M * sizeof(float);
+}
+extern "C" int mpq_linear_tokens(const void* x, int x_type, int64_t M, int64_t N, int64_t K, int64_t x_stride, int bits,
+                                 const void* w_q, int w_storage_bits, const float* w_scale, int w_gran, int act, int y_type,
+                                 void* y_out, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_token_quant(x, x_type, M, K, x_stride, bits);
+  if (rc != MPQ_OK) return rc;
+  if (M > 0 && (!ws || ws_bytes < mpq_linear_tokens_workspace_bytes(M, K))) return MPQ_ERR_WORKSPACE;
+  if (!aligned16(ws)) return MPQ_ERR_ALIGN;
+  int8_t* codes = reinterpret_cast<int8_t*>(ws);
+  float* steps = M > 0 ? reinterpret_cast<float*>(codes + token_codes_bytes(M, K)) : nullptr;
+  rc = check_qgemm_tokens_args(codes, w_q, w_storage_bits, M, N, K, steps, w_scale, w_gran, act, y_type, y_out);
+  if (rc != MPQ_OK || M == 0) return rc;
+  rc = launch_token_quant(x, x_type, M, K, x_stride, bits, codes, steps, (hipStream_t)stream);
+  if (rc != MPQ_OK) return rc;
+  return run_qgemm(codes, w_q, w_storage_bits, M, N, K, steps, w_scale, w_gran, reinterpret_cast<float*>(y_out), nullptr,
+                   token_epi(act, y_type), nullptr, (hipStream_t)stream);
 }

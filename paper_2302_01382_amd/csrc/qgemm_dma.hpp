@@ -4,7 +4,7 @@
 // options shared with the generic kernel (qgemm.hip).
 #pragma once
 
-#include "common.hpp"
+#include "types.hpp"
 
 #include <atomic>
 #include <type_traits>
@@ -15,6 +15,7 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 // the same in memory at any address an element may have
 typedef int v4i_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef int v2i_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef unsigned u32_any __attribute__((aligned(1)));
 
 // What an epilogue may do beyond Y = (float(acc) * s_A) * s_W[n]:
@@ -26,7 +27,8 @@ typedef unsigned u32_any __attribute__((aligned(1)));
 //    each other's atomics on one address);
 //  - codes: the activated output quantized on the spot (Eq. 1 with the absmax in q_absmax[0], which
 //    an earlier pass over the same product found) and stored as int8 codes, so that the fp32 layer
-//    output never travels to HBM and back on its way into the next layer's GEMM.
+//    output never travels to HBM and back on its way into the next layer's GEMM;
+//  - tokens: a step per row of A (a_scale is then [M]), the activation, and an output of y_type.
 struct EpiArgs {
   const float* yref;
   double* part;
@@ -36,8 +38,16 @@ struct EpiArgs {
   int q_bits;
   int8_t* codes;
   float* amax_part = nullptr;  // not null: a workgroup leaves its largest |Y| here, at its number, and not in amax
+  int y_type = -1;             // tokens: mpq_type of the output
 };
 constexpr EpiArgs kNoEpi = {nullptr, nullptr, 0, nullptr, nullptr, 0, nullptr};
+
+// The kernels' template argument EPI: 0 plain, 1 score, 2 activation and absmax of the output, 3 activation and int8 codes
+// of the output, 4 tokens with an fp32 output, 5 tokens with a 16-bit one.
+inline int epi_mode(const EpiArgs& epi) {
+  if (epi.y_type >= 0) return epi.y_type == MPQ_F32 ? 4 : 5;
+  return epi.yref ? 1 : epi.codes ? 3 : (epi.act || epi.amax) ? 2 : 0;
+}
 
 // GELU(y) = y Phi(y).  The epilogue's arithmetic is not hidden behind anything (every wave of the
 // workgroup is in its epilogue at the same time), so Phi is evaluated in about twenty lane
@@ -66,6 +76,17 @@ __device__ __forceinline__ float apply_act(float y, int act) {
   if (act == 1) return fmaxf(y, 0.0f);
   if (act == 2) return gelu_f(y);
   return y;
+}
+
+// four outputs in 16 bits, each rounded to nearest once; both types are formed, a uniform flag picks one
+__device__ __forceinline__ v2i to_half4(const float4& y, bool bf16) {
+  const f32x4 v = {y.x, y.y, y.z, y.w};
+  const v2i b = __builtin_bit_cast(v2i, __builtin_convertvector(v, bf16x4)), h = __builtin_bit_cast(v2i, __builtin_convertvector(v, f16x4));
+  return bf16 ? b : h;
+}
+__device__ __forceinline__ unsigned short to_half(float y, bool bf16) {
+  asm volatile("" : "+v"(y));  // its fp32 rounding stays: a product and its conversion would become one instruction that rounds once
+  return bf16 ? __builtin_bit_cast(unsigned short, (__bf16)y) : __builtin_bit_cast(unsigned short, (_Float16)y);
 }
 
 __device__ __forceinline__ float4 apply_act4(const float4& y, int act) {
@@ -195,6 +216,20 @@ __device__ __forceinline__ void request_scales(const float* w_scale, int64_t n0,
     }
   }
 }
+// The per-row A scales of the wave's rows in output tiles first .. end - 1, tile by tile into LDS: each wave reads what it
+// fetched itself, so that its own wait covers it.  A request covers 64 rows; what it brings beyond the wave's TM are the
+// rows that follow, in their place.  Rows past the edge: any scale.
+template <int BM, int TM>
+__device__ __forceinline__ void request_rows(const float* a_scale, int64_t M, int first, int end, int wm, int lane, unsigned lds_byte_off) {
+  for (int t = first; t < end; ++t) {
+#pragma unroll
+    for (int i = 0; i < TM; i += 64) {
+      const int at = wm * TM + i;
+      const int64_t m = (int64_t)t * BM + at + lane;
+      dma4(a_scale + (m < M ? m : M - 1), lds_byte_off + (unsigned)(((t - first) * BM + at) * 4));
+    }
+  }
+}
 template <int N_>
 __device__ __forceinline__ void wait_vmcnt() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N_) : "memory");
@@ -229,6 +264,8 @@ struct DmaCfg {
   static constexpr int SCALE_OFF = NSTAGE * STAGE;    // 1 KiB of per-channel W scales, then the waves' sums
   static constexpr int SUMS_OFF = SCALE_OFF + 1024;
   static constexpr int LDS_BYTES = SCALE_OFF + 2048;
+  static constexpr int ROWS_OFF = LDS_BYTES;          // tokens: the A scales of up to four output tiles' rows
+  static constexpr int ROWS_BYTES = 4 * BM * 4 + 256;
   static constexpr int NLA = BM / RPI;                // wave-loads per A stage
   static constexpr int NLB = W4 ? BN / PRPI : BN / RPI;  // wave-loads per W stage
   static constexpr int LPW = (NLA + NLB) / NW;        // wave-loads per wave per stage
@@ -426,26 +463,29 @@ struct Four {  // N % 4 == 0 and 16-byte aligned outputs
   typedef v4f F;
   typedef v4i I;
   typedef unsigned C;
+  typedef v2i H;
 };
 template <>
 struct Four<false> {
   typedef f4_any F;
   typedef v4i_any I;
   typedef u32_any C;
+  typedef v2i_any H;
 };
 
 // What a workgroup does with the accumulators of one output tile (see EpiArgs for EPI).  16x16 accumulator tile
 // (i, j): lane l holds m = l % 16 and the four consecutive n = 4 (l / 16) + 0..3: a store instruction writes 64
 // bytes of each of 16 rows.  (In 32x32 tiles it is 32 bytes of 32 rows: 67 MB stored by one workgroup per CU 14.5 us
 // against 11.5, 16.8 MB in 128 x 128 tiles 6.2 against 4.8, whole rows no better.)
-// scales: the tile's per-channel W scales in LDS.  sse, amax: the lane's running sums.
+// scales: the tile's per-channel W scales in LDS; rows: tokens, its per-row A scales there.  sse, amax: the lane's running sums.
 // Rows of N % 4 != 0 values, stored one by one before: 6846 x 1152 x 3139 121 -> 49 us, 2999 x 1152 x 1021 20.8 -> 9.7.
 template <class C, bool W4, bool VEC, int EPI, int ACT_KIND>
 __device__ __forceinline__ void epilogue_act(const v4i (&acc)[C::FM][C::FN], int64_t cur_m0, int64_t cur_n0, int wm, int wn, int lane,
-                                         const char* scales, int64_t M, int64_t N, float sa, bool want_y, float q_inv, float q_max,
-                                         float* __restrict__ Y, int32_t* __restrict__ ACC, const EpiArgs& epi, float& sse,
+                                         const char* scales, const char* rows, int64_t M, int64_t N, float sa, bool want_y, float q_inv,
+                                         float q_max, float* __restrict__ Y, int32_t* __restrict__ ACC, const EpiArgs& epi, float& sse,
                                          float& amax) {
-  constexpr bool SCORE = EPI == 1, ACT = EPI >= 2, AMAX = EPI == 2, QOUT = EPI == 3;
+  constexpr bool SCORE = EPI == 1, ACT = EPI >= 2, AMAX = EPI == 2, QOUT = EPI == 3, TOKENS = EPI >= 4, HALF = EPI == 5;
+  const bool bf16 = HALF && epi.y_type == MPQ_BF16;
   int8_t* __restrict__ CODES = epi.codes;
   const float* __restrict__ YREF = epi.yref;
   using F4 = typename Four<VEC>::F;
@@ -482,6 +522,7 @@ __device__ __forceinline__ void epilogue_act(const v4i (&acc)[C::FM][C::FN], int
         const int i = i0 + h;
         const int64_t m = cur_m0 + wm * C::TM + i * 16 + (lane & 15);
         if (m >= M) continue;
+        if (TOKENS) sa = *reinterpret_cast<const float*>(rows + (wm * C::TM + i * 16 + (lane & 15)) * 4);
         float part = 0.0f;  // the row's squares of the group, summed before they join the lane's running sum: short chains
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -504,7 +545,8 @@ __device__ __forceinline__ void epilogue_act(const v4i (&acc)[C::FM][C::FN], int
                 y = apply_act4(y, ACT_KIND);
                 if (AMAX) amax = fmaxf(fmaxf(amax, fmaxf(fabsf(y.x), fabsf(y.y))), fmaxf(fabsf(y.z), fabsf(y.w)));
               }
-              if (!QOUT && Y) *reinterpret_cast<F4*>(Y + m * N + n) = v4f{y.x, y.y, y.z, y.w};
+              if (HALF) *reinterpret_cast<typename Four<VEC>::H*>(reinterpret_cast<unsigned short*>(Y) + m * N + n) = to_half4(y, bf16);
+              else if (!QOUT && Y) *reinterpret_cast<F4*>(Y + m * N + n) = v4f{y.x, y.y, y.z, y.w};
               if (QOUT && CODES) {  // four codes, lowest n in the lowest byte
                 const unsigned c0 = (unsigned)(int)code_f(y.x, q_inv, q_max) & 0xFFu;
                 const unsigned c1 = (unsigned)(int)code_f(y.y, q_inv, q_max) & 0xFFu;
@@ -536,7 +578,8 @@ __device__ __forceinline__ void epilogue_act(const v4i (&acc)[C::FM][C::FN], int
                   y = apply_act(y, ACT_KIND);
                   if (AMAX) amax = fmaxf(amax, fabsf(y));
                 }
-                if (!QOUT && Y) Y[m * N + n + e] = y;
+                if (HALF) reinterpret_cast<unsigned short*>(Y)[m * N + n + e] = to_half(y, bf16);
+                else if (!QOUT && Y) Y[m * N + n + e] = y;
                 if (QOUT && CODES) CODES[m * N + n + e] = (int8_t)(int)code_f(y, q_inv, q_max);
                 if (SCORE && YREF) {
                   const float d = y - YREF[m * N + n + e];
@@ -556,11 +599,12 @@ __device__ __forceinline__ void epilogue_act(const v4i (&acc)[C::FM][C::FN], int
 // ReLU spends 2.3 us between its last matrix step and its last store, against 1.15 without an activation.
 template <class C, bool W4, bool VEC, int EPI>
 __device__ __forceinline__ void epilogue(const v4i (&acc)[C::FM][C::FN], int64_t cur_m0, int64_t cur_n0, int wm, int wn, int lane,
-                                         const char* scales, int64_t M, int64_t N, float sa, bool want_y, float q_inv, float q_max,
-                                         float* __restrict__ Y, int32_t* __restrict__ ACC, const EpiArgs& epi, float& sse,
+                                         const char* scales, const char* rows, int64_t M, int64_t N, float sa, bool want_y, float q_inv,
+                                         float q_max, float* __restrict__ Y, int32_t* __restrict__ ACC, const EpiArgs& epi, float& sse,
                                          float& amax) {
-#define MPQ_EPI(K_)                                                                                                     \
-  epilogue_act<C, W4, VEC, EPI, K_>(acc, cur_m0, cur_n0, wm, wn, lane, scales, M, N, sa, want_y, q_inv, q_max, Y, ACC, epi, sse, amax)
+#define MPQ_EPI(K_)                                                                                                          \
+  epilogue_act<C, W4, VEC, EPI, K_>(acc, cur_m0, cur_n0, wm, wn, lane, scales, rows, M, N, sa, want_y, q_inv, q_max, Y, ACC, \
+                                    epi, sse, amax)
   if (EPI >= 2 && epi.act == 2) MPQ_EPI(2);
   else if (EPI >= 2 && epi.act == 1) MPQ_EPI(1);
   else MPQ_EPI(0);
@@ -608,9 +652,7 @@ __device__ __forceinline__ void finish_sums(char* lds, int wave, float sse, floa
 // tiles of one output tile already fetch the first k tiles of the next one.  Chunks stay short so that the
 // hardware dispatcher, not a fixed assignment, balances the load when other kernels hold some of the CUs.
 // MINW: waves the register allocation must leave room for on one SIMD.
-// EPI: 0 plain, 1 score, 2 activation and absmax of the output, 3 activation and int8 codes of the
-// output (see EpiArgs); variants of their own because the largest tile has no registers to spare
-// for them in the plain kernel.
+// EPI: see epi_mode; variants of their own because the largest tile has no registers to spare for them in the plain kernel.
 template <int BM, int BN, int WM, int WN, int NSTAGE, bool W4, bool VEC, int KB, int MINW, int EPI>
 __global__ __launch_bounds__(WM * WN * 64, MINW) void qgemm_dma(const int8_t* __restrict__ A,
                                                           const void* __restrict__ Wv, int64_t M,
@@ -665,6 +707,8 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void qgemm_dma(const int8_t* __
   };
   start_rows(true);
   if (want_y && w_per_row) request_scales<VEC>(w_scale, n0, N, BN, lane, lds0 + C::SCALE_OFF);
+  const int first_tile = tile;
+  if (EPI >= 4) request_rows<BM, C::TM>(a_scale, M, tile, tile_end, wm, lane, lds0 + C::ROWS_OFF);
 #pragma unroll
   for (int p = 0; p < NSTAGE; ++p) {
     if (cursor.whole()) static_for<0, C::LPW>([&](auto r_) { plan.template request<decltype(r_)::value, true>(cursor, lds0 + p * C::STAGE); });
@@ -675,7 +719,7 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void qgemm_dma(const int8_t* __
   // epilogue they may come as vector loads whose arrival the compiler waits for at every store, vmcnt(0), as it
   // cannot tell on which path they were used first, and stores count in vmcnt as well: each 16-byte store of a
   // wave then waits for the one before it to be acknowledged.)
-  const float sa = want_y ? load_scalar(a_scale) : 0.0f, sw0 = want_y && !w_per_row ? load_scalar(w_scale) : 0.0f;
+  const float sa = want_y && EPI < 4 ? load_scalar(a_scale) : 0.0f, sw0 = want_y && !w_per_row ? load_scalar(w_scale) : 0.0f;
   float q_inv = 0.0f, q_max = 0.0f;
   if (QOUT) {
     float q_scale;
@@ -763,8 +807,8 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void qgemm_dma(const int8_t* __
     if (!last) wait_vmcnt<0>();
     landed = NSTAGE;
     acc_ready(acc);
-    epilogue<C, W4, VEC, EPI>(acc, (int64_t)tile * BM, n0, wm, wn, lane_again(), lds + C::SCALE_OFF, M, N, sa, want_y, q_inv, q_max,
-                              Y, ACC, epi, sse, amax);
+    epilogue<C, W4, VEC, EPI>(acc, (int64_t)tile * BM, n0, wm, wn, lane_again(), lds + C::SCALE_OFF,
+                              lds + C::ROWS_OFF + (tile - first_tile) * BM * 4, M, N, sa, want_y, q_inv, q_max, Y, ACC, epi, sse, amax);
     if (last) break;
     ++tile;
   }
@@ -791,20 +835,21 @@ inline int allow_lds(const void* kern, int bytes, std::atomic<unsigned>* done, i
 struct LaunchShape {
   int which = 0;
   int64_t tm = 0, tn = 0, grid = 0;
-  int chunk = 1, remap = 0;
+  int chunk = 1, remap = 0, lds = 0;
 };
-inline int launch_shape(int bm, int bn, int lds_bytes, int64_t M, int64_t N, const float* w_scale, int per_row, const float* y_out,
+inline int launch_shape(int bm, int bn, int lds_bytes, int rows_bytes, int64_t M, int64_t N, const float* w_scale, int per_row, const float* y_out,
                         const int32_t* acc_out, const EpiArgs& epi, int split, LaunchShape& s) {
-  // float4 / int4 stores need every 4-group of n inside the row and 16-byte aligned
-  const bool vec = (N & 3) == 0 && (!y_out || aligned16(y_out)) && (!acc_out || aligned16(acc_out)) &&
+  const int mode = epi_mode(epi);
+  // float4 / int4 stores need every 4-group of n inside the row and 16-byte aligned, four 16-bit outputs 8-byte aligned
+  const bool vec = (N & 3) == 0 && (!y_out || (reinterpret_cast<uintptr_t>(y_out) & (mode == 5 ? 7u : 15u)) == 0) && (!acc_out || aligned16(acc_out)) &&
                    (!((y_out || epi.yref || epi.amax || epi.codes) && per_row) || aligned16(w_scale)) &&
                    (!epi.yref || aligned16(epi.yref)) && (!epi.codes || (reinterpret_cast<uintptr_t>(epi.codes) & 3u) == 0);
-  const int mode = epi.yref ? 1 : epi.codes ? 3 : (epi.act || epi.amax) ? 2 : 0;
   s.which = mode * 2 + (vec ? 1 : 0);
+  s.lds = lds_bytes + (mode >= 4 ? rows_bytes : 0);
   s.tm = (M + bm - 1) / bm;
   s.tn = (N + bn - 1) / bn;
   if (s.tm * s.tn > 0x7FFFFFFF || s.tn > 0x7FFFFFFF) return MPQ_ERR_SHAPE;
-  s.chunk = chunk_tiles(s.tm, s.tn, split, lds_bytes, kNumCU);
+  s.chunk = chunk_tiles(s.tm, s.tn, split, s.lds, kNumCU);
   s.grid = (s.tm + s.chunk - 1) / s.chunk * s.tn;
   s.remap = (s.grid % 8 == 0 && s.grid >= 16) ? 1 : 0;
   return MPQ_OK;
@@ -822,25 +867,27 @@ static int launch_dma(const int8_t* a_q, const void* w_q, int64_t M, int64_t N, 
   using C = DmaCfg<BM, BN, WM, WN, NSTAGE, W4, KB>;
   using Kern = void (*)(const int8_t*, const void*, int64_t, int64_t, int64_t, const float*, const float*, int,
                         float*, int32_t*, EpiArgs, int, int, int, int, int);
-  static const Kern kerns[8] = {
+  static const Kern kerns[12] = {
       qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, false, KB, MINW, 0>, qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, true, KB, MINW, 0>,
       qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, false, KB, MINW, 1>, qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, true, KB, MINW, 1>,
       qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, false, KB, MINW, 2>, qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, true, KB, MINW, 2>,
-      qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, false, KB, MINW, 3>, qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, true, KB, MINW, 3>};
+      qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, false, KB, MINW, 3>, qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, true, KB, MINW, 3>,
+      qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, false, KB, MINW, 4>, qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, true, KB, MINW, 4>,
+      qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, false, KB, MINW, 5>, qgemm_dma<BM, BN, WM, WN, NSTAGE, W4, true, KB, MINW, 5>};
   static std::atomic<unsigned> done[kMaxDevices];
   if (prepare_only) {
-    for (int w = 0; w < 8; ++w) {
-      const int rc = allow_lds(reinterpret_cast<const void*>(kerns[w]), C::LDS_BYTES, done, w);
+    for (int w = 0; w < 12; ++w) {
+      const int rc = allow_lds(reinterpret_cast<const void*>(kerns[w]), C::LDS_BYTES + (w >= 8 ? C::ROWS_BYTES : 0), done, w);
       if (rc != MPQ_OK) return rc;
     }
     return MPQ_OK;
   }
   if (split <= 1) { split = 1; k_per_split = (int)K; }
   LaunchShape s;
-  int rc = launch_shape(BM, BN, C::LDS_BYTES, M, N, w_scale, per_row, y_out, acc_out, epi, split, s);
-  if (rc == MPQ_OK) rc = allow_lds(reinterpret_cast<const void*>(kerns[s.which]), C::LDS_BYTES, done, s.which);
+  int rc = launch_shape(BM, BN, C::LDS_BYTES, C::ROWS_BYTES, M, N, w_scale, per_row, y_out, acc_out, epi, split, s);
+  if (rc == MPQ_OK) rc = allow_lds(reinterpret_cast<const void*>(kerns[s.which]), s.lds, done, s.which);
   if (rc != MPQ_OK) return rc;
-  kerns[s.which]<<<dim3((unsigned)s.grid, (unsigned)split), C::NT, C::LDS_BYTES, st>>>(
+  kerns[s.which]<<<dim3((unsigned)s.grid, (unsigned)split), C::NT, s.lds, st>>>(
       a_q, w_q, M, N, K, a_scale, w_scale, per_row, y_out, acc_out, epi, (int)s.tn, (int)s.tm, s.chunk, s.remap, k_per_split);
   if (n_partials) *n_partials = s.grid;
   return launch_status();
@@ -872,5 +919,9 @@ int launch_dma_64(bool w4, int stages, int kb, const DmaArgs& a);
 // off with the tiled kernels.
 int skinny_waves(int64_t M, int64_t N, int64_t K, bool amax);
 int launch_skinny(int waves, bool w4, const DmaArgs& d);
+
+// The layer with a step per token where there are few tokens (qgemm_tokens.hip): whether it is better off there.
+bool token_skinny(int64_t M, int64_t N, int64_t K);
+int launch_token_skinny(bool w4, const DmaArgs& d);
 
 }  // namespace mpq

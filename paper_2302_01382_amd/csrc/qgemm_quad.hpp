@@ -136,6 +136,8 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void qgemm_quad(const int8_t* __re
     }
   };
   if (want_y && w_per_row) request_scales<VEC>(w_scale, n0, N, BN, lane, lds0 + C::SCALE_OFF);
+  const int first_tile = tile;
+  if (EPI >= 4) request_rows<BM, C::TM>(a_scale, M, tile, tile_end, wm, lane, lds0 + C::ROWS_OFF);
 #pragma unroll 1
   for (int p = 0; p < NSTAGE; ++p) {
     auto both = [&](auto whole_) {
@@ -147,7 +149,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void qgemm_quad(const int8_t* __re
     if (cursor.advance(tile_end)) start_rows(false);
   }
   // the epilogue's scalars: behind the requests, into scalar registers (see qgemm_dma)
-  const float sa = want_y ? load_scalar(a_scale) : 0.0f, sw0 = want_y && !w_per_row ? load_scalar(w_scale) : 0.0f;
+  const float sa = want_y && EPI < 4 ? load_scalar(a_scale) : 0.0f, sw0 = want_y && !w_per_row ? load_scalar(w_scale) : 0.0f;
   float q_inv = 0.0f, q_max = 0.0f;
   if (QOUT) {
     float q_scale;
@@ -258,8 +260,8 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void qgemm_quad(const int8_t* __re
     wait_vmcnt<0>();
     landed = NSTAGE;
     acc_ready(acc);
-    epilogue<C, W4, VEC, EPI>(acc, (int64_t)tile * BM, n0, wm, wn, lane_again(), lds + C::SCALE_OFF, M, N, sa, want_y, q_inv, q_max,
-                              Y, ACC, epi, sse, amax);
+    epilogue<C, W4, VEC, EPI>(acc, (int64_t)tile * BM, n0, wm, wn, lane_again(), lds + C::SCALE_OFF,
+                              lds + C::ROWS_OFF + (tile - first_tile) * BM * 4, M, N, sa, want_y, q_inv, q_max, Y, ACC, epi, sse, amax);
     if (++tile >= tile_end) break;  // block-uniform
   }
   finish_sums<C, EPI>(lds, wave, sse, amax, epi, blockIdx.x);
@@ -271,24 +273,26 @@ static int launch_quad(const DmaArgs& a) {
   using C = DmaCfg<BM, BN, WM, WN, NSTAGE, W4, 128>;
   using Kern = void (*)(const int8_t*, const void*, int64_t, int64_t, int64_t, const float*, const float*, int,
                         float*, int32_t*, EpiArgs, int, int, int, int);
-  static const Kern kerns[8] = {
+  static const Kern kerns[12] = {
       qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, false, 0>, qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, true, 0>,
       qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, false, 1>, qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, true, 1>,
       qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, false, 2>, qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, true, 2>,
-      qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, false, 3>, qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, true, 3>};
+      qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, false, 3>, qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, true, 3>,
+      qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, false, 4>, qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, true, 4>,
+      qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, false, 5>, qgemm_quad<BM, BN, WM, WN, NSTAGE, W4, true, 5>};
   static std::atomic<unsigned> done[kMaxDevices];
   if (a.prepare_only) {
-    for (int w = 0; w < 8; ++w) {
-      const int rc = allow_lds(reinterpret_cast<const void*>(kerns[w]), C::LDS_BYTES, done, w);
+    for (int w = 0; w < 12; ++w) {
+      const int rc = allow_lds(reinterpret_cast<const void*>(kerns[w]), C::LDS_BYTES + (w >= 8 ? C::ROWS_BYTES : 0), done, w);
       if (rc != MPQ_OK) return rc;
     }
     return MPQ_OK;
   }
   LaunchShape s;
-  int rc = launch_shape(BM, BN, C::LDS_BYTES, a.M, a.N, a.w_scale, a.per_row, a.y_out, a.acc_out, a.epi, 1, s);
-  if (rc == MPQ_OK) rc = allow_lds(reinterpret_cast<const void*>(kerns[s.which]), C::LDS_BYTES, done, s.which);
+  int rc = launch_shape(BM, BN, C::LDS_BYTES, C::ROWS_BYTES, a.M, a.N, a.w_scale, a.per_row, a.y_out, a.acc_out, a.epi, 1, s);
+  if (rc == MPQ_OK) rc = allow_lds(reinterpret_cast<const void*>(kerns[s.which]), s.lds, done, s.which);
   if (rc != MPQ_OK) return rc;
-  kerns[s.which]<<<(unsigned)s.grid, C::NT, C::LDS_BYTES, a.st>>>(a.a_q, a.w_q, a.M, a.N, a.K, a.a_scale, a.w_scale, a.per_row,
+  kerns[s.which]<<<(unsigned)s.grid, C::NT, s.lds, a.st>>>(a.a_q, a.w_q, a.M, a.N, a.K, a.a_scale, a.w_scale, a.per_row,
                                                                   a.y_out, a.acc_out, a.epi, (int)s.tn, (int)s.tm, s.chunk, s.remap);
   if (a.n_partials) *a.n_partials = s.grid;
   return launch_status();

@@ -29,6 +29,8 @@ EXPORTS = [
     "mpq_sse_pair_workspace_bytes", "mpq_sse_pair", "mpq_qgemm_score_workspace_bytes", "mpq_qgemm_score",
     "mpq_search_bisection", "mpq_search_greedy", "mpq_noise_inject_sweep",
     "mpq_fake_quant_scales", "mpq_scale_grad_workspace_bytes", "mpq_scale_grad", "mpq_scale_sgd_step", "mpq_qgemm_act", "mpq_qgemm_act_codes",
+    "mpq_token_quant", "mpq_qgemm_tokens", "mpq_linear_tokens_workspace_bytes", "mpq_linear_tokens",
+    "mpq_kv_append", "mpq_kv_gather", "mpq_kv_attention_workspace_bytes", "mpq_kv_attention",
     "mpq_diag_mfma_operand_bytes", "mpq_diag_mfma_rate", "mpq_diag_sweep_alu_rate", "mpq_fake_quant_step", "mpq_stack_evaluate_workspace_bytes", "mpq_stack_evaluate", "mpq_rademacher", "mpq_hutchinson_quad_workspace_bytes", "mpq_hutchinson_quad", "mpq_hutchinson_quad_signs",
 ]
 
@@ -109,6 +111,16 @@ def lib():
         L.mpq_stack_evaluate_workspace_bytes.argtypes = [vp, ci, i64]
         L.mpq_stack_evaluate_workspace_bytes.restype = C.c_size_t
         L.mpq_stack_evaluate.argtypes = [vp, ci, i64, vp, ci, ci, ci, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.mpq_token_quant.argtypes = [vp, ci, i64, i64, i64, ci, vp, vp, vp]
+        L.mpq_qgemm_tokens.argtypes = [vp, vp, ci, i64, i64, i64, vp, vp, ci, ci, ci, vp, vp]
+        L.mpq_linear_tokens_workspace_bytes.restype = sz
+        L.mpq_linear_tokens_workspace_bytes.argtypes = [i64, i64]
+        L.mpq_linear_tokens.argtypes = [vp, ci, i64, i64, i64, i64, ci, vp, ci, vp, ci, ci, ci, vp, vp, sz, vp]
+        L.mpq_kv_append.argtypes = [vp, vp, ci, vp, i64, i64, vp, i64, i64, vp]
+        L.mpq_kv_gather.argtypes = [vp, vp, ci, vp, vp, vp]
+        L.mpq_kv_attention_workspace_bytes.restype = sz
+        L.mpq_kv_attention_workspace_bytes.argtypes = [vp, vp, ci]
+        L.mpq_kv_attention.argtypes = [vp, vp, ci, vp, i64, i64, ci, C.c_float, ci, i64, vp, i64, i64, vp, sz, vp]
         L.mpq_rademacher.argtypes = [C.c_uint64, C.c_uint64, i64, i64, vp, vp]
         L.mpq_hutchinson_quad_workspace_bytes.argtypes = [i64, i64, i64]
         L.mpq_hutchinson_quad_workspace_bytes.restype = C.c_size_t
@@ -786,3 +798,243 @@ def qgemm_act_codes(a_q, w_q, a_scale, w_scale, act, absmax, bits, w_storage_bit
                                      w_gran, int(act), _ptr(absmax), int(bits), _ptr(codes), _stream()),
            "mpq_qgemm_act_codes")
     return codes
+
+
+# ---------------------------------------------------------------------------------------------
+# Serving a quantized model.  These calls take tensors of the current device only, and where they need scratch and
+# the caller gives none they take it from torch's allocator for the one call: two streams, or two captured graphs, never
+# share it.
+F32, BF16, F16 = 0, 1, 2
+_types = None
+
+
+def _type(dtype) -> int:
+    global _types
+    if _types is None:
+        torch = _torch()
+        _types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    try:
+        return _types[dtype]
+    except KeyError:
+        raise ValueError("expected float32, bfloat16 or float16, got %s" % (dtype,)) from None
+
+
+def _on_current(*tensors):
+    """All on the current device, whose current stream the call goes to."""
+    device = _torch().cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != device):
+            raise ValueError("libmpq works on tensors of the current device")
+
+
+def _dense(t, dtype, shape, what):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous %s tensor of shape %s" % (what, dtype, tuple(shape)))
+    return t
+
+
+def _scratch(ws, nbytes, device):
+    """(pointer, bytes, what keeps it alive)."""
+    if nbytes == 0:
+        return None, 0, None
+    if ws is not None:
+        return (*ws.get(nbytes), ws)
+    buf = _torch().empty(nbytes, dtype=_torch().uint8, device=device)
+    return buf.data_ptr(), nbytes, buf
+
+
+def _rows2d(x):
+    """(type, rows, columns, elements between rows) of a 2-D tensor whose columns are contiguous."""
+    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+        raise ValueError("expected a 2-D tensor with contiguous rows")
+    M, K = x.shape
+    return _type(x.dtype), M, K, x.stride(0) if M > 1 else K
+
+
+def _weights(w_q, w_scale, w_storage_bits, w_gran, K):
+    """Rows of the weights, whose tensors have to fit the layer: kernels trust the sizes they are told."""
+    torch = _torch()
+    if w_storage_bits not in (4, 8):
+        return w_q.shape[0]       # refused by the library
+    N = w_q.shape[0]
+    if w_q.dim() != 2 or w_q.shape[1] * 8 != K * w_storage_bits or not w_q.is_contiguous() or w_q.element_size() != 1:
+        raise ValueError("expected contiguous weight codes of shape [N, %s]" % ("K" if w_storage_bits == 8 else "K / 2"))
+    if w_scale.dtype != torch.float32 or w_scale.numel() != (1 if w_gran == PER_TENSOR else N) or not w_scale.is_contiguous():
+        raise ValueError("expected one float32 weight step per tensor or per output channel")
+    return N
+
+
+def token_quant(x, bits=8, codes=None, scale=None):
+    """Eq. 1 with a step per row: x [M, K] (float32, bfloat16 or float16, rows contiguous).  Returns
+    (codes int8 [M, K], scale float32 [M])."""
+    torch = _torch()
+    t, M, K, stride = _rows2d(x)
+    _on_current(x, codes, scale)
+    codes = torch.empty((M, K), dtype=torch.int8, device=x.device) if codes is None else _dense(codes, torch.int8, (M, K), "codes")
+    scale = torch.empty(M, dtype=torch.float32, device=x.device) if scale is None else _dense(scale, torch.float32, (M,), "scale")
+    _check(lib().mpq_token_quant(_ptr(x), t, M, K, stride, int(bits), _ptr(codes), _ptr(scale), _stream()), "mpq_token_quant")
+    return codes, scale
+
+
+def qgemm_tokens(a_q, w_q, a_scale, w_scale, w_storage_bits=8, w_gran=PER_ROW, act=ACT_NONE, dtype=None, y=None):
+    """The quantized linear layer with a step per token and per output channel: a_q int8 [M, K], a_scale float32 [M].
+    Returns Y [M, N] of `dtype` (float32 where neither it nor y is given)."""
+    torch = _torch()
+    a_q = _dev2d(a_q, torch.int8)
+    M, K = a_q.shape
+    _on_current(a_q, w_q, a_scale, w_scale, y)
+    _dense(a_scale, torch.float32, (M,), "a_scale")
+    N = _weights(w_q, w_scale, w_storage_bits, w_gran, K)
+    dtype = dtype or (torch.float32 if y is None else y.dtype)
+    y = torch.empty((M, N), dtype=dtype, device=a_q.device) if y is None else _dense(y, dtype, (M, N), "y")
+    _check(lib().mpq_qgemm_tokens(_ptr(a_q), _ptr(w_q), w_storage_bits, M, N, K, _ptr(a_scale), _ptr(w_scale), w_gran, int(act),
+                                  _type(dtype), _ptr(y), _stream()), "mpq_qgemm_tokens")
+    return y
+
+
+def linear_tokens_workspace_bytes(M, K) -> int:
+    return int(lib().mpq_linear_tokens_workspace_bytes(M, K))
+
+
+def linear_tokens(x, w_q, w_scale, w_storage_bits=8, w_gran=PER_ROW, bits=8, act=ACT_NONE, dtype=None, y=None,
+                  ws: Workspace = None):
+    """A linear layer from its input to its output: token_quant(x, bits) and qgemm_tokens in one call.  Returns Y [M, N]
+    of `dtype` (x's where neither it nor y is given)."""
+    torch = _torch()
+    t, M, K, stride = _rows2d(x)
+    _on_current(x, w_q, w_scale, y)
+    N = _weights(w_q, w_scale, w_storage_bits, w_gran, K)
+    dtype = dtype or (x.dtype if y is None else y.dtype)
+    y = torch.empty((M, N), dtype=dtype, device=x.device) if y is None else _dense(y, dtype, (M, N), "y")
+    wp, wn, _alive = _scratch(ws, linear_tokens_workspace_bytes(M, K), x.device)
+    _check(lib().mpq_linear_tokens(_ptr(x), t, M, N, K, stride, int(bits), _ptr(w_q), w_storage_bits, _ptr(w_scale), w_gran,
+                                   int(act), _type(dtype), _ptr(y), wp, wn, _stream()), "mpq_linear_tokens")
+    return y
+
+
+class _KvCacheStruct(C.Structure):
+    """mpq_kv_cache of include/mpq.h."""
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_absmax", C.c_void_p), ("v_absmax", C.c_void_p),
+                ("pages", C.c_int64), ("heads", C.c_int), ("dim", C.c_int), ("page", C.c_int), ("bits", C.c_int)]
+
+
+class _KvBatchStruct(C.Structure):
+    """mpq_kv_batch of include/mpq.h."""
+    _fields_ = [("starts", C.c_void_p), ("kv_len", C.c_void_p), ("table", C.c_void_p), ("rows", C.c_int64),
+                ("max_new", C.c_int64), ("max_len", C.c_int64), ("seqs", C.c_int), ("table_pages", C.c_int)]
+
+
+class KvCache:
+    """A cache of quantized pages over the caller's tensors (kept alive): k_codes int8 [pages, heads, page, dim], v_codes
+    int8 [pages, heads, page / 4, dim, 4], k_absmax and v_absmax float32 [pages, heads]."""
+
+    def __init__(self, k_codes, v_codes, k_absmax, v_absmax, bits=8):
+        torch = _torch()
+        if k_codes.dim() != 4:
+            raise ValueError("k_codes: expected [pages, heads, page, dim]")
+        pages, heads, page, dim = k_codes.shape
+        _dense(k_codes, torch.int8, k_codes.shape, "k_codes")
+        _dense(v_codes, torch.int8, (pages, heads, page // 4, dim, 4), "v_codes")
+        _dense(k_absmax, torch.float32, (pages, heads), "k_absmax")
+        _dense(v_absmax, torch.float32, (pages, heads), "v_absmax")
+        self.k_codes, self.v_codes, self.k_absmax, self.v_absmax = k_codes, v_codes, k_absmax, v_absmax
+        self.pages, self.heads, self.page, self.dim, self.bits = pages, heads, page, dim, int(bits)
+        self.device = k_codes.device
+        if any(t.device != self.device for t in (v_codes, k_absmax, v_absmax)):
+            raise ValueError("the cache's tensors lie on one device")
+        self.struct = _KvCacheStruct(_ptr(k_codes), _ptr(v_codes), _ptr(k_absmax), _ptr(v_absmax), pages, heads, dim, page, self.bits)
+        self.ref = C.byref(self.struct)
+
+    @classmethod
+    def empty(cls, pages, heads, page, dim, bits=8, device=None):
+        torch = _torch()
+        device = device or torch.device("cuda", torch.cuda.current_device())
+        codes = (torch.empty(s, dtype=torch.int8, device=device) for s in ((pages, heads, page, dim), (pages, heads, page // 4, dim, 4)))
+        absmax = (torch.empty((pages, heads), dtype=torch.float32, device=device) for _ in range(2))
+        return cls(*codes, *absmax, bits)
+
+
+class KvBatch:
+    """The sequences of a call over the caller's device tensors (kept alive, and read when a call's kernels run, so that a
+    program may go on writing new lengths into them): starts int32 [seqs + 1], kv_len int32 [seqs], table int32
+    [seqs, table_pages]; rows of the calls' tensors; max_new and max_len bound the new and all tokens of a sequence
+    (where not given: rows, and what the table has places for)."""
+
+    def __init__(self, starts, kv_len, table, rows, max_new=None, max_len=None):
+        torch = _torch()
+        if table.dim() != 2:
+            raise ValueError("table: expected [seqs, pages]")
+        seqs = table.shape[0]
+        _dense(table, torch.int32, table.shape, "table")
+        _dense(starts, torch.int32, (seqs + 1,), "starts")
+        _dense(kv_len, torch.int32, (seqs,), "kv_len")
+        self.starts, self.kv_len, self.table, self.rows = starts, kv_len, table, int(rows)
+        self.device = table.device
+        if starts.device != self.device or kv_len.device != self.device:
+            raise ValueError("the batch's tensors lie on one device")
+        self.max_new = self.rows if max_new is None else int(max_new)
+        self.max_len = 2 ** 31 - 1 if max_len is None else int(max_len)
+        self.struct = _KvBatchStruct(_ptr(starts), _ptr(kv_len), _ptr(table), self.rows, self.max_new, self.max_len, seqs, table.shape[1])
+        self.ref = C.byref(self.struct)
+
+
+def _kv_rows(cache, batch, x, heads, what):
+    """(type, elements between tokens, elements between heads) of a call's tensor [rows, heads, dim]."""
+    if cache.device != batch.device or x.device != cache.device:
+        raise ValueError("cache, batch and tensors lie on one device")
+    if x.dim() != 3 or x.shape[0] != batch.rows or x.shape[2] != cache.dim or (heads is not None and x.shape[1] != heads) \
+            or x.stride(2) != 1:
+        raise ValueError("%s: expected [%d, %s, %d] with contiguous channels" % (what, batch.rows, heads or "heads", cache.dim))
+    return _type(x.dtype), x.stride(0), x.stride(1)
+
+
+def kv_append(cache: KvCache, batch: KvBatch, k, v):
+    """Writes the rows of k and v ([rows, heads, dim], any strides of tokens and heads) into the cache."""
+    t, k_ts, k_hs = _kv_rows(cache, batch, k, cache.heads, "k")
+    tv, v_ts, v_hs = _kv_rows(cache, batch, v, cache.heads, "v")
+    if tv != t:
+        raise ValueError("k and v have one type")
+    _on_current(k)
+    _check(lib().mpq_kv_append(cache.ref, batch.ref, t, _ptr(k), k_ts, k_hs, _ptr(v), v_ts, v_hs, _stream()), "mpq_kv_append")
+
+
+def kv_gather(cache: KvCache, batch: KvBatch, dtype=None, want_k=True, want_v=True, k=None, v=None):
+    """The stored values of the batch's rows.  Returns (k | None, v | None), [rows, heads, dim] of `dtype` (float32)."""
+    torch = _torch()
+    dtype = dtype or next((t.dtype for t in (k, v) if t is not None), torch.float32)
+    shape = (batch.rows, cache.heads, cache.dim)
+    if cache.device != batch.device:
+        raise ValueError("cache and batch lie on one device")
+    _on_current(cache.k_codes, k, v)
+    if k is not None:
+        _dense(k, dtype, shape, "k")
+    elif want_k:
+        k = torch.empty(shape, dtype=dtype, device=cache.device)
+    if v is not None:
+        _dense(v, dtype, shape, "v")
+    elif want_v:
+        v = torch.empty(shape, dtype=dtype, device=cache.device)
+    _check(lib().mpq_kv_gather(cache.ref, batch.ref, _type(dtype), _ptr(k), _ptr(v), _stream()), "mpq_kv_gather")
+    return k, v
+
+
+def kv_attention_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads) -> int:
+    return int(lib().mpq_kv_attention_workspace_bytes(cache.ref, batch.ref, q_heads))
+
+
+def kv_attention(cache: KvCache, batch: KvBatch, q, causal=True, window=0, softmax_scale=None, out=None, ws: Workspace = None):
+    """Attention of q [rows, q_heads, dim] (any strides of tokens and heads) over the cache, q_heads a multiple of the cache's
+    heads.  softmax_scale: 1 / sqrt(dim) where not given.  Returns the output, [rows, q_heads, dim] of q's type."""
+    t, q_ts, q_hs = _kv_rows(cache, batch, q, None, "q")
+    heads = q.shape[1]
+    if out is None:
+        out = _torch().empty((batch.rows, heads, cache.dim), dtype=q.dtype, device=q.device)
+    to, o_ts, o_hs = _kv_rows(cache, batch, out, heads, "out")
+    if to != t:
+        raise ValueError("q and out have one type")
+    _on_current(q)
+    wp, wn, _alive = _scratch(ws, kv_attention_workspace_bytes(cache, batch, heads), q.device)
+    _check(lib().mpq_kv_attention(cache.ref, batch.ref, t, _ptr(q), q_ts, q_hs, heads,
+                                  cache.dim ** -0.5 if softmax_scale is None else float(softmax_scale), int(bool(causal)), int(window),
+                                  _ptr(out), o_ts, o_hs, wp, wn, _stream()), "mpq_kv_attention")
+    return out

@@ -1,0 +1,242 @@
+"""Refusals of the serving calls, found on the host before anything is launched, and their plain references."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import serving
+from paper_2302_01382_amd import mpq
+from test_abi_host import FAKE, FAKE16, needs_no_gpu
+
+ODD = C.c_void_p(0x10001)
+BIG = 1 << 30
+
+
+@needs_no_gpu
+def test_token_quant_refuses():
+    f = mpq.lib().mpq_token_quant
+    assert f(None, 1, 4, 8, 8, 8, FAKE, FAKE, None) == mpq.ERR_NULL
+    assert f(FAKE, 1, 4, 8, 8, 8, None, FAKE, None) == mpq.ERR_NULL
+    assert f(FAKE, 1, 4, 8, 8, 8, FAKE, None, None) == mpq.ERR_NULL
+    for t in (-1, 3):
+        assert f(FAKE, t, 4, 8, 8, 8, FAKE, FAKE, None) == mpq.ERR_SHAPE
+    assert f(FAKE, 1, -1, 8, 8, 8, FAKE, FAKE, None) == mpq.ERR_SHAPE
+    assert f(FAKE, 1, 4, 0, 8, 8, FAKE, FAKE, None) == mpq.ERR_SHAPE
+    assert f(FAKE, 1, 4, 8, 7, 8, FAKE, FAKE, None) == mpq.ERR_SHAPE      # rows overlap
+    assert f(FAKE, 1, 2 ** 40, 8, 2 ** 40, 8, FAKE, FAKE, None) == mpq.ERR_SHAPE
+    for bits in (1, 9):
+        assert f(FAKE, 1, 4, 8, 8, bits, FAKE, FAKE, None) == mpq.ERR_BITS
+    assert f(ODD, 1, 4, 8, 8, 8, FAKE, FAKE, None) == mpq.ERR_ALIGN
+    assert f(C.c_void_p(0x10002), 0, 4, 8, 8, 8, FAKE, FAKE, None) == mpq.ERR_ALIGN
+    assert f(FAKE, 1, 4, 8, 8, 8, FAKE, ODD, None) == mpq.ERR_ALIGN
+    assert f(None, 1, 0, 8, 8, 8, None, None, None) == mpq.OK             # no tokens
+
+
+@needs_no_gpu
+def test_qgemm_tokens_refuses():
+    f = mpq.lib().mpq_qgemm_tokens
+    ok = [FAKE16, FAKE16, 8, 4, 8, 16, FAKE, FAKE, 1, 0, 0, FAKE16, None]
+
+    def but(**kw):
+        a = list(ok)
+        for i, v in kw.items():
+            a[int(i[1:])] = v
+        return f(*a)
+
+    for i in (0, 1, 6, 7, 11):
+        assert but(**{"_%d" % i: None}) == mpq.ERR_NULL
+    assert but(_2=5) == mpq.ERR_BITS
+    for i in (4, 5):
+        for v in (0, -3):
+            assert but(**{"_%d" % i: v}) == mpq.ERR_SHAPE
+    assert but(_3=-1) == mpq.ERR_SHAPE
+    assert but(_5=133144) == mpq.ERR_SHAPE
+    assert but(_2=4, _5=17) == mpq.ERR_SHAPE
+    assert but(_3=2 ** 31, _4=2 ** 31) == mpq.ERR_SHAPE
+    assert but(_8=2) == mpq.ERR_GRAN
+    for act in (-1, 3):
+        assert but(_9=act) == mpq.ERR_SHAPE
+    assert but(_10=3) == mpq.ERR_SHAPE
+    assert but(_6=C.c_void_p(0x1002)) == mpq.ERR_ALIGN
+    assert but(_7=C.c_void_p(0x1002)) == mpq.ERR_ALIGN
+    assert but(_11=C.c_void_p(0x10002)) == mpq.ERR_ALIGN                   # fp32 output
+    assert but(_10=1, _11=ODD) == mpq.ERR_ALIGN
+    assert but(_3=0, _0=None, _6=None, _11=None) == mpq.OK
+    assert but(_3=0, _1=None) == mpq.ERR_NULL and but(_3=0, _5=0) == mpq.ERR_SHAPE
+
+
+@needs_no_gpu
+def test_linear_tokens_refuses():
+    L = mpq.lib()
+    q, f = L.mpq_linear_tokens_workspace_bytes, L.mpq_linear_tokens
+    assert q(3, 17) == 64 + 12 and q(0, 17) == 0 and q(3, 0) == 0 and q(-1, 4) == 0 and q(2 ** 40, 2 ** 40) == 0
+    ok = [FAKE16, 1, 4, 8, 16, 16, 8, FAKE16, 8, FAKE, 1, 0, 1, FAKE16, FAKE16, BIG, None]
+
+    def but(**kw):
+        a = list(ok)
+        for i, v in kw.items():
+            a[int(i[1:])] = v
+        return f(*a)
+
+    for i in (0, 7, 9, 13):
+        assert but(**{"_%d" % i: None}) == mpq.ERR_NULL
+    assert but(_14=None) == mpq.ERR_WORKSPACE and but(_15=q(4, 16) - 1) == mpq.ERR_WORKSPACE
+    assert but(_14=C.c_void_p(0x10008)) == mpq.ERR_ALIGN
+    assert but(_6=1) == mpq.ERR_BITS and but(_8=3) == mpq.ERR_BITS
+    assert but(_5=15) == mpq.ERR_SHAPE and but(_1=7) == mpq.ERR_SHAPE and but(_12=7) == mpq.ERR_SHAPE and but(_3=0) == mpq.ERR_SHAPE
+    assert but(_2=0, _0=None, _13=None, _14=None, _15=0) == mpq.OK
+
+
+def kv(cache=None, batch=None):
+    c = dict(k_codes=0x10000, v_codes=0x10000, k_absmax=0x1000, v_absmax=0x1000, pages=10, heads=2, dim=64, page=16, bits=8)
+    b = dict(starts=0x1000, kv_len=0x1000, table=0x1000, rows=6, max_new=3, max_len=100, seqs=2, table_pages=4)
+    c.update(cache or {})
+    b.update(batch or {})
+    return C.byref(mpq._KvCacheStruct(**c)), C.byref(mpq._KvBatchStruct(**b))
+
+
+def calls():
+    L = mpq.lib()
+    return [lambda c, b, t=1, x=FAKE16: L.mpq_kv_append(c, b, t, x, 128, 64, FAKE16, 128, 64, None),
+            lambda c, b, t=1, x=FAKE16: L.mpq_kv_gather(c, b, t, x, x, None),
+            lambda c, b, t=1, x=FAKE16: L.mpq_kv_attention(c, b, t, x, 256, 64, 4, 0.125, 1, 0, FAKE16, 256, 64, FAKE16, BIG, None)]
+
+
+@needs_no_gpu
+@pytest.mark.parametrize("which", range(3))
+def test_kv_calls_refuse(which):
+    f = calls()[which]
+    assert f(None, kv()[1]) == mpq.ERR_NULL and f(kv()[0], None) == mpq.ERR_NULL
+    for n in ("k_codes", "v_codes", "k_absmax", "v_absmax"):
+        assert f(*kv({n: None})) == mpq.ERR_NULL
+        assert f(*kv({n: 0x10002})) == mpq.ERR_ALIGN
+    assert f(*kv({"k_codes": 0x10008})) == mpq.ERR_ALIGN
+    for n in ("starts", "kv_len", "table"):
+        assert f(*kv(batch={n: None})) == mpq.ERR_NULL
+        assert f(*kv(batch={n: 0x1002})) == mpq.ERR_ALIGN
+    for n in ("pages", "heads", "dim", "page"):
+        assert f(*kv({n: 0})) == mpq.ERR_SHAPE and f(*kv({n: -16})) == mpq.ERR_SHAPE
+    for dim in (8, 24, 272):
+        assert f(*kv({"dim": dim})) == mpq.ERR_SHAPE
+    for page in (8, 48, 256):
+        assert f(*kv({"page": page})) == mpq.ERR_SHAPE
+    assert f(*kv({"pages": 1 << 45})) == mpq.ERR_SHAPE
+    for bits in (1, 9):
+        assert f(*kv({"bits": bits})) == mpq.ERR_BITS
+    for n in ("rows", "seqs", "max_new", "max_len", "table_pages"):
+        assert f(*kv(batch={n: -1})) == mpq.ERR_SHAPE
+    for n in ("rows", "max_new", "max_len"):
+        assert f(*kv(batch={n: 1 << 31})) == mpq.ERR_SHAPE
+    assert f(*kv(batch={"table_pages": 0})) == mpq.ERR_SHAPE
+    assert f(*kv(), t=3) == mpq.ERR_SHAPE
+    assert f(*kv(), x=None) == mpq.ERR_NULL
+    assert f(*kv(), x=ODD) == mpq.ERR_ALIGN and f(*kv(), t=0, x=C.c_void_p(0x10002)) == mpq.ERR_ALIGN
+    assert f(*kv(batch={"rows": 0}), x=None) == mpq.OK
+    assert f(*kv(batch={"seqs": 0, "starts": None, "kv_len": None, "table": None}), x=None) == mpq.OK
+    # grids that a launch cannot count
+    assert f(*kv(batch={"seqs": 2 ** 31 - 1, "rows": 2 ** 31 - 1, "max_new": 2 ** 31 - 1, "table_pages": 2 ** 31 - 1})) == mpq.ERR_SHAPE
+
+
+@needs_no_gpu
+def test_kv_append_refuses_strides():
+    f = mpq.lib().mpq_kv_append
+    for i in range(4):
+        s = [128, 64, 128, 64]
+        s[i] = -1
+        assert f(*kv(), 1, FAKE16, s[0], s[1], FAKE16, s[2], s[3], None) == mpq.ERR_SHAPE
+        s[i] = 1 << 62
+        assert f(*kv(), 1, FAKE16, s[0], s[1], FAKE16, s[2], s[3], None) == mpq.ERR_SHAPE
+    assert f(*kv(), 1, FAKE16, 128, 64, None, 128, 64, None) == mpq.ERR_NULL
+
+
+@needs_no_gpu
+def test_kv_attention_refuses():
+    L = mpq.lib()
+    q = L.mpq_kv_attention_workspace_bytes
+    ok = [1, FAKE16, 256, 64, 4, 0.125, 1, 0, FAKE16, 256, 64, FAKE16, BIG, None]
+
+    def but(batch=None, **kw):
+        a = list(ok)
+        for i, v in kw.items():
+            a[int(i[1:])] = v
+        return L.mpq_kv_attention(*kv(batch=batch), *a)
+
+    for heads in (0, -2, 3):
+        assert but(_4=heads) == mpq.ERR_SHAPE and q(*kv(), heads) == 0
+    for scale in (float("nan"), float("inf"), -float("inf")):
+        assert but(_5=scale) == mpq.ERR_SHAPE
+    assert but(_7=-1) == mpq.ERR_SHAPE and but(_6=0, _7=5) == mpq.ERR_SHAPE
+    for i in (2, 3, 9, 10):
+        assert but(**{"_%d" % i: -1}) == mpq.ERR_SHAPE and but(**{"_%d" % i: 1 << 62}) == mpq.ERR_SHAPE
+    assert but(_8=None) == mpq.ERR_NULL and but(_8=ODD) == mpq.ERR_ALIGN
+    long = {"max_len": 100000, "table_pages": 7000}
+    need = q(*kv(batch=long), 4)
+    assert need > 0 and q(*kv(), 4) == 0
+    assert but(long, _11=None) == mpq.ERR_WORKSPACE and but(long, _12=need - 1) == mpq.ERR_WORKSPACE
+    assert but(long, _11=C.c_void_p(0x10008)) == mpq.ERR_ALIGN
+    assert q(*kv({"bits": 1}, long), 4) == 0 and q(None, kv()[1], 4) == 0
+
+
+def test_the_binding_refuses():
+    """What the C calls cannot see: sizes of tensors, devices, types."""
+    import torch
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="current device|CUDA|2-D") if torch.cuda.is_available() else pytest.raises(Exception):
+        mpq.token_quant(x)
+    for bad in (torch.zeros(4), torch.zeros(4, 8, dtype=torch.float64), torch.zeros(4, 16)[:, ::2]):
+        with pytest.raises(ValueError):
+            mpq.token_quant(bad)
+    w, s = torch.zeros(6, 8, dtype=torch.int8), torch.zeros(6)
+    assert mpq._weights(w, s, 8, mpq.PER_ROW, 8) == 6 and mpq._weights(w, s[:1], 4, mpq.PER_TENSOR, 16) == 6
+    for w_, s_, bits, gran, k in ((w, s, 8, mpq.PER_ROW, 9), (w, s, 4, mpq.PER_ROW, 8), (w, s[:5], 8, mpq.PER_ROW, 8), (w, s, 8, mpq.PER_TENSOR, 8),
+                                  (w.t(), s, 8, mpq.PER_ROW, 6), (w.float(), s, 8, mpq.PER_ROW, 8), (w, s.double(), 8, mpq.PER_ROW, 8)):
+        with pytest.raises(ValueError):
+            mpq._weights(w_, s_, bits, gran, k)
+    k, v = torch.zeros(3, 2, 16, 64, dtype=torch.int8), torch.zeros(3, 2, 4, 64, 4, dtype=torch.int8)
+    m = torch.zeros(3, 2)
+    cache = mpq.KvCache(k, v, m, m.clone())
+    for bad in ((k[0], v, m, m), (k, v.transpose(2, 3), m, m), (k, v, m[:2], m), (k, v, m, m.double()), (k.float(), v, m, m)):
+        with pytest.raises(ValueError):
+            mpq.KvCache(*bad)
+    i32 = torch.int32
+    table, lens, starts = torch.zeros(2, 5, dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(3, dtype=i32)
+    batch = mpq.KvBatch(starts, lens, table, 4)
+    assert batch.max_new == 4
+    for bad in ((lens, lens, table), (starts, starts, table), (starts, lens, table[0]), (starts.long(), lens, table), (starts, lens, table.t())):
+        with pytest.raises(ValueError):
+            mpq.KvBatch(*bad, 4)
+    good = torch.zeros(4, 2, 64)
+    for bad in (good[:3], good[:, :1], good[..., :32], good.transpose(1, 2), good.double()):
+        with pytest.raises(ValueError):
+            mpq._kv_rows(cache, batch, bad, 2, "k")
+    with pytest.raises(ValueError):
+        mpq.kv_append(cache, batch, good, good.half())
+
+
+# ---- the references themselves --------------------------------------------------------------------------------------
+def test_reference_codes_by_hand():
+    codes, scale = serving.token_quant(np.array([[1.0, -2.0, 0.5, 0.0], [0, 0, 0, 0]], np.float32), 3)   # qmax 3, inv 1.5
+    np.testing.assert_array_equal(codes, [[2, -3, 1, 0], [0, 0, 0, 0]])                                   # 1.5 -> 2, 0.75 -> 1
+    np.testing.assert_array_equal(scale, np.array([np.float32(2) / np.float32(3), 0], np.float32))
+
+
+def test_reference_cache_by_hand():
+    """One head, one channel group: a page's maximum grows from 3 to 6 at 3 bits, the codes there are halved with ties to
+    even, and attention over two equal keys is the mean of their values."""
+    c = serving.Cache(2, 1, 16, 16, 3)
+    x = np.zeros((2, 1, 16), np.float32)
+    x[0, 0, :4] = [3, 2, 1, -3]
+    x[1, 0, :4] = [6, 0, 3, 1]
+    table = np.array([[1]])
+    c.append([0, 1], [1], table, x[:1], x[:1])
+    assert c.codes["k"][1, 0, 0, :4].tolist() == [3, 2, 1, -3] and c.absmax["k"][1, 0] == 3
+    c.append([0, 1], [2], table, x[1:], x[1:])
+    assert c.codes["v"][1, 0, 0, :4].tolist() == [2, 1, 0, -2] and c.absmax["v"][1, 0] == 6       # 1.5 -> 2, 1, 0.5 -> 0
+    assert c.codes["k"][1, 0, 1, :4].tolist() == [3, 0, 2, 0]
+    k, v = c.gather([0, 2], [2], table, 2)
+    assert k[0, 0, :4].tolist() == [4, 2, 0, -4] and v[1, 0, :4].tolist() == [6, 0, 4, 0]
+    out, _, big = c.attention([0, 1], [2], table, np.zeros((1, 1, 16), np.float32), True, 0, 1.0)
+    np.testing.assert_allclose(out[0, 0, :4], [5, 1, 2, -2])
+    assert big[0, 0] == 6
+    packed = serving.packed_values(c.codes["v"])
+    assert packed.shape == (2, 1, 4, 16, 4) and packed[1, 0, 0, 0].tolist() == [2, 3, 0, 0]
