@@ -14,8 +14,9 @@
 //
 // Precision: logits, maxima, sums and outputs are fp32.  q goes in as fp16 after a scaling by a power of two (its row's
 // largest entry to 2^14: bf16 and fp16 keep every bit down to 2^-28 of that entry), fp32 as two such terms (22 bits).
-// Probabilities, at most 1, go in as fp16 times 2^14 (rounded by 2^-11, like an fp16 output), for
-// fp32 as two terms.  Values' maxima differ from page to page: probabilities carry them relative to a power of two that is
+// Probabilities, at most 1, go in as fp16 times 2^14: as one term for bf16 (2^-11, an eighth of the output's rounding), as two
+// for the others (with one, an fp16 output's distance to 64 bits went from 2.1e-4 to 3.1e-4; the step has room for the
+// products).  Values' maxima differ from page to page: probabilities carry them relative to a power of two that is
 // at least the largest maximum so far, an exact rescaling whenever it grows.
 #include "kv.hpp"
 
@@ -67,19 +68,21 @@ struct Span {
 
 template <int T, int DH>
 struct AttnShape {
-  static constexpr int TERMS = T == MPQ_F32 ? 2 : 1;
+  static constexpr int QT = T == MPQ_F32 ? 2 : 1;   // fp16 terms of q
+  static constexpr int PT = T == MPQ_BF16 ? 1 : 2;  // ... of a probability
   static constexpr int TT = DH <= 2 ? 64 : 32;  // tokens per step
   static constexpr int NS = TT / 16;
   static constexpr int DP = DH * 64;
 };
 
 // grid: ((sequence * heads + head) * row_tiles + tile) * splits + split.  DH: dim in units of 64, rounded up.
-template <int T, int DH>
+// ONE: a page holds at least a step's tokens, which then lie on one page.
+template <int T, int DH, bool ONE>
 __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
   using S = AttnShape<T, DH>;
   using E = Elem<T>;
   typedef typename E::type El;
-  constexpr int TERMS = S::TERMS, TT = S::TT, NS = S::NS, DP = S::DP, NW = kAttnWaves;
+  constexpr int QT = S::QT, PT = S::PT, TT = S::TT, NS = S::NS, DP = S::DP, NW = kAttnWaves, NP = ONE ? 1 : NS;
   __shared__ float sm_m[NW][16], sm_l[NW][16];
   __shared__ __attribute__((aligned(16))) float sm_o[NW / 2][16][DP + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -131,7 +134,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
   }
 
   // q: lane (row, quarter) holds channels 64 c + 16 quarter .. + 15 for every c, as the keys come
-  f16x8 q[TERMS][2 * DH];
+  f16x8 q[QT][2 * DH];
   float row_scale;
   {
     const El* row = reinterpret_cast<const El*>(a.q) + (sq.row0 + i) * a.q_ts + (int64_t)qh * a.q_hs;
@@ -154,7 +157,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
         const float x = __builtin_ldexpf(v[c][e], e2);
         const _Float16 top = (_Float16)x;
         q[0][c][e] = top;
-        if (TERMS == 2) q[TERMS - 1][c][e] = (_Float16)(x - (float)top);
+        if (QT == 2) q[QT - 1][c][e] = (_Float16)(x - (float)top);
       }
     // logits in units of log 2
     const float qmax = (float)((1 << (a.c.bits - 1)) - 1);
@@ -169,6 +172,50 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
   const int64_t page_bytes = (int64_t)a.c.page * D;
   const int shift = 31 - __builtin_clz((unsigned)a.c.page);
 
+  // What a step needs of its tokens, by page: NP pages of TT / NP tokens each.  Pages are looked up a step ahead of the
+  // codes they hold, codes are requested a step ahead of the products.
+  int id[NP];
+  auto look_up = [&](int64_t t) {
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+      const int64_t tok = t * TT + u * (TT / NP);
+      id[u] = t < t1 && tok < span.hi ? table[tok >> shift] : -1;
+    }
+  };
+  const int8_t *kp[NP], *vp[NP];
+  float mk[NP], mv[NP];
+  auto locate = [&](int64_t t) {
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+      const bool ok = id[u] >= 0 && id[u] < a.c.pages;
+      const int64_t at = (int64_t)(ok ? id[u] : 0) * a.c.heads + h;
+      const int place = (int)((t * TT + u * (TT / NP)) & (a.c.page - 1));
+      kp[u] = a.c.k_codes + at * page_bytes + place * D;
+      vp[u] = a.c.v_codes + at * page_bytes + place * D;
+      mk[u] = ok ? a.c.k_absmax[at] : -1.0f;
+      mv[u] = ok ? a.c.v_absmax[at] : 0.0f;
+    }
+  };
+  v4i kw[NS][DH], vw[NS][DH];
+  auto request_k = [&]() {
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+#pragma unroll
+      for (int c = 0; c < DH; ++c) {
+        const int d = c * 64 + quarter * 16;
+        kw[u][c] = d < D ? *reinterpret_cast<const v4i*>(kp[u / (NS / NP)] + (u % (NS / NP) * 16 + r) * D + d) : v4i{0, 0, 0, 0};
+      }
+  };
+  auto request_v = [&]() {
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+#pragma unroll
+      for (int c = 0; c < DH; ++c) {
+        const int d = c * 64 + r * 4;
+        vw[u][c] = d < D ? *reinterpret_cast<const v4i*>(vp[u / (NS / NP)] + u % (NS / NP) * 16 * D + (quarter * D + d) * 4) : v4i{0, 0, 0, 0};
+      }
+  };
+
   float m_run = -__builtin_inff(), l_run = 0.0f;
   int v_exp = -100000;  // O' is in units of 2^(v_exp - kPBits)
   f32x4 o[DH][4];
@@ -177,52 +224,51 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) o[c][k] = f32x4{0, 0, 0, 0};
 
-  for (int64_t t = t0 + wave; t < t1; t += NW) {
+  int64_t t = t0 + wave;
+  if (t < t1) {
+    look_up(t);
+    locate(t);
+    request_k();
+    request_v();
+    look_up(t + NW);
+  }
+  for (; t < t1; t += NW) {
     const int64_t base = t * TT;
-    const int8_t *kp[NS], *vp[NS];
-    float mk[NS], mv[NS];
-    bool bad = false;
-#pragma unroll
-    for (int u = 0; u < NS; ++u) {
-      const int64_t tok = base + u * 16;
-      const bool in = tok < span.hi;
-      const int64_t id0 = in ? table[tok >> shift] : -1;
-      const bool ok = id0 >= 0 && id0 < a.c.pages;
-      const int64_t id = ok ? id0 : 0;
-      const int at = (int)(tok & (a.c.page - 1));
-      kp[u] = a.c.k_codes + (id * a.c.heads + h) * page_bytes + at * D;
-      vp[u] = a.c.v_codes + (id * a.c.heads + h) * page_bytes + at * D;
-      mk[u] = ok ? a.c.k_absmax[id * a.c.heads + h] : -1.0f;
-      mv[u] = ok ? a.c.v_absmax[id * a.c.heads + h] : 0.0f;
-      bad |= !ok;
-    }
+    const bool more = t + NW < t1;
     // S': tokens 16 u + 4 quarter .. + 3 of the step, row r
     f32x4 sc[NS];
 #pragma unroll
     for (int u = 0; u < NS; ++u) {
       sc[u] = f32x4{0, 0, 0, 0};
-      v4i w[DH];
 #pragma unroll
       for (int c = 0; c < DH; ++c) {
-        const int d = c * 64 + quarter * 16;
-        w[c] = d < D ? *reinterpret_cast<const v4i*>(kp[u] + r * D + d) : v4i{0, 0, 0, 0};
-      }
+        const f16x8 k0 = codes8(kw[u][c].x, kw[u][c].y), k1 = codes8(kw[u][c].z, kw[u][c].w);
 #pragma unroll
-      for (int c = 0; c < DH; ++c) {
-        const f16x8 k0 = codes8(w[c].x, w[c].y), k1 = codes8(w[c].z, w[c].w);
-#pragma unroll
-        for (int x = 0; x < TERMS; ++x) {
+        for (int x = 0; x < QT; ++x) {
           sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[x][2 * c], sc[u], 0, 0, 0);
           sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[x][2 * c + 1], sc[u], 0, 0, 0);
         }
       }
+    }
+    float mk_now[NP], mv_now[NP];
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+      mk_now[u] = mk[u];
+      mv_now[u] = mv[u];
+      bad |= mk[u] < 0.0f;
+    }
+    if (more) {
+      locate(t + NW);
+      request_k();
+      look_up(t + 2 * NW);
     }
     // logits, in scalars: where elements of the accumulator vectors themselves were overwritten under a lane's condition, the
     // compiler (hipcc 7.2) spread the first one's value over the three others
     float x[NS][4];
 #pragma unroll
     for (int u = 0; u < NS; ++u) {
-      const float f = row_scale * mk[u];
+      const float f = row_scale * mk_now[u / (NS / NP)];
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[u][e] = sc[u][e] * f;
     }
@@ -234,7 +280,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
       for (int u = 0; u < NS; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const bool out = (16 * u + e < from) | (16 * u + e >= to) | (mk[u] < 0.0f);
+          const bool out = (16 * u + e < from) | (16 * u + e >= to) | (mk_now[u / (NS / NP)] < 0.0f);
           x[u][e] = out ? -__builtin_inff() : x[u][e];
         }
     }
@@ -247,9 +293,9 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
     top = fmaxf(top, across(top, 32));
     int ve = v_exp;
 #pragma unroll
-    for (int u = 0; u < NS; ++u)
-      if (mv[u] > 0.0f) {
-        const int e = __builtin_amdgcn_frexp_expf(mv[u]);
+    for (int u = 0; u < NP; ++u)
+      if (mv_now[u] > 0.0f) {
+        const int e = __builtin_amdgcn_frexp_expf(mv_now[u]);
         ve = e > ve ? e : ve;
       }
     const float m_new = fmaxf(m_run, top);
@@ -265,10 +311,10 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
       v_exp = ve;
       m_run = m_new;
     }
-    f16x4 p[TERMS][NS];
+    f16x4 p[PT][NS];
 #pragma unroll
     for (int u = 0; u < NS; ++u) {
-      const float f = mv[u] > 0.0f ? __builtin_ldexpf(mv[u], kPBits - v_exp) : 0.0f;
+      const float v = mv_now[u / (NS / NP)], f = v > 0.0f ? __builtin_ldexpf(v, kPBits - v_exp) : 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float w = __builtin_amdgcn_exp2f(x[u][e] - m_use);
@@ -276,7 +322,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
         const float y = w * f;
         const _Float16 hi16 = (_Float16)y;
         p[0][u][e] = hi16;
-        if (TERMS == 2) p[TERMS - 1][u][e] = (_Float16)(y - (float)hi16);
+        if (PT == 2) p[PT - 1][u][e] = (_Float16)(y - (float)hi16);
       }
     }
     // O': channels 64 c + 4 (lane & 15) + k of the value operand
@@ -284,21 +330,18 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
     for (int u = 0; u < NS; u += 2) {
 #pragma unroll
       for (int c = 0; c < DH; ++c) {
-        const int d = c * 64 + r * 4;
-        const bool in = d < D;
-        const v4i w0 = in ? *reinterpret_cast<const v4i*>(vp[u] + (quarter * D + d) * 4) : v4i{0, 0, 0, 0};
-        const v4i w1 = in ? *reinterpret_cast<const v4i*>(vp[u + 1] + (quarter * D + d) * 4) : v4i{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const f16x8 v = codes8(w0[k], w1[k]);
+          const f16x8 v = codes8(vw[u][c][k], vw[u + 1][c][k]);
 #pragma unroll
-          for (int term = 0; term < TERMS; ++term) {
+          for (int term = 0; term < PT; ++term) {
             const f16x8 pp = __builtin_shufflevector(p[term][u], p[term][u + 1], 0, 1, 2, 3, 4, 5, 6, 7);
             o[c][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pp, o[c][k], 0, 0, 0);
           }
         }
       }
     }
+    if (more) request_v();
   }
   // a row's sum over its four lanes; the waves' shares joined: a lane holds, of row r, channels
   // 64 c + 16 quarter + 4 e + k in o[c][k][e]
@@ -342,6 +385,8 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
     for (int w = 0; w < NW; ++w) l += sm_l[w][row] * __builtin_amdgcn_exp2f(sm_m[w][row] - use);
 #pragma unroll
     for (int w = 0; w < NW / 2; ++w) v += *reinterpret_cast<const f32x4*>(&sm_o[w][row][d]);
+    const int64_t at = tile * 16 + row;
+    if (at >= nrows) continue;
     if (a.splits > 1) {
       *reinterpret_cast<f32x4*>(a.part_o + (slot * 16 + row) * D + d) = v;
       if (d == 0) {
@@ -350,19 +395,23 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
       }
       continue;
     }
-    const int64_t at = tile * 16 + row;
-    if (at >= nrows) continue;
     El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + at / a.group) * a.o_ts + (h * a.group + at % a.group) * a.o_hs + d;
     E::store4(to, l > 0.0f ? v / l : f32x4{0, 0, 0, 0});
   }
 }
 
-// Joins the splits of a tile of 16 rows.  grid: (sequence * heads + head) * row_tiles + tile.
+// Joins the splits of a row: a workgroup per row, its threads over groups of four channels and, as many as are left, over
+// the splits.  (A workgroup per 16 rows, each thread over all splits: 51 us for 8 tiles of 96 splits of 128 channels.)
+// grid: ((sequence * heads + head) * row_tiles + tile) * 16 + row.
 template <int T>
 __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   using E = Elem<T>;
   typedef typename E::type El;
+  __shared__ __attribute__((aligned(16))) float sm_o[kBlock * 4];
+  __shared__ float sm_l[kBlock], sm_m[kBlock / kWave];
   int64_t g = block_index();
+  const int row = (int)(g & 15);
+  g >>= 4;
   const int64_t slot = g * a.splits;
   const int64_t tile = g % a.row_tiles;
   g /= a.row_tiles;
@@ -370,25 +419,37 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   const int64_t s = g / a.c.heads;
   if (s >= a.b.seqs) return;
   const Sequence sq = sequence(a.b, a.c.page, (int)s);
-  const int64_t nrows = (int64_t)sq.n * a.group;
-  const int D = a.c.dim;
-  for (int x = threadIdx.x; x < 16 * (D >> 2); x += kBlock) {
-    const int row = x / (D >> 2), d = (x % (D >> 2)) * 4;
-    const int64_t at = tile * 16 + row;
-    if (at >= nrows) continue;
-    float top = -__builtin_inff();
-    for (int i = 0; i < a.splits; ++i) top = fmaxf(top, a.part_ml[((slot + i) * 16 + row) * 2]);
-    const float use = top == -__builtin_inff() ? 0.0f : top;
-    float l = 0.0f;
-    f32x4 v = {0, 0, 0, 0};
-    for (int i = 0; i < a.splits; ++i) {
+  const int64_t at = tile * 16 + row;
+  if (at >= (int64_t)sq.n * a.group) return;
+  const int D = a.c.dim, quads = D >> 2, parts = kBlock / quads;
+  const int d = ((int)threadIdx.x % quads) * 4, part = (int)threadIdx.x / quads;
+  float top = -__builtin_inff();
+  for (int i = threadIdx.x; i < a.splits; i += kBlock) top = fmaxf(top, a.part_ml[((slot + i) * 16 + row) * 2]);
+  top = wave_max(top);
+  if ((threadIdx.x & 63) == 0) sm_m[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
+  const float use = top == -__builtin_inff() ? 0.0f : top;
+  float l = 0.0f;
+  f32x4 v = {0, 0, 0, 0};
+  if (part < parts) {
+#pragma unroll 4
+    for (int i = part; i < a.splits; i += parts) {
       const float f = __builtin_amdgcn_exp2f(a.part_ml[((slot + i) * 16 + row) * 2] - use);
       l += a.part_ml[((slot + i) * 16 + row) * 2 + 1] * f;
       v += *reinterpret_cast<const f32x4*>(a.part_o + ((slot + i) * 16 + row) * D + d) * f;
     }
-    El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + at / a.group) * a.o_ts + (h * a.group + at % a.group) * a.o_hs + d;
-    E::store4(to, l > 0.0f ? v / l : f32x4{0, 0, 0, 0});
   }
+  *reinterpret_cast<f32x4*>(sm_o + 4 * threadIdx.x) = v;
+  sm_l[threadIdx.x] = l;
+  __syncthreads();
+  if (part > 0) return;
+  for (int i = 1; i < parts; ++i) {  // in a fixed order
+    l += sm_l[threadIdx.x + i * quads];
+    v += *reinterpret_cast<const f32x4*>(sm_o + 4 * (threadIdx.x + i * quads));
+  }
+  El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + at / a.group) * a.o_ts + (h * a.group + at % a.group) * a.o_hs + d;
+  E::store4(to, l > 0.0f ? v / l : f32x4{0, 0, 0, 0});
 }
 
 // How a call is cut up.
@@ -407,12 +468,12 @@ static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int q_he
   p.splits = 1;
   p.ws_bytes = 0;
   if (p.tiles == 0) return MPQ_OK;
-  // about three workgroups per CU, none with less than 256 tokens (a step for each of its waves)
+  // about three workgroups per CU, none with less than 512 tokens
   const int64_t len = b.max_len < (int64_t)b.table_pages * c.page ? b.max_len : (int64_t)b.table_pages * c.page;
-  const int64_t want = (3 * kNumCU + p.tiles - 1) / p.tiles, most_splits = (len + 255) / 256;
+  const int64_t want = (3 * kNumCU + p.tiles - 1) / p.tiles, most_splits = (len + 511) / 512;
   int64_t splits = want < most_splits ? want : most_splits;
   p.splits = (int)(splits < 1 ? 1 : splits);
-  if (blocks_z(p.tiles * p.splits, kAttnWaves * 64) > 65535u) return MPQ_ERR_SHAPE;
+  if (blocks_z(p.tiles * (p.splits > 16 ? p.splits : 16), kAttnWaves * 64) > 65535u) return MPQ_ERR_SHAPE;
   p.ws_bytes = p.splits > 1 ? (size_t)p.tiles * p.splits * 16 * (c.dim + 2) * sizeof(float) : 0;
   return MPQ_OK;
 }
@@ -421,12 +482,16 @@ template <int T>
 static int launch_attention(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   const dim3 grid = wide_grid(p.tiles * p.splits, kAttnWaves * 64);
   const int dh = (a.c.dim + 63) / 64;
-  if (dh == 1) kv_attention_k<T, 1><<<grid, kAttnWaves * 64, 0, st>>>(a);
-  else if (dh == 2) kv_attention_k<T, 2><<<grid, kAttnWaves * 64, 0, st>>>(a);
-  else kv_attention_k<T, 4><<<grid, kAttnWaves * 64, 0, st>>>(a);
+  const bool one = a.c.page >= (dh <= 2 ? 64 : 32);
+#define MPQ_ATTN(DH_) \
+  (one ? (void)(kv_attention_k<T, DH_, true><<<grid, kAttnWaves * 64, 0, st>>>(a)) : (void)(kv_attention_k<T, DH_, false><<<grid, kAttnWaves * 64, 0, st>>>(a)))
+  if (dh == 1) MPQ_ATTN(1);
+  else if (dh == 2) MPQ_ATTN(2);
+  else MPQ_ATTN(4);
+#undef MPQ_ATTN
   const int rc = launch_status();
   if (rc != MPQ_OK || p.splits == 1) return rc;
-  kv_attention_join_k<T><<<wide_grid(p.tiles, kBlock), kBlock, 0, st>>>(a);
+  kv_attention_join_k<T><<<wide_grid(p.tiles * 16, kBlock), kBlock, 0, st>>>(a);
   return launch_status();
 }
 
