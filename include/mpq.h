@@ -511,7 +511,7 @@ int mpq_kv_append(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type
                   int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride, void* stream);
 int mpq_kv_gather(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, void* k_out, void* v_out,
                   void* stream);
-size_t mpq_kv_attention_workspace_bytes(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int q_heads);
+size_t mpq_kv_attention_workspace_bytes(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, int q_heads);
 int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, const void* q,
                      int64_t q_token_stride, int64_t q_head_stride, int q_heads, float softmax_scale, int causal,
                      int64_t window, void* out, int64_t out_token_stride, int64_t out_head_stride, void* ws,

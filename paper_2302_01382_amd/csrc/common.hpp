@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "launch_shapes.hpp"
 #include "mpq.h"
 
@@ -46,8 +48,25 @@ int check_token_quant(const void* x, int x_type, int64_t M, int64_t K, int64_t x
 int launch_token_quant(const void* x, int x_type, int64_t M, int64_t K, int64_t x_stride, int bits, int8_t* codes, float* scale,
                        hipStream_t st);
 
+// Dynamic LDS above 64 KiB has to be allowed once per kernel and device (hipFuncSetAttribute, not a
+// stream operation).  `done` is one flag word per device, a bit per kernel variant of the caller's
+// instantiation; setting the attribute twice is harmless, so a relaxed flag is all the
+// synchronisation two host threads racing through here need.
+constexpr int kMaxDevices = 64;
+inline int allow_lds(const void* kern, int bytes, std::atomic<unsigned>* done, int which) {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
+  if (done[dev].load(std::memory_order_relaxed) & (1u << which)) return MPQ_OK;
+  hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != hipSuccess) { set_last_hip_error((int)e); return MPQ_ERR_HIP; }
+  done[dev].fetch_or(1u << which, std::memory_order_relaxed);
+  return MPQ_OK;
+}
+
 // defined in hutchinson.hip: allows its kernels the LDS they need on the current device (mpq_init)
 int prepare_hutchinson();
+// ... and in kv_prompt.hip
+int prepare_prompt();
 
 // defined in qgemm.hip: the host-side argument checks of mpq_qgemm_act / mpq_qgemm_score, for callers
 // that must validate several layers before their first launch

@@ -18,46 +18,14 @@
 // for the others (with one, an fp16 output's distance to 64 bits went from 2.1e-4 to 3.1e-4; the step has room for the
 // products).  Values' maxima differ from page to page: probabilities carry them relative to a power of two that is
 // at least the largest maximum so far, an exact rescaling whenever it grows.
-#include "kv.hpp"
+#include "kv_attn.hpp"
 
 namespace mpq {
 
-typedef int v4i __attribute__((ext_vector_type(4)));
-
-// four codes -> fp16: the byte code + 128 as the low bits of 1024 + u, less 1152 (both exact)
-__device__ __forceinline__ void codes4(int w, f16x2& lo, f16x2& hi) {
-  const unsigned u = (unsigned)w ^ 0x80808080u;
-  const f16x2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-  lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off;
-  hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off;
+__device__ __forceinline__ v4i stream16(const int8_t* p) {
+  return __builtin_nontemporal_load((const __attribute__((address_space(1))) v4i*)p);
 }
-__device__ __forceinline__ f16x8 codes8(int a, int b) {
-  f16x2 x, y, z, w;
-  codes4(a, x, y);
-  codes4(b, z, w);
-  return f16x8{x.x, x.y, y.x, y.y, z.x, z.y, w.x, w.y};
-}
-
-__device__ __forceinline__ float across(float v, int mask) { return __shfl_xor(v, mask, 64); }
-
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kPBits = 14;  // probabilities are multiplied by 2^14 before they are rounded to fp16
-
-struct AttnArgs {
-  mpq_kv_cache c;
-  mpq_kv_batch b;
-  const void* q;
-  int64_t q_ts, q_hs;
-  void* out;
-  int64_t o_ts, o_hs;
-  int q_heads, group, causal;
-  int64_t window;
-  float scale;        // softmax_scale
-  int64_t row_tiles;  // tiles of 16 (row, query head) pairs per sequence and key head
-  int splits;
-  float* part_o;      // splits > 1: [tile][split][16][dim], then
-  float* part_ml;     // [tile][split][16][2]
-};
 
 constexpr int kAttnWaves = 4;
 
@@ -203,7 +171,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
 #pragma unroll
       for (int c = 0; c < DH; ++c) {
         const int d = c * 64 + quarter * 16;
-        kw[u][c] = d < D ? *reinterpret_cast<const v4i*>(kp[u / (NS / NP)] + (u % (NS / NP) * 16 + r) * D + d) : v4i{0, 0, 0, 0};
+        kw[u][c] = d < D ? stream16(kp[u / (NS / NP)] + (u % (NS / NP) * 16 + r) * D + d) : v4i{0, 0, 0, 0};
       }
   };
   auto request_v = [&]() {
@@ -212,7 +180,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
 #pragma unroll
       for (int c = 0; c < DH; ++c) {
         const int d = c * 64 + r * 4;
-        vw[u][c] = d < D ? *reinterpret_cast<const v4i*>(vp[u / (NS / NP)] + u % (NS / NP) * 16 * D + (quarter * D + d) * 4) : v4i{0, 0, 0, 0};
+        vw[u][c] = d < D ? stream16(vp[u / (NS / NP)] + u % (NS / NP) * 16 * D + (quarter * D + d) * 4) : v4i{0, 0, 0, 0};
       }
   };
 
@@ -402,7 +370,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
 
 // Joins the splits of a row: a workgroup per row, its threads over groups of four channels and, as many as are left, over
 // the splits.  (A workgroup per 16 rows, each thread over all splits: 51 us for 8 tiles of 96 splits of 128 channels.)
-// grid: ((sequence * heads + head) * row_tiles + tile) * 16 + row.
+// grid: ((sequence * heads + head) * row_tiles + tile) * tile_rows + row.
 template <int T>
 __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   using E = Elem<T>;
@@ -410,8 +378,8 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) float sm_o[kBlock * 4];
   __shared__ float sm_l[kBlock], sm_m[kBlock / kWave];
   int64_t g = block_index();
-  const int row = (int)(g & 15);
-  g >>= 4;
+  const int row = (int)(g % a.tile_rows);
+  g /= a.tile_rows;
   const int64_t slot = g * a.splits;
   const int64_t tile = g % a.row_tiles;
   g /= a.row_tiles;
@@ -452,25 +420,34 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   E::store4(to, l > 0.0f ? v / l : f32x4{0, 0, 0, 0});
 }
 
+// Rows of a sequence and key head from which on kv_prompt.hip takes a call.
+constexpr int64_t kPromptFrom = 128;
+
 // How a call is cut up.
 struct AttnPlan {
   int64_t row_tiles, tiles;
-  int splits;
+  int splits, tile_rows;
+  int64_t wg_tiles;  // > 0: row tiles of kv_prompt.hip
   size_t ws_bytes;
 };
-static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int q_heads, AttnPlan& p) {
+static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int type, int q_heads, AttnPlan& p) {
   if (q_heads <= 0 || q_heads % c.heads) return MPQ_ERR_SHAPE;
   const int64_t most = b.max_new < b.rows ? b.max_new : b.rows;
-  if (mul_overflows(most, q_heads)) return MPQ_ERR_SHAPE;
+  if (mul_overflows(most, q_heads) || most * (q_heads / c.heads) > 0x7FFFFFFF) return MPQ_ERR_SHAPE;
   p.row_tiles = (most * (q_heads / c.heads) + 15) / 16;
   if (mul_overflows(p.row_tiles, (int64_t)b.seqs * c.heads)) return MPQ_ERR_SHAPE;
   p.tiles = p.row_tiles * b.seqs * c.heads;
   p.splits = 1;
+  p.tile_rows = (int)(p.row_tiles > 1 ? 16 : most * (q_heads / c.heads));
+  p.wg_tiles = 0;
   p.ws_bytes = 0;
   if (p.tiles == 0) return MPQ_OK;
-  // about three workgroups per CU, none with less than 512 tokens
+  // two workgroups per CU are on the chip at a time; none with less than 512 tokens
   const int64_t len = b.max_len < (int64_t)b.table_pages * c.page ? b.max_len : (int64_t)b.table_pages * c.page;
-  const int64_t want = (3 * kNumCU + p.tiles - 1) / p.tiles, most_splits = (len + 511) / 512;
+  const int64_t pair_rows = most * (q_heads / c.heads);
+  if (pair_rows >= kPromptFrom) p.wg_tiles = (pair_rows + prompt_rows(type, c.dim) - 1) / prompt_rows(type, c.dim);
+  const int64_t slots = p.wg_tiles > 0 ? kNumCU : 2 * kNumCU, units = p.wg_tiles > 0 ? p.wg_tiles * b.seqs * c.heads : p.tiles;
+  const int64_t want = slots / units, most_splits = (len + 511) / 512;
   int64_t splits = want < most_splits ? want : most_splits;
   p.splits = (int)(splits < 1 ? 1 : splits);
   if (blocks_z(p.tiles * (p.splits > 16 ? p.splits : 16), kAttnWaves * 64) > 65535u) return MPQ_ERR_SHAPE;
@@ -485,13 +462,14 @@ static int launch_attention(const AttnArgs& a, const AttnPlan& p, hipStream_t st
   const bool one = a.c.page >= (dh <= 2 ? 64 : 32);
 #define MPQ_ATTN(DH_) \
   (one ? (void)(kv_attention_k<T, DH_, true><<<grid, kAttnWaves * 64, 0, st>>>(a)) : (void)(kv_attention_k<T, DH_, false><<<grid, kAttnWaves * 64, 0, st>>>(a)))
-  if (dh == 1) MPQ_ATTN(1);
+  if (p.wg_tiles > 0) {
+  } else if (dh == 1) MPQ_ATTN(1);
   else if (dh == 2) MPQ_ATTN(2);
   else MPQ_ATTN(4);
 #undef MPQ_ATTN
-  const int rc = launch_status();
+  const int rc = p.wg_tiles > 0 ? launch_prompt(T, a, p.wg_tiles, false, st) : launch_status();
   if (rc != MPQ_OK || p.splits == 1) return rc;
-  kv_attention_join_k<T><<<wide_grid(p.tiles * 16, kBlock), kBlock, 0, st>>>(a);
+  kv_attention_join_k<T><<<wide_grid(p.tiles * p.tile_rows, kBlock), kBlock, 0, st>>>(a);
   return launch_status();
 }
 
@@ -499,9 +477,9 @@ static int launch_attention(const AttnArgs& a, const AttnPlan& p, hipStream_t st
 
 using namespace mpq;
 
-extern "C" size_t mpq_kv_attention_workspace_bytes(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int q_heads) {
+extern "C" size_t mpq_kv_attention_workspace_bytes(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, int q_heads) {
   AttnPlan p;
-  if (check_kv(cache, batch, MPQ_F32) != MPQ_OK || plan_attention(*cache, *batch, q_heads, p) != MPQ_OK) return 0;
+  if (check_kv(cache, batch, type) != MPQ_OK || plan_attention(*cache, *batch, type, q_heads, p) != MPQ_OK) return 0;
   return p.ws_bytes;
 }
 
@@ -512,7 +490,7 @@ extern "C" int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* b
   int rc = check_kv(cache, batch, type);
   if (rc != MPQ_OK) return rc;
   AttnPlan p;
-  rc = plan_attention(*cache, *batch, q_heads, p);
+  rc = plan_attention(*cache, *batch, type, q_heads, p);
   if (rc != MPQ_OK) return rc;
   if (window < 0 || (window > 0 && !causal) || !(softmax_scale == softmax_scale) || __builtin_isinf(softmax_scale)) return MPQ_ERR_SHAPE;
   if (q_token_stride < 0 || q_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0) return MPQ_ERR_SHAPE;
@@ -526,7 +504,7 @@ extern "C" int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* b
   if (p.ws_bytes > 0 && (!ws || ws_bytes < p.ws_bytes)) return MPQ_ERR_WORKSPACE;
   if (p.ws_bytes > 0 && !aligned16(ws)) return MPQ_ERR_ALIGN;
   AttnArgs a{*cache, *batch, q, q_token_stride, q_head_stride, out, out_token_stride, out_head_stride, q_heads, q_heads / cache->heads,
-             causal != 0, window, softmax_scale, p.row_tiles, p.splits, nullptr, nullptr};
+             causal != 0, window, softmax_scale, p.row_tiles, p.splits, p.tile_rows, nullptr, nullptr};
   if (p.splits > 1) {
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = a.part_o + (size_t)p.tiles * p.splits * 16 * cache->dim;

@@ -1,0 +1,443 @@
+// kv_prompt.hip -- attention over quantized pages where a sequence brings many rows: a prompt's.
+//
+// The mathematics, the operands' order and the precision are kv_attention.hip's; there the codes' bytes count, here the
+// matrix products do.  A workgroup of four waves takes 64 NQ rows of a key head (row, query head pairs: the heads of a group
+// share keys and values), NQ tiles of 16 rows a wave.  Per step of 64 tokens the workgroup turns the codes of keys and
+// values into fp16 once, on their way into a double-buffered LDS stage, and every wave multiplies them with its rows: an
+// operand read out of the LDS serves NQ matrix steps.
+//   keys    [token][chunk of 8 channels], chunks swizzled by the token so that 16 tokens' reads of one chunk fall into
+//           different banks
+//   values  [half step][quarter][channel][8 tokens]: the operand as a lane wants it, 16 lanes in 256 bytes
+// A step's softmax: logits are at most one fused multiply-add from the product, f = row's scale * page's maximum, and
+// their exponential takes the page's value factor along: P' = 2^(x - m + lg + 8), lg = log2 of the page's value maximum over
+// a power of two that no maximum so far exceeds (at least -60); the sum divides it out again, page by page.  m is a maximum
+// that may lag behind the true one by up to 6: P' then reaches 2^14, and the accumulators are rescaled only when it lags
+// by more.
+#include "kv_attn.hpp"
+
+#include <type_traits>
+
+namespace mpq {
+
+constexpr int kPromptWaves = 8, kPromptThreads = kPromptWaves * 64;
+constexpr float kLag = 6.0f, kUp = 8.0f, kLeast = -60.0f;
+
+// max over the four lanes that share a row: lane & 15
+__device__ __forceinline__ float row_max(float v) {
+  auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+  v = fmaxf(__builtin_bit_cast(float, (unsigned)a[0]), __builtin_bit_cast(float, (unsigned)a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+  return fmaxf(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
+}
+
+// this wave's LDS accesses are done, and so are everyone's (loads from memory stay in flight)
+__device__ __forceinline__ void lds_meet() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int T, int DH, int NQ>
+struct PromptCfg {
+  static constexpr int QT = T == MPQ_F32 ? 2 : 1, PT = QT;  // fp16 terms of q and of a probability
+  static constexpr int ROWS = kPromptWaves * 16 * NQ;       // rows of a workgroup
+  static constexpr int K_BYTES = 64 * DH * 128, STAGE = 2 * K_BYTES;
+  static constexpr int LDS_BYTES = 2 * STAGE;
+  static constexpr int NK = (DH + 1) / 2, NV = (DH + 3) / 4;    // 16-byte loads per thread and step: keys; pairs of them: values
+};
+
+// grid: pairs (sequence, head) fastest, so that those that share keys and values share an XCD's L2 where their number is a
+// multiple of 8; then splits; row tiles last, the last ones -- under a causal mask the longest -- first.
+template <int T, int DH, int NQ>
+__global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int64_t wg_tiles) {
+  using C = PromptCfg<T, DH, NQ>;
+  using E = Elem<T>;
+  typedef typename E::type El;
+  constexpr int QT = C::QT, PT = C::PT, TT = 64;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, quarter = lane >> 4;
+  int64_t g = block_index();
+  const int64_t pairs = (int64_t)a.b.seqs * a.c.heads, pair = g % pairs;
+  g /= pairs;
+  const int split = (int)(g % a.splits);
+  g /= a.splits;
+  if (g >= wg_tiles) return;
+  const int h = (int)(pair % a.c.heads), s = (int)(pair / a.c.heads);
+  const Sequence sq = sequence(a.b, a.c.page, s);
+  const int len = (int)(sq.len < sq.room ? sq.len : sq.room);  // (a length has 31 bits, and so has rows * group)
+  const int before = (int)sq.len - sq.n, group = a.group, nrows = sq.n * group;
+  const int64_t row0_wide = (wg_tiles - 1 - g) * C::ROWS;
+  if (row0_wide >= nrows) return;
+  const int row0 = (int)row0_wide;
+  const int D = a.c.dim;
+
+  // tokens [lo, hi) that a row sees
+  auto hi_of = [&](int row) {
+    const int p = before + row / group;
+    const int hi = a.causal && p < len ? p + 1 : len;
+    return hi > 0 ? hi : 0;
+  };
+  auto lo_of = [&](int row) {
+    const int64_t lo = a.window > 0 ? (int64_t)before + row / group - a.window + 1 : 0;
+    return lo > 0 ? (int)(lo < 0x7FFFFFFF ? lo : 0x7FFFFFFF) : 0;
+  };
+  // of some row of the workgroup, and of every row of the wave
+  const int end = row0 + C::ROWS < nrows ? row0 + C::ROWS : nrows;
+  const int w0 = row0 + wave * 16 * NQ, w1 = w0 + 16 * NQ < nrows ? w0 + 16 * NQ : nrows;
+  const int span_lo = lo_of(row0), span_hi = hi_of(end - 1);
+  const int all_lo = lo_of(w1 - 1), all_hi = hi_of(w0 < nrows ? w0 : 0);
+
+  int lo[NQ], hi[NQ];
+  f16x8 q[QT][NQ][2 * DH];
+  float row_scale[NQ];
+  const float qmax = (float)((1 << (a.c.bits - 1)) - 1);
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int idx = w0 + n * 16 + r;
+    const bool real = idx < nrows;
+    const int row_at = real ? idx : 0, i = row_at / group;
+    lo[n] = lo_of(row_at);
+    hi[n] = real ? hi_of(row_at) : 0;
+    const El* row = reinterpret_cast<const El*>(a.q) + (sq.row0 + i) * a.q_ts + (int64_t)(h * group + row_at - i * group) * a.q_hs;
+    f32x8 v[2 * DH];
+    float m = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 2 * DH; ++c) {
+      const int d = c * 32 + quarter * 8;
+      v[c] = real && d < D ? E::load8(row + d) : f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[c][e]));
+    }
+    m = row_max(m);
+    const int e2 = 14 - (m > 0.0f ? __builtin_amdgcn_frexp_expf(m) : 0);
+    const float sign = a.scale < 0.0f ? -1.0f : 1.0f;  // so that factors of products are never negative
+#pragma unroll
+    for (int c = 0; c < 2 * DH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = __builtin_ldexpf(v[c][e] * sign, e2);
+        const _Float16 top = (_Float16)x;
+        q[0][n][c][e] = top;
+        if (QT == 2) q[QT - 1][n][c][e] = (_Float16)(x - (float)top);
+      }
+    row_scale[n] = __builtin_ldexpf(fabsf(a.scale) * kLog2e / qmax, -e2);
+  }
+
+  // this workgroup's steps
+  const int first = span_lo / TT, steps = span_hi > span_lo ? (span_hi + TT - 1) / TT - first : 0;
+  const int per = (steps + a.splits - 1) / a.splits;
+  const int t0 = first + split * per, t1 = first + ((split + 1) * per < steps ? (split + 1) * per : steps);
+  const int32_t* table = a.b.table + (int64_t)s * a.b.table_pages;
+  const unsigned page_bytes = (unsigned)(a.c.page * D);
+  const int shift = 31 - __builtin_clz((unsigned)a.c.page), page_mask = a.c.page - 1;
+
+  // Pages are looked up by each lane for the tokens whose codes it fetches, two steps ahead; codes are requested one step
+  // ahead.  All through vector loads: a scalar load in flight would make every wait for the LDS a wait for memory.
+  // 16 tokens lie on one page.  Nothing here asks whether it is needed: tokens that no row sees are looked up as the last one
+  // that some row does, chunks beyond dim are fetched as the last one within (they meet zeros of q, or channels that are
+  // not stored), threads beyond the last chunk fetch an earlier one again.
+  const unsigned pages = (unsigned)(a.c.pages < 0x7FFFFFFF ? a.c.pages : 0x7FFFFFFF);
+  int k_token[C::NK], k_off[C::NK], v_token[C::NV], v_off[C::NV];  // of the thread's chunks; offsets within 16 tokens
+#pragma unroll
+  for (int j = 0; j < C::NK; ++j) {
+    const int i = tid + j * kPromptThreads, token = i / (4 * DH) & 63, d = i % (4 * DH) * 16;
+    k_token[j] = token & ~15;
+    k_off[j] = (token & 15) * D + (d < D ? d : D - 16);
+  }
+#pragma unroll
+  for (int j = 0; j < C::NV; ++j) {
+    const int i = tid + j * kPromptThreads, ksq = i / (16 * DH) & 7, d = i % (16 * DH) * 4;
+    v_token[j] = (ksq >> 2) * 32;
+    v_off[j] = ((ksq & 3) * D + (d < D ? d : D - 4)) * 4;
+  }
+  int idk[C::NK], idv[C::NV][2], idu;
+  auto look_up = [&](int t) {
+    auto page = [&](int place) {
+      const int tok = t * TT + place;
+      return table[(tok < span_hi ? tok : span_hi - 1) >> shift];
+    };
+#pragma unroll
+    for (int j = 0; j < C::NK; ++j) idk[j] = page(k_token[j]);
+#pragma unroll
+    for (int j = 0; j < C::NV; ++j) {
+      idv[j][0] = page(v_token[j]);
+      idv[j][1] = page(v_token[j] + 16);
+    }
+    idu = page((lane & 3) * 16);
+  };
+  bool page_ok;
+  float mk_in, mv_in;  // lane u (mod 4): maxima of the pages of tokens 16 u .. of the step that is in flight
+  v4i kw[C::NK], vw[C::NV][2];
+  auto request = [&](int t) {
+    auto codes_at = [&](const int8_t* codes, int id, int token, int off) {
+      const uint64_t at = (uint64_t)((unsigned)id < pages ? (unsigned)id : 0u) * (unsigned)a.c.heads + (unsigned)h;
+      return *reinterpret_cast<const v4i*>(codes + at * page_bytes + (unsigned)(((t * TT + token) & page_mask) * D + off));
+    };
+    const bool ok = (unsigned)idu < pages;
+    const uint64_t at = (uint64_t)(ok ? (unsigned)idu : 0u) * (unsigned)a.c.heads + (unsigned)h;
+    page_ok = ok;
+    mk_in = a.c.k_absmax[at];
+    mv_in = a.c.v_absmax[at];
+#pragma unroll
+    for (int j = 0; j < C::NK; ++j) kw[j] = codes_at(a.c.k_codes, idk[j], k_token[j], k_off[j]);
+#pragma unroll
+    for (int j = 0; j < C::NV; ++j) {
+      vw[j][0] = codes_at(a.c.v_codes, idv[j][0], v_token[j], v_off[j]);
+      vw[j][1] = codes_at(a.c.v_codes, idv[j][1], v_token[j] + 16, v_off[j]);
+    }
+  };
+  auto store = [&](unsigned stage) {
+#pragma unroll
+    for (int j = 0; j < C::NK; ++j) {
+      const int i = tid + j * kPromptThreads, token = i / (4 * DH) & 63, ch = i % (4 * DH) * 2;
+      const int swz = DH == 1 ? (token >> 1) & 7 : token & 15;
+      char* row = lds + stage + token * (DH * 128);
+      *reinterpret_cast<f16x8*>(row + ((ch ^ swz) << 4)) = codes8(kw[j].x, kw[j].y);
+      *reinterpret_cast<f16x8*>(row + (((ch ^ swz) << 4) ^ 16)) = codes8(kw[j].z, kw[j].w);
+    }
+#pragma unroll
+    for (int j = 0; j < C::NV; ++j) {
+      const int i = tid + j * kPromptThreads, ksq = i / (16 * DH) & 7, dq = i % (16 * DH);
+      char* to = lds + stage + C::K_BYTES + ((ksq * 64 * DH + (dq >> 4) * 64 + (dq & 15)) << 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) *reinterpret_cast<f16x8*>(to + k * 256) = codes8(vw[j][0][k], vw[j][1][k]);
+    }
+  };
+
+  float m_ref[NQ], l_run[NQ];
+  int v_exp = -100000;  // O' is in units of 2^(v_exp - 8)
+  f32x4 o[NQ][4 * DH];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    m_ref[n] = -__builtin_inff();
+    l_run[n] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4 * DH; ++k) o[n][k] = f32x4{0, 0, 0, 0};
+  }
+
+  if (t0 < t1) {
+    look_up(t0);
+    request(t0);
+    look_up(t0 + 1);
+    store(0);
+  }
+  float mk_now[4], mv_now[4];
+  auto arrived = [&]() {
+    mk_in = page_ok ? mk_in : -1.0f;
+    mv_in = page_ok ? mv_in : 0.0f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      mk_now[u] = f_from_bits(__builtin_amdgcn_readlane(bits_from_f(mk_in), u));
+      mv_now[u] = f_from_bits(__builtin_amdgcn_readlane(bits_from_f(mv_in), u));
+    }
+  };
+  if (t0 < t1) arrived();
+  lds_meet();
+  const unsigned k_at = (unsigned)(r * (DH * 128)), v_at = (unsigned)(C::K_BYTES + ((quarter * 64 * DH + r) << 4));
+  const unsigned swz = (unsigned)(DH == 1 ? (r >> 1) & 7 : r);
+  unsigned stage = 0;
+  for (int t = t0; t < t1; ++t) {
+    const bool more = t + 1 < t1;
+    if (more) {
+      request(t + 1);
+      look_up(t + 2);
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {  // 32 tokens at a time
+      const int base = t * TT + half * 32;
+      f32x4 sc[2][NQ];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) sc[u][n] = f32x4{0, 0, 0, 0};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < 2 * DH; ++c) {
+          const f16x8 kf =
+              *reinterpret_cast<const f16x8*>(lds + stage + k_at + (((unsigned)(4 * c + quarter) ^ swz) << 4) + (2 * half + u) * 16 * (DH * 128));
+#pragma unroll
+          for (int x = 0; x < QT; ++x)
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) sc[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[x][n][c], sc[u][n], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const float mk[2] = {mk_now[2 * half], mk_now[2 * half + 1]}, mv[2] = {mv_now[2 * half], mv_now[2 * half + 1]};
+      int ve = v_exp;
+      float lg[2], back[2];  // log2 of the pages' value factors, and their reciprocals
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (mv[u] > 0.0f) {
+          const int e = __builtin_amdgcn_frexp_expf(mv[u]);
+          ve = e > ve ? e : ve;
+        }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        lg[u] = mv[u] > 0.0f ? fmaxf(__builtin_amdgcn_logf(__builtin_ldexpf(mv[u], -ve)), kLeast) : 0.0f;
+        back[u] = __builtin_amdgcn_exp2f(-lg[u]);
+      }
+      v4i pw[PT][NQ];  // probabilities: eight fp16, as the value product wants them
+      auto softmax = [&](auto masked_) {
+        constexpr bool MASKED = decltype(masked_)::value;
+        int from[MASKED ? NQ : 1], to[MASKED ? NQ : 1];  // first and last visible token, counted from the lane's first
+        if (MASKED) {
+          const int at = base + quarter * 4;
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) {
+            from[MASKED ? n : 0] = lo[n] - at;
+            to[MASKED ? n : 0] = hi[n] - at;
+          }
+        }
+        // a logit: where some are masked in scalars (kv_attention.hip says why)
+        auto logit = [&](int n, int u, int e, float f) {
+          const int at = 16 * u + e;
+          const bool out = (at < from[MASKED ? n : 0]) | (at >= to[MASKED ? n : 0]) | (mk[u] < 0.0f);
+          const float x = sc[u][n][e] * f;
+          return out ? -__builtin_inff() : x;
+        };
+        float top[NQ];
+        bool grow = ve != v_exp;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          top[n] = -__builtin_inff();
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float f = row_scale[n] * mk[u];
+            if (MASKED) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) top[n] = fmaxf(top[n], logit(n, u, e, f));
+            } else {
+              top[n] = fmaxf(top[n], fmaxf(fmaxf(sc[u][n][0], sc[u][n][1]), fmaxf(sc[u][n][2], sc[u][n][3])) * f);
+            }
+          }
+          top[n] = row_max(top[n]);
+          grow |= top[n] > m_ref[n] + kLag;
+        }
+        if (__any(grow)) {
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) {
+            const float m_new = fmaxf(m_ref[n], top[n]);
+            const float alpha = __builtin_amdgcn_exp2f(m_ref[n] - (m_new == -__builtin_inff() ? 0.0f : m_new));
+            l_run[n] *= alpha;
+            const float scale = __builtin_ldexpf(alpha, v_exp - ve);
+#pragma unroll
+            for (int k = 0; k < 4 * DH; ++k) o[n][k] *= scale;
+            m_ref[n] = m_new;
+          }
+          v_exp = ve;
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          const float m_use = m_ref[n] == -__builtin_inff() ? 0.0f : m_ref[n];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            __builtin_amdgcn_sched_barrier(0);
+            const float mm = m_use - (lg[u] + kUp), f = row_scale[n] * mk[u];
+            float w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              w[e] = __builtin_amdgcn_exp2f(MASKED ? logit(n, u, e, f) - mm : __builtin_fmaf(sc[u][n][e], f, -mm));
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+              const f16x2 top16 = __builtin_convertvector(f32x2{w[e], w[e + 1]}, f16x2);
+              pw[0][n][u * 2 + e / 2] = __builtin_bit_cast(int, top16);
+              if (PT == 2)
+                pw[PT - 1][n][u * 2 + e / 2] =
+                    __builtin_bit_cast(int, __builtin_convertvector(f32x2{w[e] - (float)top16.x, w[e + 1] - (float)top16.y}, f16x2));
+            }
+            const float sum = (w[0] + w[1]) + (w[2] + w[3]);
+            l_run[n] = __builtin_fmaf(sum, back[u], l_run[n]);
+          }
+        }
+      };
+      if (mk[0] < 0.0f || mk[1] < 0.0f || base < all_lo || base + 32 > all_hi) softmax(std::true_type{});  // uniform over the wave
+      else softmax(std::false_type{});
+#pragma unroll
+      for (int k = 0; k < 4 * DH; ++k) {
+        if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+        const f16x8 vf = *reinterpret_cast<const f16x8*>(lds + stage + v_at + ((half * 4 * 64 * DH + k * 16) << 4));
+#pragma unroll
+        for (int x = 0; x < PT; ++x)
+#pragma unroll
+          for (int n = 0; n < NQ; ++n)
+            o[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, __builtin_bit_cast(f16x8, pw[x][n]), o[n][k], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    stage = (unsigned)C::STAGE - stage;
+    if (more) store(stage);
+    if (more) arrived();
+    lds_meet();
+  }
+
+  // lane (row r, quarter): channels 64 c + 16 quarter + 4 e + k in o[n][4 c + k][e]
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    float l = l_run[n];
+    l += across(l, 16);
+    l += across(l, 32);
+    const int at = w0 + n * 16 + r;
+    if (at >= nrows) continue;
+    const float f = l > 0.0f ? __builtin_ldexpf(1.0f / qmax, v_exp) * (a.splits > 1 ? __builtin_amdgcn_exp2f(-kUp) : 1.0f / l) : 0.0f;
+    const int64_t slot = (pair * a.row_tiles + (at >> 4)) * a.splits + split;
+    float* part = a.part_o + (slot * 16 + r) * D;
+    const int i = at / group;
+    El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + i) * a.o_ts + (int64_t)(h * group + at - i * group) * a.o_hs;
+#pragma unroll
+    for (int c = 0; c < DH; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int d = c * 64 + quarter * 16 + 4 * e;
+        if (d >= D) continue;
+        const f32x4 v = f32x4{o[n][4 * c][e], o[n][4 * c + 1][e], o[n][4 * c + 2][e], o[n][4 * c + 3][e]} * f;
+        if (a.splits > 1) *reinterpret_cast<f32x4*>(part + d) = v;
+        else E::store4(to + d, v);
+      }
+    if (a.splits > 1 && quarter == 0) {
+      a.part_ml[(slot * 16 + r) * 2] = m_ref[n];
+      a.part_ml[(slot * 16 + r) * 2 + 1] = l * __builtin_amdgcn_exp2f(-kUp);
+    }
+  }
+}
+
+// rows of a workgroup: as many row tiles per wave as the registers hold
+int prompt_rows(int type, int dim) {
+  const int dh = dim <= 64 ? 1 : dim <= 128 ? 2 : 4;
+  return kPromptWaves * 16 * (dh == 4 || (type == MPQ_F32 && dh == 2) ? 1 : 2);
+}
+
+template <int T, int DH, int NQ>
+static int go(const AttnArgs& a, int64_t wg_tiles, bool prepare_only, hipStream_t st) {
+  using C = PromptCfg<T, DH, NQ>;
+  static std::atomic<unsigned> done[kMaxDevices];
+  if (C::LDS_BYTES > 65536 || prepare_only) {
+    const int rc = allow_lds(reinterpret_cast<const void*>(kv_prompt_k<T, DH, NQ>), C::LDS_BYTES, done, 0);
+    if (rc != MPQ_OK || prepare_only) return rc;
+  }
+  const dim3 grid = wide_grid(wg_tiles * a.splits * a.b.seqs * a.c.heads, kPromptThreads);
+  kv_prompt_k<T, DH, NQ><<<grid, kPromptThreads, C::LDS_BYTES, st>>>(a, wg_tiles);
+  return launch_status();
+}
+
+int launch_prompt(int type, const AttnArgs& a, int64_t wg_tiles, bool prepare_only, hipStream_t st) {
+  const int dh = a.c.dim <= 64 ? 1 : a.c.dim <= 128 ? 2 : 4;
+#define MPQ_GO(T_, DH_, NQ_) go<T_, DH_, NQ_>(a, wg_tiles, prepare_only, st)
+  if (type == MPQ_F32) return dh == 1 ? MPQ_GO(MPQ_F32, 1, 2) : dh == 2 ? MPQ_GO(MPQ_F32, 2, 1) : MPQ_GO(MPQ_F32, 4, 1);
+  if (type == MPQ_BF16) return dh == 1 ? MPQ_GO(MPQ_BF16, 1, 2) : dh == 2 ? MPQ_GO(MPQ_BF16, 2, 2) : MPQ_GO(MPQ_BF16, 4, 1);
+  return dh == 1 ? MPQ_GO(MPQ_F16, 1, 2) : dh == 2 ? MPQ_GO(MPQ_F16, 2, 2) : MPQ_GO(MPQ_F16, 4, 1);
+#undef MPQ_GO
+}
+
+int prepare_prompt() {
+  for (int type : {MPQ_F32, MPQ_BF16, MPQ_F16})
+    for (int dim : {64, 128, 256}) {
+      AttnArgs a{};
+      a.c.dim = dim;
+      const int rc = launch_prompt(type, a, 0, true, nullptr);
+      if (rc != MPQ_OK) return rc;
+    }
+  return MPQ_OK;
+}
+
+}  // namespace mpq

@@ -497,7 +497,8 @@ extern "C" int mpq_init(void) {
     }
     if (rc != MPQ_OK) return rc;
   }
-  return prepare_hutchinson();
+  const int rc = prepare_hutchinson();
+  return rc == MPQ_OK ? prepare_prompt() : rc;
 }
 
 extern "C" size_t mpq_qgemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int w_storage_bits) {

@@ -6,7 +6,6 @@
 
 #include "types.hpp"
 
-#include <atomic>
 #include <type_traits>
 
 namespace mpq {
@@ -814,21 +813,6 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void qgemm_dma(const int8_t* __
   }
   finish_sums<C, EPI>(lds, wave, sse, amax, epi, blockIdx.x);
   wait_vmcnt<0>();  // the zeros, before the LDS is given back
-}
-
-// Dynamic LDS above 64 KiB has to be allowed once per kernel and device (hipFuncSetAttribute, not a
-// stream operation).  `done` is one flag word per device, a bit per kernel variant of the caller's
-// instantiation; setting the attribute twice is harmless, so a relaxed flag is all the
-// synchronisation two host threads racing through here need.
-constexpr int kMaxDevices = 64;
-inline int allow_lds(const void* kern, int bytes, std::atomic<unsigned>* done, int which) {
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
-  if (done[dev].load(std::memory_order_relaxed) & (1u << which)) return MPQ_OK;
-  hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e != hipSuccess) { set_last_hip_error((int)e); return MPQ_ERR_HIP; }
-  done[dev].fetch_or(1u << which, std::memory_order_relaxed);
-  return MPQ_OK;
 }
 
 // How a call is launched with a tile size: kernel variant (EPI * 2 + VEC), grid and chunk length.

@@ -13,6 +13,7 @@ inline int type_size(int type) { return type == MPQ_F32 ? 4 : 2; }
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 // in memory at any address that an element may have
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));

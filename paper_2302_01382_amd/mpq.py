@@ -119,7 +119,7 @@ def lib():
         L.mpq_kv_append.argtypes = [vp, vp, ci, vp, i64, i64, vp, i64, i64, vp]
         L.mpq_kv_gather.argtypes = [vp, vp, ci, vp, vp, vp]
         L.mpq_kv_attention_workspace_bytes.restype = sz
-        L.mpq_kv_attention_workspace_bytes.argtypes = [vp, vp, ci]
+        L.mpq_kv_attention_workspace_bytes.argtypes = [vp, vp, ci, ci]
         L.mpq_kv_attention.argtypes = [vp, vp, ci, vp, i64, i64, ci, C.c_float, ci, i64, vp, i64, i64, vp, sz, vp]
         L.mpq_rademacher.argtypes = [C.c_uint64, C.c_uint64, i64, i64, vp, vp]
         L.mpq_hutchinson_quad_workspace_bytes.argtypes = [i64, i64, i64]
@@ -1018,8 +1018,8 @@ def kv_gather(cache: KvCache, batch: KvBatch, dtype=None, want_k=True, want_v=Tr
     return k, v
 
 
-def kv_attention_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads) -> int:
-    return int(lib().mpq_kv_attention_workspace_bytes(cache.ref, batch.ref, q_heads))
+def kv_attention_workspace_bytes(cache: KvCache, batch: KvBatch, dtype, q_heads) -> int:
+    return int(lib().mpq_kv_attention_workspace_bytes(cache.ref, batch.ref, _type(dtype), q_heads))
 
 
 def kv_attention(cache: KvCache, batch: KvBatch, q, causal=True, window=0, softmax_scale=None, out=None, ws: Workspace = None):
@@ -1033,7 +1033,7 @@ def kv_attention(cache: KvCache, batch: KvBatch, q, causal=True, window=0, softm
     if to != t:
         raise ValueError("q and out have one type")
     _on_current(q)
-    wp, wn, _alive = _scratch(ws, kv_attention_workspace_bytes(cache, batch, heads), q.device)
+    wp, wn, _alive = _scratch(ws, int(lib().mpq_kv_attention_workspace_bytes(cache.ref, batch.ref, t, heads)), q.device)
     _check(lib().mpq_kv_attention(cache.ref, batch.ref, t, _ptr(q), q_ts, q_hs, heads,
                                   cache.dim ** -0.5 if softmax_scale is None else float(softmax_scale), int(bool(causal)), int(window),
                                   _ptr(out), o_ts, o_hs, wp, wn, _stream()), "mpq_kv_attention")

@@ -266,7 +266,7 @@ def test_long_sequences_are_split(dtype, seqs, held, group):
     c, table = filled(r, seqs, lengths, heads, dim, page, 8, dtype)
     for new in (1, 3):
         b = c.batch([new] * seqs, lengths, table, new, held)
-        assert mpq.kv_attention_workspace_bytes(c.dev, b, heads * group) > 0
+        assert mpq.kv_attention_workspace_bytes(c.dev, b, getattr(__import__("torch"), dtype), heads * group) > 0
         q = dev(r.standard_normal((b.rows, heads * group, dim)) * 2, dtype)
         out = mpq.kv_attention(c.dev, b, q)
         check_attention(c, full(out), full(q), True, 0, dim ** -0.5, dtype)

@@ -162,7 +162,7 @@ def test_kv_attention_refuses():
         return L.mpq_kv_attention(*kv(batch=batch), *a)
 
     for heads in (0, -2, 3):
-        assert but(_4=heads) == mpq.ERR_SHAPE and q(*kv(), heads) == 0
+        assert but(_4=heads) == mpq.ERR_SHAPE and q(*kv(), 1, heads) == 0
     for scale in (float("nan"), float("inf"), -float("inf")):
         assert but(_5=scale) == mpq.ERR_SHAPE
     assert but(_7=-1) == mpq.ERR_SHAPE and but(_6=0, _7=5) == mpq.ERR_SHAPE
@@ -170,11 +170,11 @@ def test_kv_attention_refuses():
         assert but(**{"_%d" % i: -1}) == mpq.ERR_SHAPE and but(**{"_%d" % i: 1 << 62}) == mpq.ERR_SHAPE
     assert but(_8=None) == mpq.ERR_NULL and but(_8=ODD) == mpq.ERR_ALIGN
     long = {"max_len": 100000, "table_pages": 7000}
-    need = q(*kv(batch=long), 4)
-    assert need > 0 and q(*kv(), 4) == 0
+    need = q(*kv(batch=long), 1, 4)
+    assert need > 0 and q(*kv(), 1, 4) == 0
     assert but(long, _11=None) == mpq.ERR_WORKSPACE and but(long, _12=need - 1) == mpq.ERR_WORKSPACE
     assert but(long, _11=C.c_void_p(0x10008)) == mpq.ERR_ALIGN
-    assert q(*kv({"bits": 1}, long), 4) == 0 and q(None, kv()[1], 4) == 0
+    assert q(*kv({"bits": 1}, long), 1, 4) == 0 and q(None, kv()[1], 1, 4) == 0 and q(*kv(batch=long), 7, 4) == 0
 
 
 def test_the_binding_refuses():
