@@ -22,12 +22,23 @@ namespace mpq {
 constexpr int kPromptWaves = 8, kPromptThreads = kPromptWaves * 64;
 constexpr float kLag = 6.0f, kUp = 8.0f, kLeast = -60.0f;
 
+// Maxima in assembly: the compiler's would first quiet every operand that it has not seen quieted.
+__device__ __forceinline__ float max2(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 // max over the four lanes that share a row: lane & 15
 __device__ __forceinline__ float row_max(float v) {
   auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
-  v = fmaxf(__builtin_bit_cast(float, (unsigned)a[0]), __builtin_bit_cast(float, (unsigned)a[1]));
+  v = max2(__builtin_bit_cast(float, (unsigned)a[0]), __builtin_bit_cast(float, (unsigned)a[1]));
   auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
-  return fmaxf(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
+  return max2(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
 }
 
 // this wave's LDS accesses are done, and so are everyone's (loads from memory stay in flight)
@@ -43,12 +54,13 @@ struct PromptCfg {
   static constexpr int ROWS = kPromptWaves * 16 * NQ;       // rows of a workgroup
   static constexpr int K_BYTES = 64 * DH * 128, STAGE = 2 * K_BYTES;
   static constexpr int LDS_BYTES = 2 * STAGE;
-  static constexpr int NK = (DH + 1) / 2, NV = (DH + 3) / 4;    // 16-byte loads per thread and step: keys; pairs of them: values
+  static constexpr int NK = (DH + 1) / 2, NV = (DH + 1) / 2;    // chunks per thread and step: 16 bytes of keys; twice 8 of values
 };
 
 // grid: pairs (sequence, head) fastest, so that those that share keys and values share an XCD's L2 where their number is a
 // multiple of 8; then splits; row tiles last, the last ones -- under a causal mask the longest -- first.
-template <int T, int DH, int NQ>
+// ONE: a page holds at least a step's tokens, which then lie on one page.
+template <int T, int DH, int NQ, bool ONE>
 __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int64_t wg_tiles) {
   using C = PromptCfg<T, DH, NQ>;
   using E = Elem<T>;
@@ -132,59 +144,80 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
   const unsigned page_bytes = (unsigned)(a.c.page * D);
   const int shift = 31 - __builtin_clz((unsigned)a.c.page), page_mask = a.c.page - 1;
 
-  // Pages are looked up by each lane for the tokens whose codes it fetches, two steps ahead; codes are requested one step
-  // ahead.  All through vector loads: a scalar load in flight would make every wait for the LDS a wait for memory.
-  // 16 tokens lie on one page.  Nothing here asks whether it is needed: tokens that no row sees are looked up as the last one
-  // that some row does, chunks beyond dim are fetched as the last one within (they meet zeros of q, or channels that are
-  // not stored), threads beyond the last chunk fetch an earlier one again.
+  // Codes are requested one step ahead, the pages that they lie on looked up two steps ahead.  All through vector loads: a
+  // scalar load in flight would make every wait for the LDS a wait for memory.  16 tokens lie on one page; where all 64
+  // do, it is the same for every lane and addresses are a scalar base and the lane's constant offset.  Nothing here asks
+  // whether it is needed: tokens that no row sees are looked up as the last one that some row does, chunks beyond dim are
+  // fetched as the last one within (they meet zeros of q, or channels that are not stored), threads beyond the last chunk fetch
+  // an earlier one again.
+  constexpr int NP = ONE ? 1 : 4;  // pages of a step
   const unsigned pages = (unsigned)(a.c.pages < 0x7FFFFFFF ? a.c.pages : 0x7FFFFFFF);
-  int k_token[C::NK], k_off[C::NK], v_token[C::NV], v_off[C::NV];  // of the thread's chunks; offsets within 16 tokens
+  int k_token[C::NK], v_token[C::NV];        // of the thread's chunks: the first of the 16 tokens they belong to
+  unsigned k_off[C::NK], v_off[C::NV];       // offset from there
 #pragma unroll
   for (int j = 0; j < C::NK; ++j) {
     const int i = tid + j * kPromptThreads, token = i / (4 * DH) & 63, d = i % (4 * DH) * 16;
     k_token[j] = token & ~15;
-    k_off[j] = (token & 15) * D + (d < D ? d : D - 16);
+    k_off[j] = (unsigned)((token & 15) * D + (d < D ? d : D - 16));
   }
+  // values: two channels of two groups of four tokens, 16 tokens apart; channels 0, 1 of four and 2, 3 go to different waves
 #pragma unroll
   for (int j = 0; j < C::NV; ++j) {
-    const int i = tid + j * kPromptThreads, ksq = i / (16 * DH) & 7, d = i % (16 * DH) * 4;
+    const int i = tid + j * kPromptThreads, ksq = i / (16 * DH) & 7, d = i % (16 * DH) * 4 + (i / (128 * DH) & 1) * 2;
     v_token[j] = (ksq >> 2) * 32;
-    v_off[j] = ((ksq & 3) * D + (d < D ? d : D - 4)) * 4;
+    v_off[j] = (unsigned)(((ksq & 3) * D + (d < D ? d : D - 2)) * 4);
   }
   int idk[C::NK], idv[C::NV][2], idu;
   auto look_up = [&](int t) {
     auto page = [&](int place) {
       const int tok = t * TT + place;
-      return table[(tok < span_hi ? tok : span_hi - 1) >> shift];
+      int at = (tok < span_hi ? tok : span_hi - 1) >> shift;
+      asm volatile("" : "+v"(at));
+      return table[at];
     };
+    if (!ONE) {
 #pragma unroll
-    for (int j = 0; j < C::NK; ++j) idk[j] = page(k_token[j]);
+      for (int j = 0; j < C::NK; ++j) idk[j] = page(k_token[j]);
 #pragma unroll
-    for (int j = 0; j < C::NV; ++j) {
-      idv[j][0] = page(v_token[j]);
-      idv[j][1] = page(v_token[j] + 16);
+      for (int j = 0; j < C::NV; ++j) {
+        idv[j][0] = page(v_token[j]);
+        idv[j][1] = page(v_token[j] + 16);
+      }
     }
-    idu = page((lane & 3) * 16);
+    idu = page(ONE ? 0 : (lane & 3) * 16);
   };
   bool page_ok;
   float mk_in, mv_in;  // lane u (mod 4): maxima of the pages of tokens 16 u .. of the step that is in flight
-  v4i kw[C::NK], vw[C::NV][2];
+  v4i kw[C::NK];
+  v2i vw[C::NV][2];
   auto request = [&](int t) {
-    auto codes_at = [&](const int8_t* codes, int id, int token, int off) {
-      const uint64_t at = (uint64_t)((unsigned)id < pages ? (unsigned)id : 0u) * (unsigned)a.c.heads + (unsigned)h;
-      return *reinterpret_cast<const v4i*>(codes + at * page_bytes + (unsigned)(((t * TT + token) & page_mask) * D + off));
-    };
-    const bool ok = (unsigned)idu < pages;
-    const uint64_t at = (uint64_t)(ok ? (unsigned)idu : 0u) * (unsigned)a.c.heads + (unsigned)h;
-    page_ok = ok;
+    page_ok = (unsigned)idu < pages;
+    uint64_t at = (uint64_t)(page_ok ? (unsigned)idu : 0u) * (unsigned)a.c.heads + (unsigned)h;
     mk_in = a.c.k_absmax[at];
     mv_in = a.c.v_absmax[at];
+    if (ONE) {
+      const uint64_t id = (unsigned)__builtin_amdgcn_readfirstlane(page_ok ? idu : 0);
+      const uint64_t first_byte = (id * (unsigned)a.c.heads + (unsigned)h) * page_bytes + (unsigned)(((t * TT) & page_mask) * D);
+      const int8_t *kp = a.c.k_codes + first_byte, *vp = a.c.v_codes + first_byte;
 #pragma unroll
-    for (int j = 0; j < C::NK; ++j) kw[j] = codes_at(a.c.k_codes, idk[j], k_token[j], k_off[j]);
+      for (int j = 0; j < C::NK; ++j) kw[j] = *reinterpret_cast<const v4i*>(kp + (unsigned)(k_off[j] + k_token[j] * D));
 #pragma unroll
-    for (int j = 0; j < C::NV; ++j) {
-      vw[j][0] = codes_at(a.c.v_codes, idv[j][0], v_token[j], v_off[j]);
-      vw[j][1] = codes_at(a.c.v_codes, idv[j][1], v_token[j] + 16, v_off[j]);
+      for (int j = 0; j < C::NV; ++j) {
+        vw[j][0] = *reinterpret_cast<const v2i*>(vp + (unsigned)(v_off[j] + v_token[j] * D));
+        vw[j][1] = *reinterpret_cast<const v2i*>(vp + (unsigned)(v_off[j] + (v_token[j] + 16) * D));
+      }
+    } else {
+      auto at_page = [&](const int8_t* codes, int id, int token, unsigned off) {
+        const uint64_t page = (uint64_t)((unsigned)id < pages ? (unsigned)id : 0u) * (unsigned)a.c.heads + (unsigned)h;
+        return codes + page * page_bytes + ((unsigned)(((t * TT + token) & page_mask) * D) + off);
+      };
+#pragma unroll
+      for (int j = 0; j < C::NK; ++j) kw[j] = *reinterpret_cast<const v4i*>(at_page(a.c.k_codes, idk[j], k_token[j], k_off[j]));
+#pragma unroll
+      for (int j = 0; j < C::NV; ++j) {
+        vw[j][0] = *reinterpret_cast<const v2i*>(at_page(a.c.v_codes, idv[j][0], v_token[j], v_off[j]));
+        vw[j][1] = *reinterpret_cast<const v2i*>(at_page(a.c.v_codes, idv[j][1], v_token[j] + 16, v_off[j]));
+      }
     }
   };
   auto store = [&](unsigned stage) {
@@ -198,19 +231,21 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
     }
 #pragma unroll
     for (int j = 0; j < C::NV; ++j) {
-      const int i = tid + j * kPromptThreads, ksq = i / (16 * DH) & 7, dq = i % (16 * DH);
-      char* to = lds + stage + C::K_BYTES + ((ksq * 64 * DH + (dq >> 4) * 64 + (dq & 15)) << 4);
+      const int i = tid + j * kPromptThreads, ksq = i / (16 * DH) & 7, dq = i % (16 * DH), two = i / (128 * DH) & 1;
+      char* to = lds + stage + C::K_BYTES + ((ksq * 64 * DH + (dq >> 4) * 64 + (dq & 15)) << 4) + two * 512;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) *reinterpret_cast<f16x8*>(to + k * 256) = codes8(vw[j][0][k], vw[j][1][k]);
+      for (int k = 0; k < 2; ++k) *reinterpret_cast<f16x8*>(to + k * 256) = codes8(vw[j][0][k], vw[j][1][k]);
     }
   };
 
-  float m_ref[NQ], l_run[NQ];
+  // m: what exponentials of the row refer to (0 before its first visible token); the maximum may pass it by kLag, up to top
+  float m_use[NQ], m_top[NQ], l_run[NQ];
   int v_exp = -100000;  // O' is in units of 2^(v_exp - 8)
   f32x4 o[NQ][4 * DH];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
-    m_ref[n] = -__builtin_inff();
+    m_use[n] = 0.0f;
+    m_top[n] = -__builtin_inff();
     l_run[n] = 0.0f;
 #pragma unroll
     for (int k = 0; k < 4 * DH; ++k) o[n][k] = f32x4{0, 0, 0, 0};
@@ -222,14 +257,27 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
     look_up(t0 + 1);
     store(0);
   }
-  float mk_now[4], mv_now[4];
+  // Of the pages of a step: keys' maximum (negative: no such page), log2 of the values' factor + 8 and the factor's
+  // reciprocal; v_next: exponent of the power of two that the factors refer to.
+  float mk[NP], lg[NP], back[NP];
+  int v_next = v_exp;
   auto arrived = [&]() {
     mk_in = page_ok ? mk_in : -1.0f;
-    mv_in = page_ok ? mv_in : 0.0f;
+    const bool any = page_ok && mv_in > 0.0f;
+    int e = any ? __builtin_amdgcn_frexp_expf(mv_in) : v_next;
+    if (!ONE) {
+      e = max(e, __builtin_amdgcn_update_dpp(0, e, kQuadSwap1, 0xF, 0xF, true));
+      e = max(e, __builtin_amdgcn_update_dpp(0, e, kQuadSwap2, 0xF, 0xF, true));
+    }
+    e = __builtin_amdgcn_readfirstlane(e);
+    v_next = e > v_next ? e : v_next;
+    const float l2 = any ? fmaxf(__builtin_amdgcn_logf(__builtin_ldexpf(mv_in, -v_next)), kLeast) : 0.0f;
+    const float inverse = __builtin_amdgcn_exp2f(-l2);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      mk_now[u] = f_from_bits(__builtin_amdgcn_readlane(bits_from_f(mk_in), u));
-      mv_now[u] = f_from_bits(__builtin_amdgcn_readlane(bits_from_f(mv_in), u));
+    for (int u = 0; u < NP; ++u) {
+      mk[u] = f_from_bits(__builtin_amdgcn_readlane(bits_from_f(mk_in), u));
+      lg[u] = f_from_bits(__builtin_amdgcn_readlane(bits_from_f(l2 + kUp), u));
+      back[u] = f_from_bits(__builtin_amdgcn_readlane(bits_from_f(inverse), u));
     }
   };
   if (t0 < t1) arrived();
@@ -263,96 +311,86 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      const float mk[2] = {mk_now[2 * half], mk_now[2 * half + 1]}, mv[2] = {mv_now[2 * half], mv_now[2 * half + 1]};
-      int ve = v_exp;
-      float lg[2], back[2];  // log2 of the pages' value factors, and their reciprocals
+      // logits over f; scalars: see kv_attention.hip
+      float x[2][NQ][4];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        if (mv[u] > 0.0f) {
-          const int e = __builtin_amdgcn_frexp_expf(mv[u]);
-          ve = e > ve ? e : ve;
-        }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        lg[u] = mv[u] > 0.0f ? fmaxf(__builtin_amdgcn_logf(__builtin_ldexpf(mv[u], -ve)), kLeast) : 0.0f;
-        back[u] = __builtin_amdgcn_exp2f(-lg[u]);
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[u][n][e] = sc[u][n][e];
+      const float mk0 = mk[ONE ? 0 : 2 * half], mk1 = mk[ONE ? 0 : 2 * half + 1];
+      if (mk0 < 0.0f || mk1 < 0.0f || base < all_lo || base + 32 > all_hi) {  // uniform over the wave
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          const int from = lo[n] - base - quarter * 4, to = hi[n] - base - quarter * 4;  // counted from the lane's first token
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool out = (16 * u + e < from) | (16 * u + e >= to) | ((u ? mk1 : mk0) < 0.0f);
+              x[u][n][e] = out ? -__builtin_inff() : x[u][n][e];
+            }
+        }
       }
+      // f: at least 1e-30, so that it leaves an infinity one (a smaller one means a logit of 0 either way).  A row's maximum
+      // passes the limit where that of one of its four lanes does.
+      float f[2][NQ], top[NQ];
+      bool grow = v_next != v_exp;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        f[0][n] = max2(row_scale[n] * mk0, 1e-30f);
+        const float a0 = max2(max3(x[0][n][0], x[0][n][1], x[0][n][2]), x[0][n][3]);
+        if (ONE) {
+          f[1][n] = f[0][n];
+          top[n] = max3(max3(a0, x[1][n][0], x[1][n][1]), x[1][n][2], x[1][n][3]) * f[0][n];
+        } else {
+          f[1][n] = max2(row_scale[n] * mk1, 1e-30f);
+          const float a1 = max2(max3(x[1][n][0], x[1][n][1], x[1][n][2]), x[1][n][3]);
+          top[n] = max2(a0 * f[0][n], a1 * f[1][n]);
+        }
+        grow |= top[n] > m_top[n];
+      }
+      if (__any(grow)) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          const float m_old = m_top[n] == -__builtin_inff() ? m_top[n] : m_use[n], m_new = max2(row_max(top[n]), m_old);
+          m_use[n] = m_new == -__builtin_inff() ? 0.0f : m_new;
+          m_top[n] = m_new + kLag;
+          const float alpha = __builtin_amdgcn_exp2f(m_old - m_use[n]);
+          l_run[n] *= alpha;
+          const float scale = __builtin_ldexpf(alpha, v_exp - v_next);
+#pragma unroll
+          for (int k = 0; k < 4 * DH; ++k) o[n][k] *= scale;
+        }
+        v_exp = v_next;
+      }
+      float half_sum[NQ];
       v4i pw[PT][NQ];  // probabilities: eight fp16, as the value product wants them
-      auto softmax = [&](auto masked_) {
-        constexpr bool MASKED = decltype(masked_)::value;
-        int from[MASKED ? NQ : 1], to[MASKED ? NQ : 1];  // first and last visible token, counted from the lane's first
-        if (MASKED) {
-          const int at = base + quarter * 4;
 #pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            from[MASKED ? n : 0] = lo[n] - at;
-            to[MASKED ? n : 0] = hi[n] - at;
+      for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          __builtin_amdgcn_sched_barrier(0);
+          const int pg = ONE ? 0 : 2 * half + u;
+          const float mm = lg[pg] - m_use[n];
+          float w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][n][e], f[u][n], mm));
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const f16x2 top16 = __builtin_convertvector(f32x2{w[e], w[e + 1]}, f16x2);
+            pw[0][n][u * 2 + e / 2] = __builtin_bit_cast(int, top16);
+            if (PT == 2)
+              pw[PT - 1][n][u * 2 + e / 2] =
+                  __builtin_bit_cast(int, __builtin_convertvector(f32x2{w[e] - (float)top16.x, w[e + 1] - (float)top16.y}, f16x2));
           }
+          const float sum = (w[0] + w[1]) + (w[2] + w[3]);
+          if (!ONE) l_run[n] = __builtin_fmaf(sum, back[pg], l_run[n]);
+          else if (u == 0) half_sum[n] = sum;
+          else l_run[n] = __builtin_fmaf(half_sum[n] + sum, back[0], l_run[n]);
         }
-        // a logit: where some are masked in scalars (kv_attention.hip says why)
-        auto logit = [&](int n, int u, int e, float f) {
-          const int at = 16 * u + e;
-          const bool out = (at < from[MASKED ? n : 0]) | (at >= to[MASKED ? n : 0]) | (mk[u] < 0.0f);
-          const float x = sc[u][n][e] * f;
-          return out ? -__builtin_inff() : x;
-        };
-        float top[NQ];
-        bool grow = ve != v_exp;
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          top[n] = -__builtin_inff();
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float f = row_scale[n] * mk[u];
-            if (MASKED) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) top[n] = fmaxf(top[n], logit(n, u, e, f));
-            } else {
-              top[n] = fmaxf(top[n], fmaxf(fmaxf(sc[u][n][0], sc[u][n][1]), fmaxf(sc[u][n][2], sc[u][n][3])) * f);
-            }
-          }
-          top[n] = row_max(top[n]);
-          grow |= top[n] > m_ref[n] + kLag;
-        }
-        if (__any(grow)) {
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            const float m_new = fmaxf(m_ref[n], top[n]);
-            const float alpha = __builtin_amdgcn_exp2f(m_ref[n] - (m_new == -__builtin_inff() ? 0.0f : m_new));
-            l_run[n] *= alpha;
-            const float scale = __builtin_ldexpf(alpha, v_exp - ve);
-#pragma unroll
-            for (int k = 0; k < 4 * DH; ++k) o[n][k] *= scale;
-            m_ref[n] = m_new;
-          }
-          v_exp = ve;
-        }
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          const float m_use = m_ref[n] == -__builtin_inff() ? 0.0f : m_ref[n];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            __builtin_amdgcn_sched_barrier(0);
-            const float mm = m_use - (lg[u] + kUp), f = row_scale[n] * mk[u];
-            float w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              w[e] = __builtin_amdgcn_exp2f(MASKED ? logit(n, u, e, f) - mm : __builtin_fmaf(sc[u][n][e], f, -mm));
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-              const f16x2 top16 = __builtin_convertvector(f32x2{w[e], w[e + 1]}, f16x2);
-              pw[0][n][u * 2 + e / 2] = __builtin_bit_cast(int, top16);
-              if (PT == 2)
-                pw[PT - 1][n][u * 2 + e / 2] =
-                    __builtin_bit_cast(int, __builtin_convertvector(f32x2{w[e] - (float)top16.x, w[e + 1] - (float)top16.y}, f16x2));
-            }
-            const float sum = (w[0] + w[1]) + (w[2] + w[3]);
-            l_run[n] = __builtin_fmaf(sum, back[u], l_run[n]);
-          }
-        }
-      };
-      if (mk[0] < 0.0f || mk[1] < 0.0f || base < all_lo || base + 32 > all_hi) softmax(std::true_type{});  // uniform over the wave
-      else softmax(std::false_type{});
+      }
 #pragma unroll
       for (int k = 0; k < 4 * DH; ++k) {
         if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
@@ -395,7 +433,7 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
         else E::store4(to + d, v);
       }
     if (a.splits > 1 && quarter == 0) {
-      a.part_ml[(slot * 16 + r) * 2] = m_ref[n];
+      a.part_ml[(slot * 16 + r) * 2] = m_top[n] == -__builtin_inff() ? m_top[n] : m_use[n];
       a.part_ml[(slot * 16 + r) * 2 + 1] = l * __builtin_amdgcn_exp2f(-kUp);
     }
   }
@@ -410,13 +448,17 @@ int prompt_rows(int type, int dim) {
 template <int T, int DH, int NQ>
 static int go(const AttnArgs& a, int64_t wg_tiles, bool prepare_only, hipStream_t st) {
   using C = PromptCfg<T, DH, NQ>;
+  using Kern = void (*)(AttnArgs, int64_t);
+  static const Kern kerns[2] = {kv_prompt_k<T, DH, NQ, false>, kv_prompt_k<T, DH, NQ, true>};
   static std::atomic<unsigned> done[kMaxDevices];
-  if (C::LDS_BYTES > 65536 || prepare_only) {
-    const int rc = allow_lds(reinterpret_cast<const void*>(kv_prompt_k<T, DH, NQ>), C::LDS_BYTES, done, 0);
-    if (rc != MPQ_OK || prepare_only) return rc;
+  for (int one = 0; one < 2; ++one) {
+    if (C::LDS_BYTES <= 65536 || (!prepare_only && one != (a.c.page >= 64))) continue;
+    const int rc = allow_lds(reinterpret_cast<const void*>(kerns[one]), C::LDS_BYTES, done, one);
+    if (rc != MPQ_OK) return rc;
   }
+  if (prepare_only) return MPQ_OK;
   const dim3 grid = wide_grid(wg_tiles * a.splits * a.b.seqs * a.c.heads, kPromptThreads);
-  kv_prompt_k<T, DH, NQ><<<grid, kPromptThreads, C::LDS_BYTES, st>>>(a, wg_tiles);
+  kerns[a.c.page >= 64]<<<grid, kPromptThreads, C::LDS_BYTES, st>>>(a, wg_tiles);
   return launch_status();
 }
 
