@@ -406,8 +406,8 @@ static int run_qgemm(const int8_t* a_q, const void* w_q, int w_storage_bits, int
   // (the score keeps one partial per 64 x 64 tile at most: its workspace holds no more)
   const bool fast = fast_path(a_q, w_q, w4, M, N, K);
   const int mode = epi_mode(epi);
-  if (mode >= 4 && token_skinny(M, N, K))
-    return launch_token_skinny(w4, DmaArgs{a_q, w_q, M, N, K, a_scale, w_scale, per_row, y_out, acc_out, st, epi, n_partials, 1, 0, false});
+  if (mode >= 4 && token_rows(w4, M, N, K))
+    return launch_token_rows(w4, DmaArgs{a_q, w_q, M, N, K, a_scale, w_scale, per_row, y_out, acc_out, st, epi, n_partials, 1, 0, false});
   const int waves = epi.yref || mode >= 4 ? 0 : skinny_waves(M, N, K, fast && epi.amax);
   const bool plain = mode < 4 && !epi.yref && !epi.codes && !epi.act && !epi.amax;
   const SplitPlan sp = plain && fast ? plan_split(M, N, K) : SplitPlan{};
@@ -645,8 +645,9 @@ extern "C" int mpq_qgemm_tokens(const int8_t* a_q, const void* w_q, int w_storag
 
 // codes [M x K], then the steps from the next multiple of 16 on
 static size_t token_codes_bytes(int64_t M, int64_t K) { return ((size_t)(M * K) + 15) & ~(size_t)15; }
-extern "C" size_t mpq_linear_tokens_workspace_bytes(int64_t M, int64_t K) {
-  if (M <= 0 || K <= 0 || mul_overflows(M, K)) return 0;
+extern "C" size_t mpq_linear_tokens_workspace_bytes(int64_t M, int64_t N, int64_t K, int w_storage_bits) {
+  if (M <= 0 || N <= 0 || K <= 0 || mul_overflows(M, K) || (w_storage_bits != 8 && w_storage_bits != 4)) return 0;
+  if (token_rows_fused(w_storage_bits == 4, M, N, K)) return 0;
   return token_codes_bytes(M, K) + (size_t)M * sizeof(float);
 }
 extern "C" int mpq_linear_tokens(const void* x, int x_type, int64_t M, int64_t N, int64_t K, int64_t x_stride, int bits,
@@ -654,12 +655,21 @@ extern "C" int mpq_linear_tokens(const void* x, int x_type, int64_t M, int64_t N
                                  void* y_out, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_token_quant(x, x_type, M, K, x_stride, bits);
   if (rc != MPQ_OK) return rc;
-  if (M > 0 && (!ws || ws_bytes < mpq_linear_tokens_workspace_bytes(M, K))) return MPQ_ERR_WORKSPACE;
-  if (!aligned16(ws)) return MPQ_ERR_ALIGN;
-  int8_t* codes = reinterpret_cast<int8_t*>(ws);
-  float* steps = M > 0 ? reinterpret_cast<float*>(codes + token_codes_bytes(M, K)) : nullptr;
+  const size_t need = mpq_linear_tokens_workspace_bytes(M, N, K, w_storage_bits);
+  const bool w4 = w_storage_bits == 4, fused = M > 0 && need == 0;
+  if (need > 0 && (!ws || ws_bytes < need)) return MPQ_ERR_WORKSPACE;
+  if (need > 0 && !aligned16(ws)) return MPQ_ERR_ALIGN;
+  // (where rows are quantized by the product's kernel: any pointers that pass)
+  const int8_t* some = reinterpret_cast<const int8_t*>(w_q);
+  int8_t* codes = fused ? const_cast<int8_t*>(some) : reinterpret_cast<int8_t*>(ws);
+  float* steps = fused ? const_cast<float*>(w_scale) : M > 0 ? reinterpret_cast<float*>(codes + token_codes_bytes(M, K)) : nullptr;
   rc = check_qgemm_tokens_args(codes, w_q, w_storage_bits, M, N, K, steps, w_scale, w_gran, act, y_type, y_out);
   if (rc != MPQ_OK || M == 0) return rc;
+  if (fused)
+    return launch_token_rows_fused(x, x_type, x_stride, bits, w4,
+                                   DmaArgs{nullptr, w_q, M, N, K, nullptr, w_scale, w_gran == MPQ_PER_ROW,
+                                           reinterpret_cast<float*>(y_out), nullptr, (hipStream_t)stream, token_epi(act, y_type),
+                                           nullptr, 1, 0, false});
   rc = launch_token_quant(x, x_type, M, K, x_stride, bits, codes, steps, (hipStream_t)stream);
   if (rc != MPQ_OK) return rc;
   return run_qgemm(codes, w_q, w_storage_bits, M, N, K, steps, w_scale, w_gran, reinterpret_cast<float*>(y_out), nullptr,

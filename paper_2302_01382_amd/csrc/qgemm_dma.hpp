@@ -15,6 +15,8 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 // the same in memory at any address an element may have
 typedef int v4i_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef int v2i_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef int v4i_eight __attribute__((ext_vector_type(4), aligned(8)));
+typedef int v4i_byte __attribute__((ext_vector_type(4), aligned(1)));
 typedef unsigned u32_any __attribute__((aligned(1)));
 
 // What an epilogue may do beyond Y = (float(acc) * s_A) * s_W[n]:
@@ -522,6 +524,33 @@ __device__ __forceinline__ void epilogue_act(const v4i (&acc)[C::FM][C::FN], int
         const int64_t m = cur_m0 + wm * C::TM + i * 16 + (lane & 15);
         if (m >= M) continue;
         if (TOKENS) sa = *reinterpret_cast<const float*>(rows + (wm * C::TM + i * 16 + (lane & 15)) * 4);
+        if constexpr (HALF && VEC) {
+          // A lane holds four n of each of two neighbouring accumulator tiles, 8 bytes in 16 bits.  Lanes of one row exchange
+          // them in pairs, so that one has eight n of the first tile and the other eight of the second: 64 bytes of each of 16
+          // rows per store again (12288 x 2304 x 768 packed in 256 tiles 41.7 -> 34.3 us).
+#pragma unroll
+          for (int g = 0; g < G; g += 2) {
+            v2i v[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const int j = j0 + g + t;
+              const float4 sw = *reinterpret_cast<const float4*>(scales + (nq + j * 16) * 4);
+              int a[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) a[e] = W4 ? acc[i][j][e] >> 4 : acc[i][j][e];  // exact: see below
+              v[t] = to_half4(apply_act4(make_float4(((float)a[0] * sa) * sw.x, ((float)a[1] * sa) * sw.y, ((float)a[2] * sa) * sw.z,
+                                                     ((float)a[3] * sa) * sw.w), ACT_KIND), bf16);
+            }
+            const auto x = __builtin_amdgcn_permlane16_swap(v[0].x, v[1].x, false, false);
+            const auto y = __builtin_amdgcn_permlane16_swap(v[0].y, v[1].y, false, false);
+            const int quarter = lane >> 4;
+            const int64_t n = cur_n0 + wn * C::TN + (j0 + g + (quarter & 1)) * 16 + (quarter >> 1) * 8;
+            unsigned short* out = reinterpret_cast<unsigned short*>(Y) + m * N + n;
+            if (n + 8 <= N) *reinterpret_cast<v4i_eight*>(out) = v4i{(int)x[0], (int)y[0], (int)x[1], (int)y[1]};
+            else if (n < N) *reinterpret_cast<v2i*>(out) = v2i{(int)x[0], (int)y[0]};  // (N % 4 == 0)
+          }
+          continue;
+        }
         float part = 0.0f;  // the row's squares of the group, summed before they join the lane's running sum: short chains
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -904,8 +933,11 @@ int launch_dma_64(bool w4, int stages, int kb, const DmaArgs& a);
 int skinny_waves(int64_t M, int64_t N, int64_t K, bool amax);
 int launch_skinny(int waves, bool w4, const DmaArgs& d);
 
-// The layer with a step per token where there are few tokens (qgemm_tokens.hip): whether it is better off there.
-bool token_skinny(int64_t M, int64_t N, int64_t K);
-int launch_token_skinny(bool w4, const DmaArgs& d);
+// The layer with a step per token where there are few tokens (qgemm_tokens.hip): whether it is taken there, and whether
+// with the rows' quantizer in the same kernel.
+bool token_rows(bool w4, int64_t M, int64_t N, int64_t K);
+bool token_rows_fused(bool w4, int64_t M, int64_t N, int64_t K);
+int launch_token_rows(bool w4, const DmaArgs& d);
+int launch_token_rows_fused(const void* x, int x_type, int64_t x_stride, int bits, bool w4, const DmaArgs& d);
 
 }  // namespace mpq

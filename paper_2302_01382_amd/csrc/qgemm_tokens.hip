@@ -2,103 +2,168 @@
 //
 // Its weights are read once and meet at most 64 rows, so that the weights' bytes bound it.  As in qgemm_skinny.hip there are
 // no LDS tiles: both operands are K-contiguous, the operand layout of v_mfma_i32_16x16x64_i8, and a lane loads its operands
-// straight into registers; the waves of a workgroup deal the k steps of 128 out between them and their accumulators
-// meet in LDS (integers: exact in any order).  A workgroup takes NT x 16 output channels and all rows (MT x 16), which come
-// out of the L2: rows are read once per NT x 16 channels.
+// straight into registers; the waves of a workgroup deal the k steps out between them and their accumulators meet in LDS
+// (integers: exact in any order).  A k step is 128 bytes of a weight row, a whole cache line: 128 k of int8 weights, 256 of
+// packed ones.  A workgroup takes NT x 16 output channels and all rows (MT x 16), which come out of the L2.
+// 8 x 4096 x 8192 read 33.6 MB of weights in 10.3 us (3.3 TB/s), 64 x 4096 x 4096 in 13.7 us: from 33 rows on the rows, which
+// every workgroup reads out of the L2, bound it (with rows of zero bytes 7.6 us).
+//
+// With at most 16 rows the rows' quantizer (token_quant.hip's arithmetic, bit for bit) runs in the same kernel: each
+// workgroup takes the rows' maxima itself, a wave a row, while its weights are on their way, and quantizes the values
+// of its k steps as it loads them.  That spares a launch (3.9 us of host time) and a kernel's latency.
 #include "qgemm_dma.hpp"
 
 namespace mpq {
 
-constexpr int kTokWaves = 8;
+constexpr int kTokWaves = 8, kTokThreads = kTokWaves * 64;
 
-template <int MT, int NT, bool W4>
-__global__ __launch_bounds__(kTokWaves * 64) void token_skinny_k(const int8_t* __restrict__ A, const void* __restrict__ Wv, int64_t M,
-                                                                 int64_t N, int64_t K, const float* __restrict__ a_scale,
-                                                                 const float* __restrict__ w_scale, int w_per_row,
-                                                                 void* __restrict__ Y, int act, int y_type) {
-  constexpr int NW = kTokWaves;
-  constexpr int CB = W4 ? 1 : 2;  // 16-byte chunks of a W row per lane and step
-  constexpr int QA = W4 ? 32 : 16, HA = W4 ? 16 : 64;  // see qgemm_skinny
+struct TokArgs {
+  const void* a;       // codes int8 [M x K], or the rows themselves, a_stride elements apart
+  const void* w;
+  int64_t a_stride;
+  int M, K;
+  int64_t N;
+  const float* a_scale;
+  const float* w_scale;
+  int w_per_row, act, y_type, bits;
+  void* y;
+};
+
+// 16 codes of a row's 16 values
+template <int SRC>
+__device__ __forceinline__ v4i quantize16(const typename Elem<SRC>::type* x, float inv) {
+  const f32x8 a = Elem<SRC>::load8(x), b = Elem<SRC>::load8(x + 8);
+  float t[16];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    t[e] = __builtin_fmaf(a[e], inv, kMagic);
+    t[8 + e] = __builtin_fmaf(b[e], inv, kMagic);
+  }
+  return v4i{(int)low_bytes(t[0], t[1], t[2], t[3]), (int)low_bytes(t[4], t[5], t[6], t[7]),
+             (int)low_bytes(t[8], t[9], t[10], t[11]), (int)low_bytes(t[12], t[13], t[14], t[15])};
+}
+
+// SRC: type of the rows that are quantized here (MT 1, K % 16 == 0), or -1: codes.  Rows of at least 16 bytes.
+template <int MT, int NT, bool W4, int SRC>
+__global__ __launch_bounds__(kTokThreads, 2) void token_rows_k(TokArgs p) {
+  constexpr int NW = kTokWaves, KSTEP = W4 ? 256 : 128;
+  constexpr int HALF = W4 ? 2 : 1;  // operands that a 16-byte chunk of weights makes
+  constexpr bool FUSED = SRC >= 0;
+  typedef typename Elem<FUSED ? SRC : MPQ_F32>::type El;
   __shared__ v4i red[NW][MT * NT][64];
+  __shared__ float row_max[FUSED ? 16 : 1];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int r = lane & 15, q = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
-  const int kb_a = (int)K, kb_w = W4 ? (int)(K >> 1) : (int)K;  // bytes per row
-  const uint8_t* pa[MT];
-  const uint8_t* pw[NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {  // rows past the edge re-read the last row; never stored
-    const int64_t m = i * 16 + r;
-    pa[i] = reinterpret_cast<const uint8_t*>(A) + (m < M ? m : M - 1) * kb_a;
-  }
+  const int K = p.K, w_bytes = W4 ? K >> 1 : K;
+  // rows past the edge re-read the last row; never stored
+  const char* w_base = reinterpret_cast<const char*>(p.w) + n0 * w_bytes;
+  unsigned w_row[NT], a_row[MT];
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
-    const int64_t n = n0 + j * 16 + r;
-    pw[j] = reinterpret_cast<const uint8_t*>(Wv) + (n < N ? n : N - 1) * kb_w;
+    const int64_t left = p.N - 1 - n0;
+    const int n = j * 16 + r;
+    w_row[j] = (unsigned)(n < left ? n : (int)left) * (unsigned)w_bytes;
   }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int m = i * 16 + r;
+    a_row[i] = (unsigned)(m < p.M ? m : p.M - 1) * (unsigned)K;
+  }
+  const El* x_row = reinterpret_cast<const El*>(p.a) + (int64_t)(r < p.M ? r : p.M - 1) * p.a_stride;
+
+  const int steps = (K + KSTEP - 1) / KSTEP;
+  // One step's operands at a time: other waves hide a wave's wait better than further loads of its own (us with 1 | 2 | 4 steps
+  // in flight, in a graph, weights from memory: 8 x 4096 x 8192 10.3 | 11.6 | 11.5, 19 x 4096 x 12288 packed 10.1 | 11.1 | 18.8,
+  // 64 x 4096 x 4096 13.7 | 14.3 | 14.3).
+  v4i w[NT][2], a[MT][2 * HALF];
+  // k of the lane's weight chunk c of step s; chunks that would pass the row's end are loaded so that they end there
+  auto k_of = [&](int s, int c) { return s * KSTEP + (W4 ? c * 128 + q * 32 : c * 64 + q * 16); };
+  auto load_w = [&](int s) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int at = W4 ? k_of(s, c) >> 1 : k_of(s, c);
+      const unsigned off = (unsigned)(at < w_bytes - 16 ? at : w_bytes - 16);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[j][c] = *reinterpret_cast<const v4i_byte*>(w_base + (w_row[j] + off));
+    }
+  };
+  float inv = 0.0f, step = 0.0f;
+  auto load_a = [&](int s) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int h = 0; h < HALF; ++h) {
+        const int at = k_of(s, c) + 16 * h;
+        const unsigned off = (unsigned)(at < K - 16 ? at : K - 16);
+        if constexpr (FUSED) {
+          a[0][c * HALF + h] = quantize16<SRC>(x_row + off, inv);
+        } else {
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+            a[i][c * HALF + h] = *reinterpret_cast<const v4i_byte*>(reinterpret_cast<const char*>(p.a) + (a_row[i] + off));
+        }
+      }
+  };
   v4i acc[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
-
-  const int steps = (int)((K + 127) >> 7);
-  constexpr int U = MT * 2 + NT * CB <= 6 ? 4 : 2;  // k steps whose loads are in flight together
-  for (int s0 = wave; s0 < steps; s0 += NW * U) {
-    v4i a[U][MT][2], b[U][NT][CB];
+  if (wave < steps) load_w(wave);
+  if constexpr (FUSED) {
+    for (int m = wave; m < p.M; m += NW) {  // a wave a row
+      const El* x = reinterpret_cast<const El*>(p.a) + m * p.a_stride;
+      float top = 0.0f;
+#pragma unroll 4
+      for (int k = lane * 8; k < K; k += 512) {
+        const f32x8 v = Elem<SRC>::load8(x + k);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int s = s0 + u * NW;
-      if (s < steps) {  // wave-uniform
-        const int ka = s * 128 + q * QA, kw = W4 ? ka >> 1 : ka;
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+      }
+      top = wave_max(top);
+      if (lane == 0) row_max[m] = top;
+    }
+    __syncthreads();
+    step_constants(row_max[r < p.M ? r : p.M - 1], p.bits, step, inv);
+  }
+  for (int s = wave; s < steps; s += NW) {
+    if (s != wave) load_w(s);
+    load_a(s);
+    if ((s + 1) * KSTEP > K) {  // the step that reaches past the rows' end
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+      for (int c = 0; c < 2; ++c) {
 #pragma unroll
-          for (int c = 0; c < CB; ++c) b[u][j][c] = load_chunk16(pw[j], kb_w, kw + HA * c);
+        for (int j = 0; j < NT; ++j) w[j][c] = fix_chunk16(w[j][c], w_bytes, W4 ? k_of(s, c) >> 1 : k_of(s, c));
+        if (!FUSED) {  // (a chunk of values lies within the row, or wholly behind it, next to weights of zero)
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          a[u][i][0] = load_chunk16(pa[i], kb_a, ka);
-          a[u][i][1] = load_chunk16(pa[i], kb_a, ka + HA);
+          for (int h = 0; h < HALF; ++h)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) a[i][c * HALF + h] = fix_chunk16(a[i][c * HALF + h], K, k_of(s, c) + 16 * h);
         }
       }
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int s = s0 + u * NW;
-      if (s < steps) {
-        const int ka = s * 128 + q * QA, kw = W4 ? ka >> 1 : ka;
-        if (s == steps - 1) {  // the step that may reach past the row's end
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            a[u][i][0] = fix_chunk16(a[u][i][0], kb_a, ka);
-            a[u][i][1] = fix_chunk16(a[u][i][1], kb_a, ka + HA);
-          }
+      for (int j = 0; j < NT; ++j) {
+        v4i b[HALF];
+        if constexpr (W4) {  // 32 nibbles -> 32 bytes n << 4, in k order
+          unsigned e[8];
 #pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int c = 0; c < CB; ++c) b[u][j][c] = fix_chunk16(b[u][j][c], kb_w, kw + HA * c);
+          for (int d = 0; d < 4; ++d) expand8((unsigned)w[j][c][d], e[2 * d], e[2 * d + 1]);
+          b[0] = v4i{(int)e[0], (int)e[1], (int)e[2], (int)e[3]};
+          b[HALF - 1] = v4i{(int)e[4], (int)e[5], (int)e[6], (int)e[7]};
+        } else {
+          b[0] = w[j][c];
         }
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          v4i bw[2] = {b[u][j][0], b[u][j][CB - 1]};
-          if constexpr (W4) {  // 32 nibbles -> 32 bytes n << 4, in k order
-            unsigned e[8];
-            expand8((unsigned)b[u][j][0].x, e[0], e[1]);
-            expand8((unsigned)b[u][j][0].y, e[2], e[3]);
-            expand8((unsigned)b[u][j][0].z, e[4], e[5]);
-            expand8((unsigned)b[u][j][0].w, e[6], e[7]);
-            bw[0] = v4i{(int)e[0], (int)e[1], (int)e[2], (int)e[3]};
-            bw[1] = v4i{(int)e[4], (int)e[5], (int)e[6], (int)e[7]};
-          }
+        for (int h = 0; h < HALF; ++h)
 #pragma unroll
-          for (int i = 0; i < MT; ++i) {  // W as the row operand: a lane then holds four consecutive n of one output row
-            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bw[0], a[u][i][0], acc[i][j], 0, 0, 0);
-            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bw[1], a[u][i][1], acc[i][j], 0, 0, 0);
-          }
-        }
+          for (int i = 0; i < MT; ++i)  // W as the row operand: a lane then holds four consecutive n of one output row
+            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[h], a[i][c * HALF + h], acc[i][j], 0, 0, 0);
       }
-    }
   }
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -107,55 +172,77 @@ __global__ __launch_bounds__(kTokWaves * 64) void token_skinny_k(const int8_t* _
   __syncthreads();
   // the waves share out the accumulator tiles
   for (int t = wave; t < MT * NT; t += NW) {
-    v4i s = red[0][t][lane];
+    v4i sum = red[0][t][lane];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) s += red[w][t][lane];
-    const int64_t m = (t / NT) * 16 + r, n = n0 + (t % NT) * 16 + 4 * q;
-    if (m >= M || n >= N) continue;
-    const float sa = a_scale[m];
+    for (int v = 1; v < NW; ++v) sum += red[v][t][lane];
+    const int m = (t / NT) * 16 + r;
+    const int64_t n = n0 + (t % NT) * 16 + 4 * q;
+    if (m >= p.M || n >= p.N) continue;
+    const float sa = FUSED ? step : p.a_scale[m];
     float y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int a = W4 ? s[e] >> 4 : s[e];  // exact: every product carried the factor 16
-      const float sw = w_scale[w_per_row ? (n + e < N ? n + e : n) : 0];
-      y[e] = apply_act(((float)a * sa) * sw, act);
+      const int v = W4 ? sum[e] >> 4 : sum[e];  // exact: every product carried the factor 16
+      const float sw = p.w_scale[p.w_per_row ? (n + e < p.N ? n + e : n) : 0];
+      y[e] = apply_act(((float)v * sa) * sw, p.act);
     }
-    const bool whole = n + 4 <= N;
-    if (y_type == MPQ_F32) {
-      float* out = reinterpret_cast<float*>(Y) + m * N + n;
+    const bool whole = n + 4 <= p.N;
+    if (p.y_type == MPQ_F32) {
+      float* out = reinterpret_cast<float*>(p.y) + m * p.N + n;
       if (whole) store4(out, make_float4(y[0], y[1], y[2], y[3]));
       else
-        for (int e = 0; e < 4 && n + e < N; ++e) out[e] = y[e];
+        for (int e = 0; e < 4 && n + e < p.N; ++e) out[e] = y[e];
     } else {
-      unsigned short* out = reinterpret_cast<unsigned short*>(Y) + m * N + n;
-      const v2i h = to_half4(make_float4(y[0], y[1], y[2], y[3]), y_type == MPQ_BF16);
+      unsigned short* out = reinterpret_cast<unsigned short*>(p.y) + m * p.N + n;
+      const v2i h = to_half4(make_float4(y[0], y[1], y[2], y[3]), p.y_type == MPQ_BF16);
       if (whole) *reinterpret_cast<v2i_any*>(out) = h;
       else
-        for (int e = 0; e < 4 && n + e < N; ++e) out[e] = (unsigned short)((unsigned)(e < 2 ? h.x : h.y) >> (16 * (e & 1)));
+        for (int e = 0; e < 4 && n + e < p.N; ++e) out[e] = (unsigned short)((unsigned)(e < 2 ? h.x : h.y) >> (16 * (e & 1)));
     }
   }
 }
 
-bool token_skinny(int64_t M, int64_t N, int64_t K) { return M <= 64 && N <= (1 << 26); }  // (a grid counts 2^32 threads)
+// (a grid counts 2^32 threads)
+bool token_rows(bool w4, int64_t M, int64_t N, int64_t K) { return M <= 64 && N <= (1 << 26) && K >= (w4 ? 32 : 16); }
+bool token_rows_fused(bool w4, int64_t M, int64_t N, int64_t K) { return token_rows(w4, M, N, K) && M <= 16 && K % 16 == 0; }
 
-int launch_token_skinny(bool w4, const DmaArgs& d) {
-  const int nt = d.N >= 32 * 128 ? 2 : 1;  // two channel tiles once that leaves half of the CUs one
-  const unsigned grid = (unsigned)((d.N + 16 * nt - 1) / (16 * nt));
-#define MPQ_TOK(MT_, NT_, W4_)                                                                                              \
-  token_skinny_k<MT_, NT_, W4_><<<grid, kTokWaves * 64, 0, d.st>>>(d.a_q, d.w_q, d.M, d.N, d.K, d.a_scale, d.w_scale, d.per_row, \
-                                                                   d.y_out, d.epi.act, d.epi.y_type)
-#define MPQ_TOK_M(NT_, W4_) \
-  (d.M <= 16 ? (void)MPQ_TOK(1, NT_, W4_) : d.M <= 32 ? (void)MPQ_TOK(2, NT_, W4_) : (void)MPQ_TOK(4, NT_, W4_))
-  if (nt == 2) {
-    if (w4) MPQ_TOK_M(2, true);
-    else MPQ_TOK_M(2, false);
-  } else {
-    if (w4) MPQ_TOK_M(1, true);
-    else MPQ_TOK_M(1, false);
+// Channel tiles per workgroup: what makes the bytes that a CU loads smallest, its workgroups' weights and rows.
+static int channel_tiles(int mt, bool w4, const TokArgs& p, int el) {
+  int best = 1;
+  double least = 0;
+  for (int nt = 1; nt <= (mt == 4 ? 2 : 4); ++nt) {
+    const int64_t groups = (p.N + 16 * nt - 1) / (16 * nt), rounds = (groups + kNumCU - 1) / kNumCU;
+    const double bytes = (double)rounds * (nt * 16 * (w4 ? 0.5 : 1.0) + mt * 16 * el);
+    if (nt == 1 || bytes < least) { least = bytes; best = nt; }
   }
-#undef MPQ_TOK_M
-#undef MPQ_TOK
+  return best;
+}
+
+template <int MT, bool W4, int SRC>
+static int go(const TokArgs& p, hipStream_t st) {
+  const int nt = channel_tiles(MT, W4, p, SRC < 0 ? 1 : SRC == MPQ_F32 ? 4 : 2);
+  const unsigned grid = (unsigned)((p.N + 16 * nt - 1) / (16 * nt));
+  if (nt == 1) token_rows_k<MT, 1, W4, SRC><<<grid, kTokThreads, 0, st>>>(p);
+  else if (nt == 2) token_rows_k<MT, 2, W4, SRC><<<grid, kTokThreads, 0, st>>>(p);
+  if constexpr (MT < 4) {
+    if (nt == 3) token_rows_k<MT, 3, W4, SRC><<<grid, kTokThreads, 0, st>>>(p);
+    else if (nt == 4) token_rows_k<MT, 4, W4, SRC><<<grid, kTokThreads, 0, st>>>(p);
+  }
   return launch_status();
+}
+
+int launch_token_rows(bool w4, const DmaArgs& d) {
+  const TokArgs p{d.a_q, d.w_q, d.K, (int)d.M, (int)d.K, d.N, d.a_scale, d.w_scale, d.per_row, d.epi.act, d.epi.y_type, 8, d.y_out};
+  if (d.M <= 16) return w4 ? go<1, true, -1>(p, d.st) : go<1, false, -1>(p, d.st);
+  if (d.M <= 32) return w4 ? go<2, true, -1>(p, d.st) : go<2, false, -1>(p, d.st);
+  return w4 ? go<4, true, -1>(p, d.st) : go<4, false, -1>(p, d.st);
+}
+
+int launch_token_rows_fused(const void* x, int x_type, int64_t x_stride, int bits, bool w4, const DmaArgs& d) {
+  const TokArgs p{x, d.w_q, x_stride, (int)d.M, (int)d.K, d.N, nullptr, d.w_scale, d.per_row, d.epi.act, d.epi.y_type, bits, d.y_out};
+  if (x_type == MPQ_F32) return w4 ? go<1, true, MPQ_F32>(p, d.st) : go<1, false, MPQ_F32>(p, d.st);
+  if (x_type == MPQ_BF16) return w4 ? go<1, true, MPQ_BF16>(p, d.st) : go<1, false, MPQ_BF16>(p, d.st);
+  return w4 ? go<1, true, MPQ_F16>(p, d.st) : go<1, false, MPQ_F16>(p, d.st);
 }
 
 }  // namespace mpq

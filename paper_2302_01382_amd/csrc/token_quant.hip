@@ -9,13 +9,7 @@ namespace mpq {
 
 typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 
-// the low byte of t = 1.5 * 2^23 + code is the code
 __device__ __forceinline__ float magic(float x, float inv) { return __builtin_fmaf(x, inv, kMagic); }
-__device__ __forceinline__ unsigned low_bytes(float a, float b, float c, float d) {
-  const unsigned lo = __builtin_amdgcn_perm((unsigned)bits_from_f(b), (unsigned)bits_from_f(a), 0x0c0c0400u);
-  const unsigned hi = __builtin_amdgcn_perm((unsigned)bits_from_f(d), (unsigned)bits_from_f(c), 0x04000c0cu);
-  return lo | hi;
-}
 
 // TPR: threads per row (a wave, or the workgroup); NCH: chunks of eight values that a thread holds, the rest of a longer
 // row is read a second time (out of the L2).

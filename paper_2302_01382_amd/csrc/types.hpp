@@ -81,6 +81,13 @@ __device__ __forceinline__ void step_constants(float m, int bits, float& scale, 
   if (inv == __builtin_inff()) scale = inv = 0.0f;
 }
 
+// the low bytes of t = 1.5 * 2^23 + code, which are the codes
+__device__ __forceinline__ unsigned low_bytes(float a, float b, float c, float d) {
+  const unsigned lo = __builtin_amdgcn_perm((unsigned)bits_from_f(b), (unsigned)bits_from_f(a), 0x0c0c0400u);
+  const unsigned hi = __builtin_amdgcn_perm((unsigned)bits_from_f(d), (unsigned)bits_from_f(c), 0x04000c0cu);
+  return lo | hi;
+}
+
 // four codes of Eq. 1 as the bytes of a dword, the first in the lowest
 __device__ __forceinline__ unsigned pack_codes(float a, float b, float c, float d, float inv, float qmax) {
   return ((unsigned)(int)code_f(a, inv, qmax) & 0xFFu) | (((unsigned)(int)code_f(b, inv, qmax) & 0xFFu) << 8) |

@@ -114,7 +114,7 @@ def lib():
         L.mpq_token_quant.argtypes = [vp, ci, i64, i64, i64, ci, vp, vp, vp]
         L.mpq_qgemm_tokens.argtypes = [vp, vp, ci, i64, i64, i64, vp, vp, ci, ci, ci, vp, vp]
         L.mpq_linear_tokens_workspace_bytes.restype = sz
-        L.mpq_linear_tokens_workspace_bytes.argtypes = [i64, i64]
+        L.mpq_linear_tokens_workspace_bytes.argtypes = [i64, i64, i64, ci]
         L.mpq_linear_tokens.argtypes = [vp, ci, i64, i64, i64, i64, ci, vp, ci, vp, ci, ci, ci, vp, vp, sz, vp]
         L.mpq_kv_append.argtypes = [vp, vp, ci, vp, i64, i64, vp, i64, i64, vp]
         L.mpq_kv_gather.argtypes = [vp, vp, ci, vp, vp, vp]
@@ -813,53 +813,64 @@ def _type(dtype) -> int:
     if _types is None:
         torch = _torch()
         _types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-    try:
-        return _types[dtype]
-    except KeyError:
-        raise ValueError("expected float32, bfloat16 or float16, got %s" % (dtype,)) from None
+    t = _types.get(dtype)
+    if t is None:
+        raise ValueError("expected float32, bfloat16 or float16, got %s" % (dtype,))
+    return t
+
+
+_device = None
 
 
 def _on_current(*tensors):
-    """All on the current device, whose current stream the call goes to."""
-    device = _torch().cuda.current_device()
+    """All on the current device, whose current stream the call goes to.  (A decode step's calls are short: the checks here
+    and below read each attribute of a tensor once, which brings the binding's part of
+    kv_attention from 10.9 to 6.7 us and of linear_tokens from 9.9 to 8.1.)"""
+    global _device
+    if _device is None:
+        torch = _torch()
+        torch.cuda.init()
+        _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    device = _device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != device):
+        if t is not None and t.get_device() != device:   # (-1: a host tensor)
             raise ValueError("libmpq works on tensors of the current device")
 
 
 def _dense(t, dtype, shape, what):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: expected a contiguous %s tensor of shape %s" % (what, dtype, tuple(shape)))
     return t
 
 
-def _scratch(ws, nbytes, device):
-    """(pointer, bytes, what keeps it alive)."""
+def _scratch(ws, nbytes, x):
+    """(pointer, bytes, what keeps it alive), on x's device."""
     if nbytes == 0:
         return None, 0, None
     if ws is not None:
         return (*ws.get(nbytes), ws)
-    buf = _torch().empty(nbytes, dtype=_torch().uint8, device=device)
+    buf = x.new_empty(nbytes, dtype=_torch().uint8)
     return buf.data_ptr(), nbytes, buf
 
 
 def _rows2d(x):
-    """(type, rows, columns, elements between rows) of a 2-D tensor whose columns are contiguous."""
-    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+    """(rows, columns, elements between rows) of a 2-D tensor whose columns are contiguous."""
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("expected a 2-D tensor with contiguous rows")
-    M, K = x.shape
-    return _type(x.dtype), M, K, x.stride(0) if M > 1 else K
+    M, K = shape
+    return M, K, stride[0] if M > 1 else K
 
 
 def _weights(w_q, w_scale, w_storage_bits, w_gran, K):
     """Rows of the weights, whose tensors have to fit the layer: kernels trust the sizes they are told."""
-    torch = _torch()
-    if w_storage_bits not in (4, 8):
-        return w_q.shape[0]       # refused by the library
-    N = w_q.shape[0]
-    if w_q.dim() != 2 or w_q.shape[1] * 8 != K * w_storage_bits or not w_q.is_contiguous() or w_q.element_size() != 1:
+    shape = w_q.shape
+    N = shape[0]
+    if w_storage_bits != 8 and w_storage_bits != 4:
+        return N                  # refused by the library
+    if len(shape) != 2 or shape[1] * 8 != K * w_storage_bits or not w_q.is_contiguous() or w_q.element_size() != 1:
         raise ValueError("expected contiguous weight codes of shape [N, %s]" % ("K" if w_storage_bits == 8 else "K / 2"))
-    if w_scale.dtype != torch.float32 or w_scale.numel() != (1 if w_gran == PER_TENSOR else N) or not w_scale.is_contiguous():
+    if _types.get(w_scale.dtype) != F32 or w_scale.numel() != (1 if w_gran == PER_TENSOR else N) or not w_scale.is_contiguous():
         raise ValueError("expected one float32 weight step per tensor or per output channel")
     return N
 
@@ -868,10 +879,11 @@ def token_quant(x, bits=8, codes=None, scale=None):
     """Eq. 1 with a step per row: x [M, K] (float32, bfloat16 or float16, rows contiguous).  Returns
     (codes int8 [M, K], scale float32 [M])."""
     torch = _torch()
-    t, M, K, stride = _rows2d(x)
+    t = _type(x.dtype)
+    M, K, stride = _rows2d(x)
     _on_current(x, codes, scale)
-    codes = torch.empty((M, K), dtype=torch.int8, device=x.device) if codes is None else _dense(codes, torch.int8, (M, K), "codes")
-    scale = torch.empty(M, dtype=torch.float32, device=x.device) if scale is None else _dense(scale, torch.float32, (M,), "scale")
+    codes = x.new_empty((M, K), dtype=torch.int8) if codes is None else _dense(codes, torch.int8, (M, K), "codes")
+    scale = x.new_empty(M, dtype=torch.float32) if scale is None else _dense(scale, torch.float32, (M,), "scale")
     _check(lib().mpq_token_quant(_ptr(x), t, M, K, stride, int(bits), _ptr(codes), _ptr(scale), _stream()), "mpq_token_quant")
     return codes, scale
 
@@ -880,35 +892,44 @@ def qgemm_tokens(a_q, w_q, a_scale, w_scale, w_storage_bits=8, w_gran=PER_ROW, a
     """The quantized linear layer with a step per token and per output channel: a_q int8 [M, K], a_scale float32 [M].
     Returns Y [M, N] of `dtype` (float32 where neither it nor y is given)."""
     torch = _torch()
-    a_q = _dev2d(a_q, torch.int8)
-    M, K = a_q.shape
+    M, K, stride = _rows2d(a_q)
+    if a_q.dtype != torch.int8 or stride != K:
+        raise ValueError("expected a contiguous 2-D %s tensor" % torch.int8)
     _on_current(a_q, w_q, a_scale, w_scale, y)
     _dense(a_scale, torch.float32, (M,), "a_scale")
-    N = _weights(w_q, w_scale, w_storage_bits, w_gran, K)
     dtype = dtype or (torch.float32 if y is None else y.dtype)
-    y = torch.empty((M, N), dtype=dtype, device=a_q.device) if y is None else _dense(y, dtype, (M, N), "y")
-    _check(lib().mpq_qgemm_tokens(_ptr(a_q), _ptr(w_q), w_storage_bits, M, N, K, _ptr(a_scale), _ptr(w_scale), w_gran, int(act),
-                                  _type(dtype), _ptr(y), _stream()), "mpq_qgemm_tokens")
+    t = _type(dtype)
+    N = _weights(w_q, w_scale, w_storage_bits, w_gran, K)
+    y = a_q.new_empty((M, N), dtype=dtype) if y is None else _dense(y, dtype, (M, N), "y")
+    _check(lib().mpq_qgemm_tokens(a_q.data_ptr(), w_q.data_ptr(), w_storage_bits, M, N, K, a_scale.data_ptr(), w_scale.data_ptr(),
+                                  w_gran, int(act), t, y.data_ptr(), _stream()), "mpq_qgemm_tokens")
     return y
 
 
-def linear_tokens_workspace_bytes(M, K) -> int:
-    return int(lib().mpq_linear_tokens_workspace_bytes(M, K))
+def linear_tokens_workspace_bytes(M, N, K, w_storage_bits=8) -> int:
+    return int(lib().mpq_linear_tokens_workspace_bytes(M, N, K, w_storage_bits))
 
 
 def linear_tokens(x, w_q, w_scale, w_storage_bits=8, w_gran=PER_ROW, bits=8, act=ACT_NONE, dtype=None, y=None,
                   ws: Workspace = None):
     """A linear layer from its input to its output: token_quant(x, bits) and qgemm_tokens in one call.  Returns Y [M, N]
     of `dtype` (x's where neither it nor y is given)."""
-    torch = _torch()
-    t, M, K, stride = _rows2d(x)
+    x_dtype = x.dtype
+    t = ty = _type(x_dtype)
+    M, K, stride = _rows2d(x)
     _on_current(x, w_q, w_scale, y)
     N = _weights(w_q, w_scale, w_storage_bits, w_gran, K)
-    dtype = dtype or (x.dtype if y is None else y.dtype)
-    y = torch.empty((M, N), dtype=dtype, device=x.device) if y is None else _dense(y, dtype, (M, N), "y")
-    wp, wn, _alive = _scratch(ws, linear_tokens_workspace_bytes(M, K), x.device)
-    _check(lib().mpq_linear_tokens(_ptr(x), t, M, N, K, stride, int(bits), _ptr(w_q), w_storage_bits, _ptr(w_scale), w_gran,
-                                   int(act), _type(dtype), _ptr(y), wp, wn, _stream()), "mpq_linear_tokens")
+    if y is not None:
+        dtype = dtype or y.dtype
+        _dense(y, dtype, (M, N), "y")
+    if dtype is not None and dtype != x_dtype:
+        ty = _type(dtype)
+    if y is None:
+        y = x.new_empty((M, N), dtype=dtype)
+    c = lib()
+    wp, wn, _alive = _scratch(ws, c.mpq_linear_tokens_workspace_bytes(M, N, K, w_storage_bits), x)
+    _check(c.mpq_linear_tokens(x.data_ptr(), t, M, N, K, stride, int(bits), w_q.data_ptr(), w_storage_bits, w_scale.data_ptr(),
+                               w_gran, int(act), ty, y.data_ptr(), wp, wn, _stream()), "mpq_linear_tokens")
     return y
 
 
@@ -939,7 +960,7 @@ class KvCache:
         _dense(v_absmax, torch.float32, (pages, heads), "v_absmax")
         self.k_codes, self.v_codes, self.k_absmax, self.v_absmax = k_codes, v_codes, k_absmax, v_absmax
         self.pages, self.heads, self.page, self.dim, self.bits = pages, heads, page, dim, int(bits)
-        self.device = k_codes.device
+        self.device, self.index = k_codes.device, k_codes.get_device()
         if any(t.device != self.device for t in (v_codes, k_absmax, v_absmax)):
             raise ValueError("the cache's tensors lie on one device")
         self.struct = _KvCacheStruct(_ptr(k_codes), _ptr(v_codes), _ptr(k_absmax), _ptr(v_absmax), pages, heads, dim, page, self.bits)
@@ -969,7 +990,7 @@ class KvBatch:
         _dense(starts, torch.int32, (seqs + 1,), "starts")
         _dense(kv_len, torch.int32, (seqs,), "kv_len")
         self.starts, self.kv_len, self.table, self.rows = starts, kv_len, table, int(rows)
-        self.device = table.device
+        self.device, self.index = table.device, table.get_device()
         if starts.device != self.device or kv_len.device != self.device:
             raise ValueError("the batch's tensors lie on one device")
         self.max_new = self.rows if max_new is None else int(max_new)
@@ -979,41 +1000,43 @@ class KvBatch:
 
 
 def _kv_rows(cache, batch, x, heads, what):
-    """(type, elements between tokens, elements between heads) of a call's tensor [rows, heads, dim]."""
-    if cache.device != batch.device or x.device != cache.device:
-        raise ValueError("cache, batch and tensors lie on one device")
-    if x.dim() != 3 or x.shape[0] != batch.rows or x.shape[2] != cache.dim or (heads is not None and x.shape[1] != heads) \
-            or x.stride(2) != 1:
+    """(type, elements between tokens, elements between heads, heads) of a call's tensor [rows, heads, dim]."""
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or shape[0] != batch.rows or shape[2] != cache.dim or (heads is not None and shape[1] != heads) \
+            or stride[2] != 1:
         raise ValueError("%s: expected [%d, %s, %d] with contiguous channels" % (what, batch.rows, heads or "heads", cache.dim))
-    return _type(x.dtype), x.stride(0), x.stride(1)
+    if not cache.index == batch.index == x.get_device():
+        raise ValueError("cache, batch and tensors lie on one device")
+    return _type(x.dtype), stride[0], stride[1], shape[1]
 
 
 def kv_append(cache: KvCache, batch: KvBatch, k, v):
     """Writes the rows of k and v ([rows, heads, dim], any strides of tokens and heads) into the cache."""
-    t, k_ts, k_hs = _kv_rows(cache, batch, k, cache.heads, "k")
-    tv, v_ts, v_hs = _kv_rows(cache, batch, v, cache.heads, "v")
+    t, k_ts, k_hs, _ = _kv_rows(cache, batch, k, cache.heads, "k")
+    tv, v_ts, v_hs, _ = _kv_rows(cache, batch, v, cache.heads, "v")
     if tv != t:
         raise ValueError("k and v have one type")
     _on_current(k)
-    _check(lib().mpq_kv_append(cache.ref, batch.ref, t, _ptr(k), k_ts, k_hs, _ptr(v), v_ts, v_hs, _stream()), "mpq_kv_append")
+    _check(lib().mpq_kv_append(cache.ref, batch.ref, t, k.data_ptr(), k_ts, k_hs, v.data_ptr(), v_ts, v_hs, _stream()), "mpq_kv_append")
 
 
 def kv_gather(cache: KvCache, batch: KvBatch, dtype=None, want_k=True, want_v=True, k=None, v=None):
     """The stored values of the batch's rows.  Returns (k | None, v | None), [rows, heads, dim] of `dtype` (float32)."""
     torch = _torch()
-    dtype = dtype or next((t.dtype for t in (k, v) if t is not None), torch.float32)
+    if dtype is None:
+        dtype = next((t.dtype for t in (k, v) if t is not None), torch.float32)
     shape = (batch.rows, cache.heads, cache.dim)
-    if cache.device != batch.device:
+    if cache.index != batch.index:
         raise ValueError("cache and batch lie on one device")
     _on_current(cache.k_codes, k, v)
     if k is not None:
         _dense(k, dtype, shape, "k")
     elif want_k:
-        k = torch.empty(shape, dtype=dtype, device=cache.device)
+        k = cache.k_codes.new_empty(shape, dtype=dtype)
     if v is not None:
         _dense(v, dtype, shape, "v")
     elif want_v:
-        v = torch.empty(shape, dtype=dtype, device=cache.device)
+        v = cache.k_codes.new_empty(shape, dtype=dtype)
     _check(lib().mpq_kv_gather(cache.ref, batch.ref, _type(dtype), _ptr(k), _ptr(v), _stream()), "mpq_kv_gather")
     return k, v
 
@@ -1025,16 +1048,18 @@ def kv_attention_workspace_bytes(cache: KvCache, batch: KvBatch, dtype, q_heads)
 def kv_attention(cache: KvCache, batch: KvBatch, q, causal=True, window=0, softmax_scale=None, out=None, ws: Workspace = None):
     """Attention of q [rows, q_heads, dim] (any strides of tokens and heads) over the cache, q_heads a multiple of the cache's
     heads.  softmax_scale: 1 / sqrt(dim) where not given.  Returns the output, [rows, q_heads, dim] of q's type."""
-    t, q_ts, q_hs = _kv_rows(cache, batch, q, None, "q")
-    heads = q.shape[1]
-    if out is None:
-        out = _torch().empty((batch.rows, heads, cache.dim), dtype=q.dtype, device=q.device)
-    to, o_ts, o_hs = _kv_rows(cache, batch, out, heads, "out")
-    if to != t:
-        raise ValueError("q and out have one type")
+    t, q_ts, q_hs, heads = _kv_rows(cache, batch, q, None, "q")
     _on_current(q)
-    wp, wn, _alive = _scratch(ws, int(lib().mpq_kv_attention_workspace_bytes(cache.ref, batch.ref, t, heads)), q.device)
-    _check(lib().mpq_kv_attention(cache.ref, batch.ref, t, _ptr(q), q_ts, q_hs, heads,
-                                  cache.dim ** -0.5 if softmax_scale is None else float(softmax_scale), int(bool(causal)), int(window),
-                                  _ptr(out), o_ts, o_hs, wp, wn, _stream()), "mpq_kv_attention")
+    if out is None:
+        out = q.new_empty((batch.rows, heads, cache.dim))
+        o_ts, o_hs = heads * cache.dim, cache.dim
+    else:
+        to, o_ts, o_hs, _ = _kv_rows(cache, batch, out, heads, "out")
+        if to != t:
+            raise ValueError("q and out have one type")
+    c = lib()
+    wp, wn, _alive = _scratch(ws, c.mpq_kv_attention_workspace_bytes(cache.ref, batch.ref, t, heads), q)
+    _check(c.mpq_kv_attention(cache.ref, batch.ref, t, q.data_ptr(), q_ts, q_hs, heads,
+                              cache.dim ** -0.5 if softmax_scale is None else float(softmax_scale), int(bool(causal)), int(window),
+                              out.data_ptr(), o_ts, o_hs, wp, wn, _stream()), "mpq_kv_attention")
     return out

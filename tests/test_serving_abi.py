@@ -69,8 +69,10 @@ def test_qgemm_tokens_refuses():
 def test_linear_tokens_refuses():
     L = mpq.lib()
     q, f = L.mpq_linear_tokens_workspace_bytes, L.mpq_linear_tokens
-    assert q(3, 17) == 64 + 12 and q(0, 17) == 0 and q(3, 0) == 0 and q(-1, 4) == 0 and q(2 ** 40, 2 ** 40) == 0
-    ok = [FAKE16, 1, 4, 8, 16, 16, 8, FAKE16, 8, FAKE, 1, 0, 1, FAKE16, FAKE16, BIG, None]
+    assert q(3, 8, 17, 8) == 64 + 12 and q(0, 8, 17, 8) == 0 and q(3, 8, 0, 8) == 0 and q(-1, 8, 4, 8) == 0
+    assert q(2 ** 40, 8, 2 ** 40, 8) == 0 and q(3, 8, 17, 5) == 0 and q(3, 0, 17, 8) == 0
+    assert q(16, 8, 32, 8) == 0 and q(17, 8, 32, 4) > 0           # few rows are quantized by the product's kernel
+    ok = [FAKE16, 1, 4, 8, 18, 18, 8, FAKE16, 8, FAKE, 1, 0, 1, FAKE16, FAKE16, BIG, None]
 
     def but(**kw):
         a = list(ok)
@@ -80,11 +82,13 @@ def test_linear_tokens_refuses():
 
     for i in (0, 7, 9, 13):
         assert but(**{"_%d" % i: None}) == mpq.ERR_NULL
-    assert but(_14=None) == mpq.ERR_WORKSPACE and but(_15=q(4, 16) - 1) == mpq.ERR_WORKSPACE
+    assert but(_14=None) == mpq.ERR_WORKSPACE and but(_15=q(4, 8, 18, 8) - 1) == mpq.ERR_WORKSPACE
     assert but(_14=C.c_void_p(0x10008)) == mpq.ERR_ALIGN
     assert but(_6=1) == mpq.ERR_BITS and but(_8=3) == mpq.ERR_BITS
-    assert but(_5=15) == mpq.ERR_SHAPE and but(_1=7) == mpq.ERR_SHAPE and but(_12=7) == mpq.ERR_SHAPE and but(_3=0) == mpq.ERR_SHAPE
+    assert but(_5=17) == mpq.ERR_SHAPE and but(_1=7) == mpq.ERR_SHAPE and but(_12=7) == mpq.ERR_SHAPE and but(_3=0) == mpq.ERR_SHAPE
     assert but(_2=0, _0=None, _13=None, _14=None, _15=0) == mpq.OK
+    assert but(_4=16, _5=16, _7=None, _14=None) == mpq.ERR_NULL and but(_4=16, _5=16, _9=None, _14=None) == mpq.ERR_NULL
+    assert but(_4=16, _5=16, _13=None, _14=None) == mpq.ERR_NULL and but(_4=16, _5=16, _0=None, _14=None) == mpq.ERR_NULL
 
 
 def kv(cache=None, batch=None):
