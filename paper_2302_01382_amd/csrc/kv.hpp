@@ -10,6 +10,8 @@ int check_kv(const mpq_kv_cache* c, const mpq_kv_batch* b, int type);
 
 #if defined(__HIPCC__)
 
+constexpr int64_t kMostTokens = 0x7FFFF000;  // of a sequence: a token's number and a few steps keep within 31 bits
+
 // A sequence of a call.  Device arrays may hold anything: ranges are cut to the call's rows and to the table.
 struct Sequence {
   int64_t row0;  // first row
@@ -27,7 +29,8 @@ __device__ __forceinline__ Sequence sequence(const mpq_kv_batch& b, int page, in
   q.row0 = s0;
   q.n = (int)(s1 - s0);
   q.len = len < 0 ? 0 : len;
-  q.room = (int64_t)b.table_pages * page;
+  const int64_t room = (int64_t)b.table_pages * page;
+  q.room = room < kMostTokens ? room : kMostTokens;
   return q;
 }
 

@@ -1,8 +1,8 @@
 // kv_prompt.hip -- attention over quantized pages where a sequence brings many rows: a prompt's.
 //
 // The mathematics, the operands' order and the precision are kv_attention.hip's; there the codes' bytes count, here the
-// matrix products do.  A workgroup of four waves takes 64 NQ rows of a key head (row, query head pairs: the heads of a group
-// share keys and values), NQ tiles of 16 rows a wave.  Per step of 64 tokens the workgroup turns the codes of keys and
+// matrix products do.  A wave takes NQ tiles of 16 rows of a key head (row, query head pairs: the heads of a group share keys
+// and values), a workgroup its waves' rows.  Per step of 64 tokens the workgroup turns the codes of keys and
 // values into fp16 once, on their way into a double-buffered LDS stage, and every wave multiplies them with its rows: an
 // operand read out of the LDS serves NQ matrix steps.
 //   keys    [token][chunk of 8 channels], chunks swizzled by the token so that 16 tokens' reads of one chunk fall into
@@ -13,13 +13,19 @@
 // a power of two that no maximum so far exceeds (at least -60); the sum divides it out again, page by page.  m is a maximum
 // that may lag behind the true one by up to 6: P' then reaches 2^14, and the accumulators are rescaled only when it lags
 // by more.
+//
+// Two prompts of up to 4500 rows behind up to 1000 tokens, 16 query and 4 key heads of 128 channels in bf16: 292 us, 780
+// TFLOP/s of the pairs that the mask leaves.  Matrix steps take 28 % of the SIMDs' cycles, vector instructions (a third of them the
+// exponentials, a quarter the codes' way into fp16) 40 %, with two waves per SIMD that 220 registers leave room for; a sixth of the
+// time is the last workgroups' alone.  What did not help: the next keys' matrix steps between the exponentials (302 against
+// 302), two groups of waves that take turns with matrix steps and softmax behind barriers (327 against 304), s_setprio around
+// the matrix steps (302 to 307), 64 rows a wave (spilled).
 #include "kv_attn.hpp"
 
 #include <type_traits>
 
 namespace mpq {
 
-constexpr int kPromptWaves = 8, kPromptThreads = kPromptWaves * 64;
 constexpr float kLag = 6.0f, kUp = 8.0f, kLeast = -60.0f;
 
 // Maxima in assembly: the compiler's would first quiet every operand that it has not seen quieted.
@@ -51,17 +57,22 @@ __device__ __forceinline__ void lds_meet() {
 template <int T, int DH, int NQ>
 struct PromptCfg {
   static constexpr int QT = T == MPQ_F32 ? 2 : 1, PT = QT;  // fp16 terms of q and of a probability
-  static constexpr int ROWS = kPromptWaves * 16 * NQ;       // rows of a workgroup
+  // Waves: two workgroups of four share a CU, each at its own pace, and work comes in smaller pieces than with eight; dim > 128
+  // fills the LDS with one workgroup (us, 8 | 4 waves: two prompts of up to 4500 rows of 16 / 4 heads of 128 306 | 292; 8 of 1000
+  // of 12 heads of 64 60 | 42; 4096 rows of 32 / 8 heads of 128, no mask, where every piece is equal, 297 | 323; 4 of 300 of
+  // 8 / 2 heads of 256 46.3 | 47.8).
+  static constexpr int NW = DH == 4 ? 8 : 4, THREADS = NW * 64;
+  static constexpr int ROWS = NW * 16 * NQ;                 // rows of a workgroup
   static constexpr int K_BYTES = 64 * DH * 128, STAGE = 2 * K_BYTES;
   static constexpr int LDS_BYTES = 2 * STAGE;
-  static constexpr int NK = (DH + 1) / 2, NV = (DH + 1) / 2;    // chunks per thread and step: 16 bytes of keys; twice 8 of values
+  static constexpr int NK = 256 * DH / THREADS, NV = NK;    // chunks per thread and step: 16 bytes of keys; twice 8 of values
 };
 
-// grid: pairs (sequence, head) fastest, so that those that share keys and values share an XCD's L2 where their number is a
-// multiple of 8; then splits; row tiles last, the last ones -- under a causal mask the longest -- first.
+// grid: pairs (sequence, head) fastest, a place further from one row tile to the next, so that each XCD has tiles of long and of
+// short sequences; then splits; row tiles last, the last ones -- under a causal mask the longest -- first.
 // ONE: a page holds at least a step's tokens, which then lie on one page.
 template <int T, int DH, int NQ, bool ONE>
-__global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int64_t wg_tiles) {
+__global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) void kv_prompt_k(AttnArgs a, int64_t wg_tiles) {
   using C = PromptCfg<T, DH, NQ>;
   using E = Elem<T>;
   typedef typename E::type El;
@@ -70,8 +81,9 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, quarter = lane >> 4;
   int64_t g = block_index();
-  const int64_t pairs = (int64_t)a.b.seqs * a.c.heads, pair = g % pairs;
+  const int64_t pairs = (int64_t)a.b.seqs * a.c.heads, turn = g % pairs;
   g /= pairs;
+  const int64_t pair = (turn + g) % pairs;
   const int split = (int)(g % a.splits);
   g /= a.splits;
   if (g >= wg_tiles) return;
@@ -156,21 +168,21 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
   unsigned k_off[C::NK], v_off[C::NV];       // offset from there
 #pragma unroll
   for (int j = 0; j < C::NK; ++j) {
-    const int i = tid + j * kPromptThreads, token = i / (4 * DH) & 63, d = i % (4 * DH) * 16;
+    const int i = tid + j * C::THREADS, token = i / (4 * DH) & 63, d = i % (4 * DH) * 16;
     k_token[j] = token & ~15;
     k_off[j] = (unsigned)((token & 15) * D + (d < D ? d : D - 16));
   }
   // values: two channels of two groups of four tokens, 16 tokens apart; channels 0, 1 of four and 2, 3 go to different waves
 #pragma unroll
   for (int j = 0; j < C::NV; ++j) {
-    const int i = tid + j * kPromptThreads, ksq = i / (16 * DH) & 7, d = i % (16 * DH) * 4 + (i / (128 * DH) & 1) * 2;
+    const int i = tid + j * C::THREADS, ksq = i / (16 * DH) & 7, d = i % (16 * DH) * 4 + (i / (128 * DH) & 1) * 2;
     v_token[j] = (ksq >> 2) * 32;
     v_off[j] = (unsigned)(((ksq & 3) * D + (d < D ? d : D - 2)) * 4);
   }
   int idk[C::NK], idv[C::NV][2], idu;
   auto look_up = [&](int t) {
     auto page = [&](int place) {
-      const int tok = t * TT + place;
+      const int tok = t * TT + place;  // (at most a few steps past kMostTokens)
       int at = (tok < span_hi ? tok : span_hi - 1) >> shift;
       asm volatile("" : "+v"(at));
       return table[at];
@@ -223,7 +235,7 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
   auto store = [&](unsigned stage) {
 #pragma unroll
     for (int j = 0; j < C::NK; ++j) {
-      const int i = tid + j * kPromptThreads, token = i / (4 * DH) & 63, ch = i % (4 * DH) * 2;
+      const int i = tid + j * C::THREADS, token = i / (4 * DH) & 63, ch = i % (4 * DH) * 2;
       const int swz = DH == 1 ? (token >> 1) & 7 : token & 15;
       char* row = lds + stage + token * (DH * 128);
       *reinterpret_cast<f16x8*>(row + ((ch ^ swz) << 4)) = codes8(kw[j].x, kw[j].y);
@@ -231,7 +243,7 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
     }
 #pragma unroll
     for (int j = 0; j < C::NV; ++j) {
-      const int i = tid + j * kPromptThreads, ksq = i / (16 * DH) & 7, dq = i % (16 * DH), two = i / (128 * DH) & 1;
+      const int i = tid + j * C::THREADS, ksq = i / (16 * DH) & 7, dq = i % (16 * DH), two = i / (128 * DH) & 1;
       char* to = lds + stage + C::K_BYTES + ((ksq * 64 * DH + (dq >> 4) * 64 + (dq & 15)) << 4) + two * 512;
 #pragma unroll
       for (int k = 0; k < 2; ++k) *reinterpret_cast<f16x8*>(to + k * 256) = codes8(vw[j][0][k], vw[j][1][k]);
@@ -442,7 +454,7 @@ __global__ __launch_bounds__(kPromptThreads, 1) void kv_prompt_k(AttnArgs a, int
 // rows of a workgroup: as many row tiles per wave as the registers hold
 int prompt_rows(int type, int dim) {
   const int dh = dim <= 64 ? 1 : dim <= 128 ? 2 : 4;
-  return kPromptWaves * 16 * (dh == 4 || (type == MPQ_F32 && dh == 2) ? 1 : 2);
+  return dh == 4 ? 128 : type == MPQ_F32 && dh == 2 ? 64 : 128;
 }
 
 template <int T, int DH, int NQ>
@@ -457,8 +469,8 @@ static int go(const AttnArgs& a, int64_t wg_tiles, bool prepare_only, hipStream_
     if (rc != MPQ_OK) return rc;
   }
   if (prepare_only) return MPQ_OK;
-  const dim3 grid = wide_grid(wg_tiles * a.splits * a.b.seqs * a.c.heads, kPromptThreads);
-  kerns[a.c.page >= 64]<<<grid, kPromptThreads, C::LDS_BYTES, st>>>(a, wg_tiles);
+  const dim3 grid = wide_grid(wg_tiles * a.splits * a.b.seqs * a.c.heads, C::THREADS);
+  kerns[a.c.page >= 64]<<<grid, C::THREADS, C::LDS_BYTES, st>>>(a, wg_tiles);
   return launch_status();
 }
 
