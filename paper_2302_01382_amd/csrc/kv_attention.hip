@@ -420,14 +420,21 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   E::store4(to, l > 0.0f ? v / l : f32x4{0, 0, 0, 0});
 }
 
-// Rows of a sequence and key head from which on kv_prompt.hip takes a call.
-constexpr int64_t kPromptFrom = 128;
-
+// Which kernel takes a call, in what pieces.  us on the device, prompt kernel | decode kernel (rows, heads x group, dim; nothing
+// held): 300 12x1 64 11.3 | 8.7, 300 2x8 128 13.2 | 12.9, 1200 1x1 64 17.7 | 12.8, 600 2x4 256 35 | 29 -- 300 8x4 128 13.7 | 18.4,
+// 600 8x4 128 24 | 37, 2400 12x1 64 58 | 66, 1200 2x4 256 48 | 67: the prompt kernel from half a chip of 64-row pieces on.
+// Pieces of 128 rows read and convert codes for twice the rows, but a step takes long with few workgroups on a CU (us, 128 |
+// 64 rows): 600 8x4 128 32 | 24, 1200 8x4 128 53 | 38, 2400 12x1 64 80 | 58 -- 2400 8x4 128 87 | 98, 8 x 1000 12x1 64 42 | 47, 2 x 4500
+// 4x4 128 288 | 390: 64 while 128 make at most a round of the chip.
+// Splits along the tokens (us, one or two workgroups' worth per CU): 300 rows behind 16000 tokens 8x4 128 137 split in six |
+// 179 in three, 4 x 40 behind 4000 39 | 48; 1500 behind 500 4x4 128 76 in two | 67 in one, 2400 1x1 64 29 in four, 21 in one: where pieces leave
+// half the chip idle, and none of less than 768 tokens.
 // How a call is cut up.
 struct AttnPlan {
   int64_t row_tiles, tiles;
   int splits, tile_rows;
-  int64_t wg_tiles;  // > 0: row tiles of kv_prompt.hip
+  int64_t wg_tiles;  // > 0: row tiles of kv_prompt.hip, of
+  int wg_rows;       // so many rows
   size_t ws_bytes;
 };
 static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int type, int q_heads, AttnPlan& p) {
@@ -439,17 +446,24 @@ static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int type
   p.tiles = p.row_tiles * b.seqs * c.heads;
   p.splits = 1;
   p.tile_rows = (int)(p.row_tiles > 1 ? 16 : most * (q_heads / c.heads));
-  p.wg_tiles = 0;
+  p.wg_tiles = p.wg_rows = 0;
   p.ws_bytes = 0;
   if (p.tiles == 0) return MPQ_OK;
-  // two workgroups per CU are on the chip at a time; none with less than 512 tokens
   const int64_t len = b.max_len < (int64_t)b.table_pages * c.page ? b.max_len : (int64_t)b.table_pages * c.page;
-  const int64_t pair_rows = most * (q_heads / c.heads);
-  if (pair_rows >= kPromptFrom) p.wg_tiles = (pair_rows + prompt_rows(type, c.dim) - 1) / prompt_rows(type, c.dim);
-  const int64_t slots = p.wg_tiles > 0 ? kNumCU : 2 * kNumCU, units = p.wg_tiles > 0 ? p.wg_tiles * b.seqs * c.heads : p.tiles;
-  const int64_t want = slots / units, most_splits = (len + 511) / 512;
-  int64_t splits = want < most_splits ? want : most_splits;
-  p.splits = (int)(splits < 1 ? 1 : splits);
+  const int64_t pair_rows = most * (q_heads / c.heads), pairs = (int64_t)b.seqs * c.heads;
+  auto pieces = [&](int64_t rows) { return (pair_rows + rows - 1) / rows * pairs; };
+  const int wide = prompt_rows(type, c.dim);
+  const int64_t units = pieces(wide);
+  const int64_t cut = (c.dim <= 128 ? 2 : 1) * kNumCU / units, most_cut = len < 768 ? 1 : len / 768;
+  const int64_t splits = units > kNumCU / 2 ? 1 : cut < most_cut ? cut : most_cut;
+  if (pair_rows >= 128 && pieces(64) * splits >= kNumCU / 2) {
+    p.splits = (int)splits;
+    p.wg_rows = splits == 1 && units <= 2 * kNumCU && c.dim <= 128 ? 64 : wide;
+    p.wg_tiles = (pair_rows + p.wg_rows - 1) / p.wg_rows;
+  } else {  // two workgroups per CU are on the chip at a time; none with less than 512 tokens
+    const int64_t want = 2 * kNumCU / p.tiles, most_splits = (len + 511) / 512, n = want < most_splits ? want : most_splits;
+    p.splits = (int)(n < 1 ? 1 : n);
+  }
   if (blocks_z(p.tiles * (p.splits > 16 ? p.splits : 16), kAttnWaves * 64) > 65535u) return MPQ_ERR_SHAPE;
   p.ws_bytes = p.splits > 1 ? (size_t)p.tiles * p.splits * 16 * (c.dim + 2) * sizeof(float) : 0;
   return MPQ_OK;
@@ -467,7 +481,7 @@ static int launch_attention(const AttnArgs& a, const AttnPlan& p, hipStream_t st
   else if (dh == 2) MPQ_ATTN(2);
   else MPQ_ATTN(4);
 #undef MPQ_ATTN
-  const int rc = p.wg_tiles > 0 ? launch_prompt(T, a, p.wg_tiles, false, st) : launch_status();
+  const int rc = p.wg_tiles > 0 ? launch_prompt(T, a, p.wg_tiles, p.wg_rows, false, st) : launch_status();
   if (rc != MPQ_OK || p.splits == 1) return rc;
   kv_attention_join_k<T><<<wide_grid(p.tiles * p.tile_rows, kBlock), kBlock, 0, st>>>(a);
   return launch_status();

@@ -25,9 +25,10 @@ struct AttnArgs {
   float* part_ml;     // [tile][split][16][2]
 };
 
-// defined in kv_prompt.hip: rows of a workgroup there, and the launch of wg_tiles such row tiles per sequence and key head
+// defined in kv_prompt.hip: the most rows of a workgroup there, and the launch of wg_tiles row tiles of wg_rows (those, or for
+// dim <= 128 also 64) per sequence and key head
 int prompt_rows(int type, int dim);
-int launch_prompt(int type, const AttnArgs& a, int64_t wg_tiles, bool prepare_only, hipStream_t st);
+int launch_prompt(int type, const AttnArgs& a, int64_t wg_tiles, int wg_rows, bool prepare_only, hipStream_t st);
 
 #if defined(__HIPCC__)
 

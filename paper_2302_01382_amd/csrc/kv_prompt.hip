@@ -451,11 +451,8 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
   }
 }
 
-// rows of a workgroup: as many row tiles per wave as the registers hold
-int prompt_rows(int type, int dim) {
-  const int dh = dim <= 64 ? 1 : dim <= 128 ? 2 : 4;
-  return dh == 4 ? 128 : type == MPQ_F32 && dh == 2 ? 64 : 128;
-}
+// as many row tiles per wave as the registers hold
+int prompt_rows(int type, int dim) { return type == MPQ_F32 && dim > 64 && dim <= 128 ? 64 : 128; }
 
 template <int T, int DH, int NQ>
 static int go(const AttnArgs& a, int64_t wg_tiles, bool prepare_only, hipStream_t st) {
@@ -474,23 +471,29 @@ static int go(const AttnArgs& a, int64_t wg_tiles, bool prepare_only, hipStream_
   return launch_status();
 }
 
-int launch_prompt(int type, const AttnArgs& a, int64_t wg_tiles, bool prepare_only, hipStream_t st) {
-  const int dh = a.c.dim <= 64 ? 1 : a.c.dim <= 128 ? 2 : 4;
-#define MPQ_GO(T_, DH_, NQ_) go<T_, DH_, NQ_>(a, wg_tiles, prepare_only, st)
-  if (type == MPQ_F32) return dh == 1 ? MPQ_GO(MPQ_F32, 1, 2) : dh == 2 ? MPQ_GO(MPQ_F32, 2, 1) : MPQ_GO(MPQ_F32, 4, 1);
-  if (type == MPQ_BF16) return dh == 1 ? MPQ_GO(MPQ_BF16, 1, 2) : dh == 2 ? MPQ_GO(MPQ_BF16, 2, 2) : MPQ_GO(MPQ_BF16, 4, 1);
-  return dh == 1 ? MPQ_GO(MPQ_F16, 1, 2) : dh == 2 ? MPQ_GO(MPQ_F16, 2, 2) : MPQ_GO(MPQ_F16, 4, 1);
-#undef MPQ_GO
+template <int T>
+static int go_type(const AttnArgs& a, int64_t wg_tiles, int wg_rows, bool prepare_only, hipStream_t st) {
+  constexpr int WIDE = T == MPQ_F32 ? 1 : 2;
+  if (a.c.dim > 128) return go<T, 4, 1>(a, wg_tiles, prepare_only, st);
+  if (a.c.dim > 64) return wg_rows == 64 ? go<T, 2, 1>(a, wg_tiles, prepare_only, st) : go<T, 2, WIDE>(a, wg_tiles, prepare_only, st);
+  return wg_rows == 64 ? go<T, 1, 1>(a, wg_tiles, prepare_only, st) : go<T, 1, 2>(a, wg_tiles, prepare_only, st);
+}
+
+int launch_prompt(int type, const AttnArgs& a, int64_t wg_tiles, int wg_rows, bool prepare_only, hipStream_t st) {
+  if (type == MPQ_F32) return go_type<MPQ_F32>(a, wg_tiles, wg_rows, prepare_only, st);
+  if (type == MPQ_BF16) return go_type<MPQ_BF16>(a, wg_tiles, wg_rows, prepare_only, st);
+  return go_type<MPQ_F16>(a, wg_tiles, wg_rows, prepare_only, st);
 }
 
 int prepare_prompt() {
   for (int type : {MPQ_F32, MPQ_BF16, MPQ_F16})
-    for (int dim : {64, 128, 256}) {
-      AttnArgs a{};
-      a.c.dim = dim;
-      const int rc = launch_prompt(type, a, 0, true, nullptr);
-      if (rc != MPQ_OK) return rc;
-    }
+    for (int dim : {64, 128, 256})
+      for (int rows : {64, 128}) {
+        AttnArgs a{};
+        a.c.dim = dim;
+        const int rc = launch_prompt(type, a, 0, rows, true, nullptr);
+        if (rc != MPQ_OK) return rc;
+      }
   return MPQ_OK;
 }
 
