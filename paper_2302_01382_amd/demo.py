@@ -9,7 +9,9 @@
 3. the two searches (Alg. 1 bisection, Alg. 2 greedy) for the lowest-precision configuration whose
    score stays above the target (a fraction of the score with every layer at the widest width),
 4. the deployment estimates of the result: model size and latency relative to the widest width
-   (kernel latencies measured on this GPU).
+   (kernel latencies measured on this GPU),
+5. the same searches over a self-attention layer as a generating model serves it: its weights and its key/value cache
+   get a width each.
 
 The score is 1 - ||Y - Y_ref||^2 / ||Y_ref||^2 against the fp32 output of the unquantized stack: a
 stand-in for the task accuracy of the paper, whose datasets and trained weights are not needed here.
@@ -19,6 +21,7 @@ from __future__ import annotations
 import argparse
 
 from . import hessian, latency, mpq, workloads
+from .attention import QuantAttention
 from .stack import QuantStack
 
 
@@ -75,6 +78,24 @@ def main() -> None:
             print("%-8s %-10s %-40s %8.6f %6d %9.3f %9.3f"
                   % (name, search, " ".join(str(b) for b in bits), score, model.evaluations - before,
                      latency.relative_footprint(shapes, bits, top), table.relative(shapes, bits, top)))
+    # a self-attention layer: four ragged prompts, then four tokens of each one by one
+    g = torch.Generator().manual_seed(args.seed)
+    dim = 64 if args.width % 64 == 0 else 16
+    heads = max(1, args.width // dim)
+    kv_heads = max(1, heads // 4) if heads % 4 == 0 else heads
+    lengths = [max(1, args.rows // 8 * n // 4) + 4 for n in (4, 3, 2, 1)]
+    rand = lambda *shape: torch.randn(*shape, generator=g).cuda()  # noqa: E731
+    att = QuantAttention(rand(sum(lengths), args.width), lengths, rand((heads + 2 * kv_heads) * dim, args.width) * args.width ** -0.5,
+                         rand(args.width, heads * dim) * (heads * dim) ** -0.5, kv_heads, dim, args.bits, single_tokens=4)
+    base = att.evaluate_once([top] * len(att))
+    lost = att.sensitivity(low)
+    order = att.order_by(lost)
+    print("\nself-attention layer: %d query and %d key heads of %d channels, sequences of %s tokens; score at %d bits: %.6f"
+          % (heads, kv_heads, dim, ", ".join(str(n) for n in lengths), top, base))
+    print("lost at %d bits: %s" % (low, ", ".join("%s %.2e" % (n, l) for n, l in zip(att.TENSORS, lost))))
+    for search, run in (("bisection", att.bisection), ("greedy", att.greedy)):
+        bits, asked = run(order, args.target * base)
+        print("%-10s %s: score %.6f" % (search, ", ".join("%s %d" % (n, b) for n, b in zip(att.TENSORS, bits)), att.evaluate_once(bits)))
     print("\n(evals: evaluations that ran on the GPU; configurations already scored are answered from a table)")
 
 
