@@ -364,7 +364,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
       continue;
     }
     El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + at / a.group) * a.o_ts + (h * a.group + at % a.group) * a.o_hs + d;
-    E::store4(to, l > 0.0f ? v / l : f32x4{0, 0, 0, 0});
+    E::store4(to, l == 0.0f ? f32x4{0, 0, 0, 0} : v / l);  // (a row with a NaN in q has one in l)
   }
 }
 
@@ -417,7 +417,7 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
     v += *reinterpret_cast<const f32x4*>(sm_o + 4 * (threadIdx.x + i * quads));
   }
   El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + at / a.group) * a.o_ts + (h * a.group + at % a.group) * a.o_hs + d;
-  E::store4(to, l > 0.0f ? v / l : f32x4{0, 0, 0, 0});
+  E::store4(to, l == 0.0f ? f32x4{0, 0, 0, 0} : v / l);  // (a row with a NaN in q has one in l)
 }
 
 // Which kernel takes a call, in what pieces.  us on the device, prompt kernel | decode kernel (rows, heads x group, dim; nothing

@@ -14,9 +14,9 @@
 // that may lag behind the true one by up to 6: P' then reaches 2^14, and the accumulators are rescaled only when it lags
 // by more.
 //
-// Two prompts of up to 4500 rows behind up to 1000 tokens, 16 query and 4 key heads of 128 channels in bf16: 292 us, 780
-// TFLOP/s of the pairs that the mask leaves.  Matrix steps take 28 % of the SIMDs' cycles, vector instructions (a third of them the
-// exponentials, a quarter the codes' way into fp16) 40 %, with two waves per SIMD that 220 registers leave room for; a sixth of the
+// Two prompts of up to 4500 rows behind up to 1000 tokens, 16 query and 4 key heads of 128 channels in bf16: 283 us, 805
+// TFLOP/s of the pairs that the mask leaves.  Matrix steps take 32 % of the SIMDs' cycles, vector instructions (a third of them the
+// exponentials, a quarter the codes' way into fp16) 50 %, with two waves per SIMD that 220 registers leave room for; a sixth of the
 // time is the last workgroups' alone.  What did not help: the next keys' matrix steps between the exponentials (302 against
 // 302), two groups of waves that take turns with matrix steps and softmax behind barriers (327 against 304), s_setprio around
 // the matrix steps (302 to 307), 64 rows a wave (spilled).
@@ -56,9 +56,11 @@ __device__ __forceinline__ void lds_meet() {
 
 template <int T, int DH, int NQ>
 struct PromptCfg {
-  static constexpr int QT = T == MPQ_F32 ? 2 : 1, PT = QT;  // fp16 terms of q and of a probability
+  // fp16 terms of q, and of a probability: a second one takes a fifth of the time (fp16, two prompts of up to 4500 rows 283 | 347 us)
+  // and an fp16 output's distance to 64 bits from 3.0e-4 to 2.1e-4, its own rounding's; bf16's is 1.7e-3 either way
+  static constexpr int QT = T == MPQ_F32 ? 2 : 1, PT = T == MPQ_BF16 ? 1 : 2;
   // Waves: two workgroups of four share a CU, each at its own pace, and work comes in smaller pieces than with eight; dim > 128
-  // fills the LDS with one workgroup (us, 8 | 4 waves: two prompts of up to 4500 rows of 16 / 4 heads of 128 306 | 292; 8 of 1000
+  // fills the LDS with one workgroup (us, 8 | 4 waves: two prompts of up to 4500 rows of 16 / 4 heads of 128 306 | 283; 8 of 1000
   // of 12 heads of 64 60 | 42; 4096 rows of 32 / 8 heads of 128, no mask, where every piece is equal, 297 | 323; 4 of 300 of
   // 8 / 2 heads of 256 46.3 | 47.8).
   static constexpr int NW = DH == 4 ? 8 : 4, THREADS = NW * 64;
@@ -429,7 +431,7 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
     l += across(l, 32);
     const int at = w0 + n * 16 + r;
     if (at >= nrows) continue;
-    const float f = l > 0.0f ? __builtin_ldexpf(1.0f / qmax, v_exp) * (a.splits > 1 ? __builtin_amdgcn_exp2f(-kUp) : 1.0f / l) : 0.0f;
+    const float f = l == 0.0f ? 0.0f : __builtin_ldexpf(1.0f / qmax, v_exp) * (a.splits > 1 ? __builtin_amdgcn_exp2f(-kUp) : 1.0f / l);
     const int64_t slot = (pair * a.row_tiles + (at >> 4)) * a.splits + split;
     float* part = a.part_o + (slot * 16 + r) * D;
     const int i = at / group;

@@ -3,7 +3,7 @@ of 64 rows of a key head, of 128, and split along the tokens.  Bounds: check_att
 import numpy as np
 import pytest
 
-from test_gpu_kv import DTYPES, check_attention, filled, tables, tokens, Pair
+from test_gpu_kv import DTYPES, NAN, check_attention, filled, tables, tokens, Pair
 from test_gpu_parity import mpq
 from test_gpu_tokens import dev, full, rng
 
@@ -137,6 +137,25 @@ def test_prompts_from_a_replayed_graph_on_another_stream_and_twice():
             other = mpq.kv_attention(c.dev, b, q)
         torch.cuda.synchronize()
         assert torch.equal(other, want) and torch.equal(outs[0], want) and torch.equal(outs[1], want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new,held", [(1, 90), (1, 5000), (128, 20), (64, 1600)])
+def test_a_row_with_nan_or_inf_spoils_itself_alone(dtype, new, held):
+    """Single tokens and prompts, split and not."""
+    import torch
+    r = rng(new + held)
+    lengths = [new + held] * 8
+    c, table = filled(r, 8, lengths, 4, 64, 64, 8, dtype)
+    b = c.batch([new] * 8, lengths, table, new, new + held)
+    q = queries(r, b.rows, 8, 64, dtype)
+    clean = mpq.kv_attention(c.dev, b, q)
+    spoilt = q.clone()
+    spoilt[3, 2, 5], spoilt[b.rows - 1, 7, :], spoilt[0, 0, 63] = NAN, NAN, float("inf")
+    got = mpq.kv_attention(c.dev, b, spoilt)
+    bad = torch.zeros(b.rows, 8, dtype=torch.bool, device="cuda")
+    bad[3, 2] = bad[b.rows - 1, 7] = bad[0, 0] = True
+    assert got[bad].isnan().all() and torch.equal(got[~bad], clean[~bad])
 
 
 def test_offsets_past_32_bits_of_a_prompt():
