@@ -471,8 +471,8 @@ int mpq_linear_tokens(const void* x, int x_type, int64_t M, int64_t N, int64_t K
  *   kv_len    device int32 [seqs]: tokens of each sequence, those rows included
  *   table     device int32 [seqs][table_pages]
  *   rows      of the call's tensors;  max_new >= every starts[s + 1] - starts[s] and max_len >= every kv_len[s] (HOST
- *             bounds that size the launches: rows past max_new of a sequence are not processed, max_len only
- *             decides how the work is split)
+ *             bounds that size the launches: of a sequence with more rows than max_new only a part is processed,
+ *             max_len only decides how the work is split).  Tokens of a sequence from 2^31 - 4096 on have no place
  *   Contents of device arrays are not checked on the host and never cause a fault: ranges are cut to rows and to the
  *   table, and tokens on a page outside 0 .. pages - 1 count as absent.  A page may stand in several tables as long as
  *   no call appends to it.
@@ -488,7 +488,9 @@ int mpq_linear_tokens(const void* x, int x_type, int64_t M, int64_t N, int64_t K
  *     out = sum_j P_j V_j,  P = softmax over the visible j of softmax_scale * (q . K_j),  K, V = code * m / qmax_b;
  *   visible: j < kv_len and on a valid page; with `causal` also j <= p, and with window > 0 (causal only) j > p - window.
  *   A row that sees nothing gives 0.  q, out [rows][q_heads][dim] of `type`, dim contiguous, strides in
- *   elements.  Statistics and sums in fp32; fp32 tensors are multiplied as two 16-bit terms (about 22 bits).
+ *   elements, max_new * q_heads / heads < 2^31.  Statistics and sums in fp32; fp32 tensors are multiplied as two 16-bit
+ *   terms (about 22 bits).  Values are summed relative to the largest page maximum that neighbouring rows (up to 128) see,
+ *   to 2^-33 of it: pages whose values are smaller by many orders lose bits beside it.
  *   Workspace from the query, 16-byte aligned (0 where one workgroup takes a sequence's keys).
  * Errors (all three): MPQ_ERR_NULL, MPQ_ERR_SHAPE, MPQ_ERR_BITS, MPQ_ERR_ALIGN (codes, maxima, elements),
  *   MPQ_ERR_WORKSPACE.  rows = 0 or seqs = 0: nothing is launched. */

@@ -92,7 +92,8 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
   const int h = (int)(pair % a.c.heads), s = (int)(pair / a.c.heads);
   const Sequence sq = sequence(a.b, a.c.page, s);
   const int len = (int)(sq.len < sq.room ? sq.len : sq.room);  // (a length has 31 bits, and so has rows * group)
-  const int before = (int)sq.len - sq.n, group = a.group, nrows = sq.n * group;
+  const int64_t most = a.b.max_new < a.b.rows ? a.b.max_new : a.b.rows;  // (row_tiles, and 31 bits, were made for so many)
+  const int before = (int)sq.len - sq.n, group = a.group, nrows = (int)(sq.n < most ? sq.n : most) * group;
   const int64_t row0_wide = (wg_tiles - 1 - g) * C::ROWS;
   if (row0_wide >= nrows) return;
   const int row0 = (int)row0_wide;

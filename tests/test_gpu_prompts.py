@@ -158,6 +158,31 @@ def test_a_row_with_nan_or_inf_spoils_itself_alone(dtype, new, held):
     assert got[bad].isnan().all() and torch.equal(got[~bad], clean[~bad])
 
 
+def test_more_rows_than_the_call_was_told_of_stay_inside():
+    """Device arrays that name more rows of a sequence than max_new: a part is processed, and nothing is written outside the
+    workspace or to rows that were not."""
+    import ctypes
+    import torch
+    r = rng(77)
+    new, lengths, group = 128, [1628] * 8, 2
+    c, table = filled(r, 8, lengths, 4, 64, 64, 8, "bfloat16")
+    b = c.batch([new] * 8, lengths, table, 65, 1628)
+    q = queries(r, b.rows, 4 * group, 64, "bfloat16")
+    size = mpq.kv_attention_workspace_bytes(c.dev, b, torch.bfloat16, 4 * group)
+    assert size > 0
+    ws = torch.full((size + (1 << 20),), 85, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, 9.0)
+    rc = mpq.lib().mpq_kv_attention(c.dev.ref, b.ref, mpq.BF16, q.data_ptr(), 512, 64, 8, 0.125, 1, 0, out.data_ptr(), 512, 64,
+                                    ws.data_ptr(), size, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    assert rc == 0 and (ws[size:] == 85).all()
+    got = out.view(8, new, 8, 64)
+    assert (got[:, 72:] == 9.0).all()      # (65 rows of two heads end in the ninth tile of 16)
+    whole = c.batch([new] * 8, lengths, table, new, 1628)
+    got[:, 65:] = mpq.kv_attention(c.dev, whole, q).view(8, new, 8, 64)[:, 65:]
+    check_attention(c, full(out), full(q), True, 0, 0.125, "bfloat16")
+
+
 def test_offsets_past_32_bits_of_a_prompt():
     """Pages behind the first 4 GiB of codes."""
     import torch
