@@ -27,8 +27,6 @@ __device__ __forceinline__ v4i stream16(const int8_t* p) {
 }
 constexpr int kPBits = 14;  // probabilities are multiplied by 2^14 before they are rounded to fp16
 
-constexpr int kAttnWaves = 4;
-
 // What a workgroup's rows may see: tokens [lo, hi).
 struct Span {
   int64_t lo, hi;
@@ -44,25 +42,20 @@ struct AttnShape {
 };
 
 // grid: ((sequence * heads + head) * row_tiles + tile) * splits + split.  DH: dim in units of 64, rounded up.
-// ONE: a page holds at least a step's tokens, which then lie on one page.
-template <int T, int DH, bool ONE>
-__global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
+// ONE: a page holds at least a step's tokens, which then lie on one page.  NW: waves.
+template <int T, int DH, bool ONE, int NW>
+__global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
   using S = AttnShape<T, DH>;
   using E = Elem<T>;
   typedef typename E::type El;
-  constexpr int QT = S::QT, PT = S::PT, TT = S::TT, NS = S::NS, DP = S::DP, NW = kAttnWaves, NP = ONE ? 1 : NS;
+  constexpr int QT = S::QT, PT = S::PT, TT = S::TT, NS = S::NS, DP = S::DP, NP = ONE ? 1 : NS;
   __shared__ float sm_m[NW][16], sm_l[NW][16];
   __shared__ __attribute__((aligned(16))) float sm_o[NW / 2][16][DP + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int r = lane & 15, quarter = lane >> 4;
-  int64_t g = block_index();
-  const int split = (int)(g % a.splits);
-  const int64_t slot = g;  // of the partial results
-  g /= a.splits;
-  const int64_t tile = g % a.row_tiles;
-  g /= a.row_tiles;
-  const int h = (int)(g % a.c.heads);
-  const int64_t s = g / a.c.heads;
+  const Digits g = digits(a.splits, a.row_tiles, a.c.heads);
+  const int split = (int)g.d[0], h = (int)g.d[2];
+  const int64_t slot = block_index(), tile = g.d[1], s = g.d[3];  // slot: of the partial results
   if (s >= a.b.seqs) return;
   const Sequence sq = sequence(a.b, a.c.page, (int)s);
   const int64_t len = sq.len < sq.room ? sq.len : sq.room;
@@ -71,10 +64,10 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
   const int D = a.c.dim;
 
   // this lane's row: its position, what it sees
-  const int64_t idx = tile * 16 + r;
+  const unsigned group = (unsigned)a.group, row0 = (unsigned)(tile * 16), idx = row0 + (unsigned)r;  // (32 bits: row_tiles)
   const bool real = idx < nrows;
-  const int64_t i = real ? idx / a.group : 0;
-  const int qh = h * a.group + (int)(real ? idx % a.group : 0);
+  const int64_t i = real ? idx / group : 0;
+  const int qh = h * a.group + (real ? (int)(idx - (unsigned)i * group) : 0);
   auto seen = [&](int64_t row, int64_t& lo, int64_t& hi) {
     const int64_t p = sq.len - sq.n + row;
     hi = a.causal && p + 1 < len ? p + 1 : len;
@@ -84,21 +77,20 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
   seen(i, lo, hi);
   if (!real) hi = 0;
   // of the whole tile: its first and last token row
+  const int64_t first_row = row0 / group, last_row = (row0 + 15 < nrows ? row0 + 15 : (unsigned)(nrows - 1)) / group;
   Span span;
   {
     int64_t unused;
-    const int64_t last = tile * 16 + 15 < nrows ? tile * 16 + 15 : nrows - 1;
-    seen(tile * 16 / a.group, span.lo, unused);
-    seen(last / a.group, unused, span.hi);
+    seen(first_row, span.lo, unused);
+    seen(last_row, unused, span.hi);
   }
   if (span.hi < span.lo) span.hi = span.lo;
   // tokens that every row of the tile sees need no mask
   int64_t all_lo, all_hi;
   {
     int64_t unused;
-    const int64_t last = tile * 16 + 15 < nrows ? tile * 16 + 15 : nrows - 1;
-    seen(last / a.group, all_lo, unused);
-    seen(tile * 16 / a.group, unused, all_hi);
+    seen(last_row, all_lo, unused);
+    seen(first_row, unused, all_hi);
   }
 
   // q: lane (row, quarter) holds channels 64 c + 16 quarter .. + 15 for every c, as the keys come
@@ -134,7 +126,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
 
   // this workgroup's tokens: whole steps, dealt out to the splits in one piece each and to the waves in turn
   const int64_t first = span.lo / TT, steps = (span.hi + TT - 1) / TT - first;
-  const int64_t per = steps > 0 ? (steps + a.splits - 1) / a.splits : 0;
+  const int64_t per = steps > 0 ? (unsigned)(steps + a.splits - 1) / (unsigned)a.splits : 0;
   const int64_t t0 = first + split * per, t1 = first + ((split + 1) * per < steps ? (split + 1) * per : steps);
   const int32_t* table = a.b.table + s * a.b.table_pages;
   const int64_t page_bytes = (int64_t)a.c.page * D;
@@ -363,7 +355,8 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kv_attention_k(AttnArgs a) {
       }
       continue;
     }
-    El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + at / a.group) * a.o_ts + (h * a.group + at % a.group) * a.o_hs + d;
+    const unsigned token = (unsigned)at / group;
+    El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + token) * a.o_ts + (int64_t)(h * a.group + (int)((unsigned)at - token * group)) * a.o_hs + d;
     E::store4(to, l == 0.0f ? f32x4{0, 0, 0, 0} : v / l);  // (a row with a NaN in q has one in l)
   }
 }
@@ -377,14 +370,9 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   typedef typename E::type El;
   __shared__ __attribute__((aligned(16))) float sm_o[kBlock * 4];
   __shared__ float sm_l[kBlock], sm_m[kBlock / kWave];
-  int64_t g = block_index();
-  const int row = (int)(g % a.tile_rows);
-  g /= a.tile_rows;
-  const int64_t slot = g * a.splits;
-  const int64_t tile = g % a.row_tiles;
-  g /= a.row_tiles;
-  const int h = (int)(g % a.c.heads);
-  const int64_t s = g / a.c.heads;
+  const Digits g = digits(a.tile_rows, a.row_tiles, a.c.heads);
+  const int row = (int)g.d[0], h = (int)g.d[2];
+  const int64_t tile = g.d[1], s = g.d[3], slot = ((s * a.c.heads + h) * a.row_tiles + tile) * a.splits;
   if (s >= a.b.seqs) return;
   const Sequence sq = sequence(a.b, a.c.page, (int)s);
   const int64_t at = tile * 16 + row;
@@ -416,7 +404,8 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
     l += sm_l[threadIdx.x + i * quads];
     v += *reinterpret_cast<const f32x4*>(sm_o + 4 * (threadIdx.x + i * quads));
   }
-  El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + at / a.group) * a.o_ts + (h * a.group + at % a.group) * a.o_hs + d;
+  const unsigned group = (unsigned)a.group, token = (unsigned)at / group;
+  El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + token) * a.o_ts + (int64_t)(h * a.group + (int)((unsigned)at - token * group)) * a.o_hs + d;
   E::store4(to, l == 0.0f ? f32x4{0, 0, 0, 0} : v / l);  // (a row with a NaN in q has one in l)
 }
 
@@ -429,6 +418,9 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
 // Splits along the tokens (us, one or two workgroups' worth per CU): 300 rows behind 16000 tokens 8x4 128 137 split in six |
 // 179 in three, 4 x 40 behind 4000 39 | 48; 1500 behind 500 4x4 128 76 in two | 67 in one, 2400 1x1 64 29 in four, 21 in one: where pieces leave
 // half the chip idle, and none of less than 768 tokens.
+// The decode kernel's splits fill the chip once with workgroups of eight waves, from 768 tokens on and of at least 256 (us, so |
+// twice, of at least 512, the whole in one: one of 2500 tokens 8x4 128 11.8 | 13.1 | 19.1, of 130000 52.9 | 54.3 | -, 8 of 3000
+// 17.7 | 20.7 | 23.5, 24 of 2500 8x1 128 30.4 | 32.9 | -; one of 600 in two 12.2, in one 10.6).
 // How a call is cut up.
 struct AttnPlan {
   int64_t row_tiles, tiles;
@@ -460,27 +452,33 @@ static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int type
     p.splits = (int)splits;
     p.wg_rows = splits == 1 && units <= 2 * kNumCU && c.dim <= 128 ? 64 : wide;
     p.wg_tiles = (pair_rows + p.wg_rows - 1) / p.wg_rows;
-  } else {  // two workgroups per CU are on the chip at a time; none with less than 512 tokens
-    const int64_t want = 2 * kNumCU / p.tiles, most_splits = (len + 511) / 512, n = want < most_splits ? want : most_splits;
+  } else {
+    const int64_t want = kNumCU / p.tiles, most_splits = len <= 768 ? 1 : (len + 255) / 256, n = want < most_splits ? want : most_splits;
     p.splits = (int)(n < 1 ? 1 : n);
   }
-  if (blocks_z(p.tiles * (p.splits > 16 ? p.splits : 16), kAttnWaves * 64) > 65535u) return MPQ_ERR_SHAPE;
+  if (blocks_z(p.tiles * (p.splits > 16 ? p.splits : 16), 512) > 65535u) return MPQ_ERR_SHAPE;
   p.ws_bytes = p.splits > 1 ? (size_t)p.tiles * p.splits * 16 * (c.dim + 2) * sizeof(float) : 0;
   return MPQ_OK;
 }
 
 template <int T>
 static int launch_attention(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
-  const dim3 grid = wide_grid(p.tiles * p.splits, kAttnWaves * 64);
-  const int dh = (a.c.dim + 63) / 64;
+  const int dh = a.c.dim <= 64 ? 1 : a.c.dim <= 128 ? 2 : 4;
   const bool one = a.c.page >= (dh <= 2 ? 64 : 32);
-#define MPQ_ATTN(DH_) \
-  (one ? (void)(kv_attention_k<T, DH_, true><<<grid, kAttnWaves * 64, 0, st>>>(a)) : (void)(kv_attention_k<T, DH_, false><<<grid, kAttnWaves * 64, 0, st>>>(a)))
-  if (p.wg_tiles > 0) {
-  } else if (dh == 1) MPQ_ATTN(1);
-  else if (dh == 2) MPQ_ATTN(2);
-  else MPQ_ATTN(4);
-#undef MPQ_ATTN
+  // Eight waves where a CU gets one workgroup, four where it gets several (us, 8 | 4 waves, one query each: one sequence of 384
+  // tokens 16x1 64 7.1 | 8.0, 8x4 128 8.8 | 9.9, 16 of 500 16x1 64 8.0 | 9.1; 32 of 600 8x4 128 18.5 either way)
+  const bool many_waves = dh <= 2 && p.tiles * p.splits <= kNumCU;  // (dim > 128: their shares of the output pass the LDS)
+  if (p.wg_tiles == 0) {
+    using Kern = void (*)(AttnArgs);
+    static const Kern kerns[3][2] = {{kv_attention_k<T, 1, false, 4>, kv_attention_k<T, 1, true, 4>},
+                                     {kv_attention_k<T, 2, false, 4>, kv_attention_k<T, 2, true, 4>},
+                                     {kv_attention_k<T, 4, false, 4>, kv_attention_k<T, 4, true, 4>}};
+    static const Kern wide[2][2] = {{kv_attention_k<T, 1, false, 8>, kv_attention_k<T, 1, true, 8>},
+                                    {kv_attention_k<T, 2, false, 8>, kv_attention_k<T, 2, true, 8>}};
+    const int threads = many_waves ? 512 : 256;
+    const Kern k = many_waves ? wide[dh - 1][one] : kerns[dh >> 1][one];
+    k<<<wide_grid(p.tiles * p.splits, threads), threads, 0, st>>>(a);
+  }
   const int rc = p.wg_tiles > 0 ? launch_prompt(T, a, p.wg_tiles, p.wg_rows, false, st) : launch_status();
   if (rc != MPQ_OK || p.splits == 1) return rc;
   kv_attention_join_k<T><<<wide_grid(p.tiles * p.tile_rows, kBlock), kBlock, 0, st>>>(a);

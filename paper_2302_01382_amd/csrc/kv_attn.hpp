@@ -46,6 +46,32 @@ __device__ __forceinline__ f16x8 codes8(int a, int b) {
   return f16x8{x.x, x.y, y.x, y.y, z.x, z.y, w.x, w.y};
 }
 
+// The digits of g: g % a, g / a % b, g / a / b % c, g / a / b / c.  A division in 64 bits is 150 scalar instructions, which a
+// wave has to itself here, so that they are done in 32 where the grid is that small (one token of one sequence of 384 tokens:
+// with the rows' divisions 8.9 -> 7.9 us).
+struct Digits {
+  int64_t d[4];
+};
+template <typename I>
+__device__ __forceinline__ Digits split_digits(I g, I a, I b, I c) {
+  Digits r;
+  r.d[0] = (int64_t)(g % a);
+  g /= a;
+  r.d[1] = (int64_t)(g % b);
+  g /= b;
+  r.d[2] = (int64_t)(g % c);
+  r.d[3] = (int64_t)(g / c);
+  return r;
+}
+__device__ __forceinline__ Digits digits(int64_t a, int64_t b, int64_t c) {
+  if (gridDim.z == 1) return split_digits<unsigned>(blockIdx.x, (unsigned)a, (unsigned)b, (unsigned)c);
+  return split_digits<uint64_t>((uint64_t)block_index(), (uint64_t)a, (uint64_t)b, (uint64_t)c);
+}
+
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((unsigned)a / (unsigned)b) : a / b;
+}
+
 __device__ __forceinline__ float across(float v, int mask) { return __shfl_xor(v, mask, 64); }
 
 #endif

@@ -82,14 +82,14 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, quarter = lane >> 4;
-  int64_t g = block_index();
-  const int64_t pairs = (int64_t)a.b.seqs * a.c.heads, turn = g % pairs;
-  g /= pairs;
-  const int64_t pair = (turn + g) % pairs;
-  const int split = (int)(g % a.splits);
-  g /= a.splits;
-  if (g >= wg_tiles) return;
-  const int h = (int)(pair % a.c.heads), s = (int)(pair / a.c.heads);
+  const int64_t pairs = (int64_t)a.b.seqs * a.c.heads;
+  const Digits at_grid = digits(pairs, a.splits, wg_tiles);
+  if (at_grid.d[3] > 0) return;
+  const int64_t g = at_grid.d[2];
+  const int split = (int)at_grid.d[1];
+  int64_t pair = at_grid.d[0] + (g - divide(g, pairs) * pairs);
+  if (pair >= pairs) pair -= pairs;
+  const int s = (int)divide(pair, a.c.heads), h = (int)(pair - (int64_t)s * a.c.heads);
   const Sequence sq = sequence(a.b, a.c.page, s);
   const int len = (int)(sq.len < sq.room ? sq.len : sq.room);  // (a length has 31 bits, and so has rows * group)
   const int64_t most = a.b.max_new < a.b.rows ? a.b.max_new : a.b.rows;  // (row_tiles, and 31 bits, were made for so many)
