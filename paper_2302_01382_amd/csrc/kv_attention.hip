@@ -279,7 +279,10 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
       for (int e = 0; e < 4; ++e) {
         const float w = __builtin_amdgcn_exp2f(x[u][e] - m_use);
         l_run += w;
-        const float y = w * f;
+        float y = w * f;
+        // its fp32 rounding stays: the product and its conversion would become one instruction that rounds once, the difference
+        // below would be to another fp16 value, and one probability in a thousand off by 2^-10
+        asm("" : "+v"(y));
         const _Float16 hi16 = (_Float16)y;
         p[0][u][e] = hi16;
         if (PT == 2) p[PT - 1][u][e] = (_Float16)(y - (float)hi16);

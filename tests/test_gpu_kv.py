@@ -357,3 +357,28 @@ def test_decode_steps_from_a_replayed_graph():
     np.testing.assert_array_equal(host(twin.k_codes), host(c.dev.k_codes))
     np.testing.assert_array_equal(host(twin.v_codes), host(c.dev.v_codes))
     np.testing.assert_array_equal(host(twin.k_absmax), host(c.dev.k_absmax))
+
+
+def test_no_probability_of_fp32_is_off_by_a_step_of_fp16():
+    """Probabilities are multiplied as two fp16 terms, which together have about 22 bits.  With a value of its own channel for each
+    of 64 tokens an output is a token's probability.  Products of whole numbers are exact here, so that a logit below 8 is
+    off by its scalings alone (8 * 4 * 2^-24 = 2^-19) and a probability by that, its exponential, its terms and the sum (2^-21,
+    2^-21, 64 * 2^-24): below 2^-17 together; a step of fp16 is 2^-11."""
+    r = rng(21)
+    heads, dim, page = 16, 64, 16
+    for seed in range(12):
+        pages, table = tables(r, 1, 4)
+        c = Pair(pages, heads, page, dim, 8)
+        b = c.batch([64], [64], table)
+        k = r.integers(-127, 128, (64, heads, dim)).astype(np.float64)
+        k[::page] = 127.0                      # a page's maximum, so that codes are the numbers
+        v = np.broadcast_to(np.eye(64)[:, None, :] * (1 + seed / 16), (64, heads, dim))
+        c.append(b, dev(k), dev(v))
+        b = c.batch([1], [64], table)
+        q = r.integers(-3, 4, (1, heads, dim)).astype(np.float64)
+        scale = 1 / 1024
+        got = full(mpq.kv_attention(c.dev, b, dev(q), causal=False, softmax_scale=scale)).astype(np.float64)
+        x = np.einsum("jhd,hd->hj", k, q[0]) * scale
+        p = np.exp(x - x.max(1, keepdims=True))
+        p = p / p.sum(1, keepdims=True) * (1 + seed / 16)
+        assert np.abs(x).max() < 8 and (np.abs(got[0] / p - 1) < 2.0 ** -16).all(), np.abs(got[0] / p - 1).max()
