@@ -113,6 +113,14 @@ __global__ __launch_bounds__(kMaxKvThreads) void kv_append_k(mpq_kv_cache c, mpq
   float* absmax = (values ? c.v_absmax : c.k_absmax) + id * c.heads + w.h;
   int8_t* codes = (values ? c.v_codes : c.k_codes) + (id * c.heads + w.h) * ((int64_t)c.page * D);
   const float was = p.lo > 0 ? *absmax : 0.0f;
+  // values: what is there already, also bytes behind the last token, which stay as they are (requested with the maximum: for a
+  // single token each memory access that waits for another counts)
+  v4i* to = reinterpret_cast<v4i*>(codes + (grp * D + at) * 4);
+  v4i v[2] = {v4i{0, 0, 0, 0}, v4i{0, 0, 0, 0}};
+  if (values && mine && (4 * grp < p.lo || 4 * grp + 4 > p.hi)) {
+    v[0] = to[0];
+    v[1] = to[1];
+  }
   if (mine) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -150,13 +158,6 @@ __global__ __launch_bounds__(kMaxKvThreads) void kv_append_k(mpq_kv_cache c, mpq
                                                               (int)pack_codes(f[t][4], f[t][5], f[t][6], f[t][7], inv, qmax)};
     }
   } else if (mine) {
-    v4i* to = reinterpret_cast<v4i*>(codes + (grp * D + at) * 4);
-    // what is there already: also bytes behind the last token, which stay as they are
-    v4i v[2] = {v4i{0, 0, 0, 0}, v4i{0, 0, 0, 0}};
-    if (4 * grp < p.lo || 4 * grp + 4 > p.hi) {
-      v[0] = to[0];
-      v[1] = to[1];
-    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int before = v[e >> 2][e & 3];
