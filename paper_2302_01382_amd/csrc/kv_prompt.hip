@@ -14,10 +14,11 @@
 // that may lag behind the true one by up to 6: P' then reaches 2^14, and the accumulators are rescaled only when it lags
 // by more.
 //
-// Two prompts of up to 4500 rows behind up to 1000 tokens, 16 query and 4 key heads of 128 channels in bf16: 283 us, 805
+// Two prompts of up to 4500 rows behind up to 1000 tokens, 16 query and 4 key heads of 128 channels in bf16: 262 us, 868
 // TFLOP/s of the pairs that the mask leaves.  Matrix steps take 32 % of the SIMDs' cycles, vector instructions (a third of them the
 // exponentials, a quarter the codes' way into fp16) 50 %, with two waves per SIMD that 220 registers leave room for; a sixth of the
-// time is the last workgroups' alone.  What did not help: the next keys' matrix steps between the exponentials (302 against
+// time is the last workgroups' alone.  Operands are read out of the LDS four reads ahead, the first values' under the softmax (282
+// with the compiler's one or two).  What did not help: the next keys' matrix steps between the exponentials (302 against
 // 302), two groups of waves that take turns with matrix steps and softmax behind barriers (327 against 304), s_setprio around
 // the matrix steps (302 to 307), 64 rows a wave (spilled).
 #include "kv_attn.hpp"
@@ -310,20 +311,31 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
     for (int half = 0; half < 2; ++half) {  // 32 tokens at a time
       const int base = t * TT + half * 32;
       f32x4 sc[2][NQ];
+      // reads are issued so many ahead of the matrix steps that take them
+      constexpr int NR = 4 * DH, kAhead = 4;
+      auto read_k = [&](int i) {
+        const int c = i >> 1, u = i & 1;
+        return *reinterpret_cast<const f16x8*>(lds + stage + k_at + (((unsigned)(4 * c + quarter) ^ swz) << 4) + (2 * half + u) * 16 * (DH * 128));
+      };
+      auto read_v = [&](int k) { return *reinterpret_cast<const f16x8*>(lds + stage + v_at + ((half * 4 * 64 * DH + k * 16) << 4)); };
+      f16x8 kf[kAhead], vf[kAhead];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int i = 0; i < kAhead; ++i) kf[i] = read_k(i);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int n = 0; n < NQ; ++n) sc[u][n] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
         __builtin_amdgcn_sched_barrier(0);
+        const f16x8 now = kf[i % kAhead];
 #pragma unroll
-        for (int c = 0; c < 2 * DH; ++c) {
-          const f16x8 kf =
-              *reinterpret_cast<const f16x8*>(lds + stage + k_at + (((unsigned)(4 * c + quarter) ^ swz) << 4) + (2 * half + u) * 16 * (DH * 128));
+        for (int x = 0; x < QT; ++x)
 #pragma unroll
-          for (int x = 0; x < QT; ++x)
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) sc[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[x][n][c], sc[u][n], 0, 0, 0);
-        }
+          for (int n = 0; n < NQ; ++n)
+            sc[i & 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now, q[x][n][i >> 1], sc[i & 1][n], 0, 0, 0);
+        if (i + kAhead < NR) kf[i % kAhead] = read_k(i + kAhead);
+        else vf[i + kAhead - NR] = read_v(i + kAhead - NR);
       }
       __builtin_amdgcn_sched_barrier(0);
       // logits over f; scalars: see kv_attention.hip
@@ -408,13 +420,14 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
       }
 #pragma unroll
       for (int k = 0; k < 4 * DH; ++k) {
-        if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-        const f16x8 vf = *reinterpret_cast<const f16x8*>(lds + stage + v_at + ((half * 4 * 64 * DH + k * 16) << 4));
+        __builtin_amdgcn_sched_barrier(0);
+        const f16x8 now = vf[k % kAhead];
 #pragma unroll
         for (int x = 0; x < PT; ++x)
 #pragma unroll
           for (int n = 0; n < NQ; ++n)
-            o[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, __builtin_bit_cast(f16x8, pw[x][n]), o[n][k], 0, 0, 0);
+            o[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now, __builtin_bit_cast(f16x8, pw[x][n]), o[n][k], 0, 0, 0);
+        if (k + kAhead < NR) vf[k % kAhead] = read_v(k + kAhead);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
