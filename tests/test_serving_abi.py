@@ -244,3 +244,17 @@ def test_reference_cache_by_hand():
     assert big[0, 0] == 6
     packed = serving.packed_values(c.codes["v"])
     assert packed.shape == (2, 1, 4, 16, 4) and packed[1, 0, 0, 0].tolist() == [2, 3, 0, 0]
+
+
+@needs_no_gpu
+def test_kv_sizes_that_indexes_cannot_count():
+    """More heads than a grid of keys and values counts; more rows of a key head than 31 bits."""
+    L = mpq.lib()
+    c, b = kv({"heads": 1 << 30, "pages": 1, "dim": 16})
+    for f in calls():
+        assert f(c, b) == mpq.ERR_SHAPE
+    many = {"rows": 1 << 29, "max_new": 1 << 29}
+    assert L.mpq_kv_attention_workspace_bytes(*kv(batch=many), 1, 8) == 0
+    assert L.mpq_kv_attention(*kv(batch=many), 1, FAKE16, 512, 64, 8, 0.125, 1, 0, FAKE16, 512, 64, FAKE16, BIG, None) == mpq.ERR_SHAPE
+    few = {"rows": 1 << 29, "max_new": 1}          # (a bound on the rows of a sequence, not of the call)
+    assert L.mpq_kv_attention_workspace_bytes(*kv(batch=few), 1, 8) == 0
