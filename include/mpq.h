@@ -449,7 +449,8 @@ int mpq_qgemm_tokens(const int8_t* a_q, const void* w_q, int w_storage_bits, int
 /* ---- both in one call: a linear layer from its input to its output --------------------------------
  * mpq_token_quant(x, bits) followed by mpq_qgemm_tokens: the same results bit for bit.
  * Workspace: the codes and steps of the tokens, size from the query, 16-byte aligned; 0 (ws may be NULL) where M = 0
- * and where the product's kernel quantizes the rows itself (at most 16 of them, K a multiple of 16). */
+ * and where the product's kernel quantizes the rows itself (at most 16 rows of at most 65536 values in all, K a multiple
+ * of 16). */
 size_t mpq_linear_tokens_workspace_bytes(int64_t M, int64_t N, int64_t K, int w_storage_bits);
 int mpq_linear_tokens(const void* x, int x_type, int64_t M, int64_t N, int64_t K, int64_t x_stride, int bits,
                       const void* w_q, int w_storage_bits, const float* w_scale, int w_gran, int act, int y_type,

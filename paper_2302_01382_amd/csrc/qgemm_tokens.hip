@@ -8,7 +8,7 @@
 // 8 x 4096 x 8192 read 33.6 MB of weights in 10.3 us (3.3 TB/s), 64 x 4096 x 4096 in 13.7 us: from 33 rows on the rows, which
 // every workgroup reads out of the L2, bound it (with rows of zero bytes 7.6 us).
 //
-// With at most 16 rows the rows' quantizer (token_quant.hip's arithmetic, bit for bit) runs in the same kernel: each
+// With few values in at most 16 rows the rows' quantizer (token_quant.hip's arithmetic, bit for bit) runs in the same kernel: each
 // workgroup takes the rows' maxima itself, a wave a row, while its weights are on their way, and quantizes the values
 // of its k steps as it loads them.  That spares a launch (3.9 us of host time) and a kernel's latency.
 #include "qgemm_dma.hpp"
@@ -204,7 +204,12 @@ __global__ __launch_bounds__(kTokThreads, 2) void token_rows_k(TokArgs p) {
 
 // (a grid counts 2^32 threads)
 bool token_rows(bool w4, int64_t M, int64_t N, int64_t K) { return M <= 64 && N <= (1 << 26) && K >= (w4 ? 32 : 16); }
-bool token_rows_fused(bool w4, int64_t M, int64_t N, int64_t K) { return token_rows(w4, M, N, K) && M <= 16 && K % 16 == 0; }
+// Every workgroup reads and quantizes all rows, so that there must not be much of them (us on the device, one kernel | two;
+// a launch more costs the host 4: 1 x 4096 x 4096 6.8 | -, 8 x 4096 x 4096 packed 7.9 | 8.8, 16 x 4096 x 4096 11.9 | 10.7, x 12288 fp32
+// 23.1 | 17.9, 16 x 11008 x 4096 27.1 | 21.1; with more than 16 rows 32 x 1024 x 1024 8.3 | 6.5, 19 x 4096 x 12288 packed 24.6 | 13.8).
+bool token_rows_fused(bool w4, int64_t M, int64_t N, int64_t K) {
+  return token_rows(w4, M, N, K) && M <= 16 && K % 16 == 0 && M * K <= 65536;
+}
 
 // Channel tiles per workgroup: what makes the bytes that a CU loads smallest, its workgroups' weights and rows.
 static int channel_tiles(int mt, bool w4, const TokArgs& p, int el) {

@@ -217,3 +217,22 @@ def test_replayed_graphs_and_other_streams_give_the_eager_results():
         torch.cuda.synchronize()
         for a, b, c, d in zip(want, other, outs, eager):
             assert torch.equal(a, b) and torch.equal(a, c) and torch.equal(a, d)
+
+
+@pytest.mark.parametrize("M,N,K,w_bits", [(16, 100, 4096, 8), (16, 100, 4112, 8), (9, 257, 2064, 4), (1, 33, 16, 8), (2, 5, 32, 4), (15, 300, 48, 8),
+                                          (16, 12, 4096, 4), (5, 40, 13104, 8), (1, 20, 65536, 8), (1, 20, 65552, 4)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_one_kernel_or_two_are_the_same(M, N, K, w_bits, dtype):
+    """Rows that the product's kernel quantizes itself, and the first sizes that it does not."""
+    import torch
+    r = rng(M + K)
+    x = dev(r.standard_normal((M, K + 5)) * np.exp(3 * r.standard_normal((M, 1))), dtype)[:, 2:2 + K]
+    x[M // 2] = 0
+    _, w, w_scale = weights(r, N, K, w_bits)
+    ws = dev(w_scale)
+    fused = M * K <= 65536
+    assert (mpq.linear_tokens_workspace_bytes(M, N, K, w_bits) == 0) == fused
+    for bits, out in ((8, None), (3, torch.float32)):
+        a, s = mpq.token_quant(x, bits)
+        two = mpq.qgemm_tokens(a, w, s, ws, w_bits, dtype=out or x.dtype)
+        assert torch.equal(mpq.linear_tokens(x, w, ws, w_bits, mpq.PER_ROW, bits, dtype=out), two)
