@@ -850,7 +850,7 @@ def _scratch(ws, nbytes, x):
         return None, 0, None
     if ws is not None:
         return (*ws.get(nbytes), ws)
-    buf = x.new_empty(nbytes, dtype=_torch().uint8)
+    buf = x.new(-(-nbytes // x.element_size()))
     return buf.data_ptr(), nbytes, buf
 
 
