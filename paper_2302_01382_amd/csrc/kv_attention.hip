@@ -27,11 +27,6 @@ __device__ __forceinline__ v4i stream16(const int8_t* p) {
 }
 constexpr int kPBits = 14;  // probabilities are multiplied by 2^14 before they are rounded to fp16
 
-// What a workgroup's rows may see: tokens [lo, hi).
-struct Span {
-  int64_t lo, hi;
-};
-
 template <int T, int DH>
 struct AttnShape {
   static constexpr int QT = T == MPQ_F32 ? 2 : 1;   // fp16 terms of q
@@ -68,30 +63,13 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
   const bool real = idx < nrows;
   const int64_t i = real ? idx / group : 0;
   const int qh = h * a.group + (real ? (int)(idx - (unsigned)i * group) : 0);
-  auto seen = [&](int64_t row, int64_t& lo, int64_t& hi) {
-    const int64_t p = sq.len - sq.n + row;
-    hi = a.causal && p + 1 < len ? p + 1 : len;
-    lo = a.window > 0 && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
-  };
-  int64_t lo, hi;
-  seen(i, lo, hi);
-  if (!real) hi = 0;
-  // of the whole tile: its first and last token row
+  auto row_sees = [&](int64_t row) { return seen(sq.len - sq.n + row, len, a.causal, a.window); };
+  const Span own = row_sees(i);
+  const int64_t lo = own.lo, hi = real ? own.hi : 0;
+  // of the whole tile: its first and last token row, what some row of it sees, and what every row does, which needs no mask
   const int64_t first_row = row0 / group, last_row = (row0 + 15 < nrows ? row0 + 15 : (unsigned)(nrows - 1)) / group;
-  Span span;
-  {
-    int64_t unused;
-    seen(first_row, span.lo, unused);
-    seen(last_row, unused, span.hi);
-  }
-  if (span.hi < span.lo) span.hi = span.lo;
-  // tokens that every row of the tile sees need no mask
-  int64_t all_lo, all_hi;
-  {
-    int64_t unused;
-    seen(last_row, all_lo, unused);
-    seen(first_row, unused, all_hi);
-  }
+  const Span of_first = row_sees(first_row), of_last = row_sees(last_row), span = {of_first.lo, of_last.hi};
+  const int64_t all_lo = of_last.lo, all_hi = of_first.hi;
 
   // q: lane (row, quarter) holds channels 64 c + 16 quarter .. + 15 for every c, as the keys come
   f16x8 q[QT][2 * DH];
@@ -125,9 +103,8 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
   }
 
   // this workgroup's tokens: whole steps, dealt out to the splits in one piece each and to the waves in turn
-  const int64_t first = span.lo / TT, steps = (span.hi + TT - 1) / TT - first;
-  const int64_t per = steps > 0 ? (unsigned)(steps + a.splits - 1) / (unsigned)a.splits : 0;
-  const int64_t t0 = first + split * per, t1 = first + ((split + 1) * per < steps ? (split + 1) * per : steps);
+  const Steps share = steps_of(span, TT, a.splits, split);
+  const int64_t t0 = share.t0, t1 = share.t1;
   const int32_t* table = a.b.table + s * a.b.table_pages;
   const int64_t page_bytes = (int64_t)a.c.page * D;
   const int shift = 31 - __builtin_clz((unsigned)a.c.page);

@@ -1,6 +1,7 @@
 // kv_attn.hpp -- what the kernels of the attention over quantized pages share.
 #pragma once
 
+#include "attn_span.hpp"
 #include "kv.hpp"
 
 namespace mpq {

@@ -1,0 +1,33 @@
+"""The cache and its attention where device arrays and tensors hold what a program rarely gives them: lengths beyond the table,
+windows and values at the end of their ranges.  Bounds: check_attention's."""
+import numpy as np
+import pytest
+
+from test_gpu_kv import DTYPES, Pair, check_attention, filled, tables, tokens
+from test_gpu_parity import mpq
+from test_gpu_tokens import dev, full, rng
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new,group", [(1, 1), (1, 16), (12, 3), (70, 2)])
+@pytest.mark.parametrize("dim,page", [(64, 64), (128, 16), (256, 32)])
+def test_a_window_behind_the_tables_end_sees_nothing(dtype, new, group, dim, page):
+    """A length beyond what the table holds, and a window that ends short of it: rows see nothing and give 0, those of a sequence
+    whose window reaches back into the table see its end.  The table lies inside a larger tensor of valid page numbers."""
+    r = rng(dim + page + new)
+    room, window = 192, 75
+    lengths = [room, room, room, 150]
+    c, table = filled(r, 4, lengths, 1, dim, page, 8, dtype)
+    table = table[:, :room // page]
+    wide = np.zeros((40, room // page), np.int32)
+    wide[:4] = table
+    whole = dev(wide, "int32")
+    said = [1000, room + 40, room + window + new, 150]
+    b = c.batch([new] * 4, said, table)
+    b = mpq.KvBatch(b.starts, b.kv_len, whole[:4], b.rows, new, 1024)
+    q = dev(r.standard_normal((b.rows, group, dim)) * 2, dtype)
+    out = full(mpq.kv_attention(c.dev, b, q, window=window))
+    assert not out[:new].any() and out[new:2 * new].any(axis=(1, 2)).all() and not out[3 * new - 1].any()
+    check_attention(c, out, full(q), True, window, dim ** -0.5, dtype)
