@@ -16,6 +16,10 @@ namespace mpq {
 struct Span {
   int64_t lo, hi;
 };
+// A window as seen() takes it: positions lie within 2^31 of 0, so that one of 2^32 reaches as far as any wider one, and p - window
+// stays far from the ends of 64 bits.
+MPQ_ANYWHERE int64_t cut_window(int64_t window) { return window < ((int64_t)1 << 32) ? window : (int64_t)1 << 32; }
+
 // What a row at position p sees of len tokens.  len is cut to the table's places, p is not: with a window lo may lie far behind
 // len.
 MPQ_ANYWHERE Span seen(int64_t p, int64_t len, bool causal, int64_t window) {

@@ -496,7 +496,7 @@ extern "C" int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* b
   if (p.ws_bytes > 0 && (!ws || ws_bytes < p.ws_bytes)) return MPQ_ERR_WORKSPACE;
   if (p.ws_bytes > 0 && !aligned16(ws)) return MPQ_ERR_ALIGN;
   AttnArgs a{*cache, *batch, q, q_token_stride, q_head_stride, out, out_token_stride, out_head_stride, q_heads, q_heads / cache->heads,
-             causal != 0, window, softmax_scale, p.row_tiles, p.splits, p.tile_rows, nullptr, nullptr};
+             causal != 0, cut_window(window), softmax_scale, p.row_tiles, p.splits, p.tile_rows, nullptr, nullptr};
   if (p.splits > 1) {
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = a.part_o + (size_t)p.tiles * p.splits * 16 * cache->dim;

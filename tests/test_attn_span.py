@@ -1,6 +1,6 @@
 """The arithmetic of the attention's spans and steps (csrc/attn_span.hpp), compiled into a plain C++ program that walks over
 every step that a workgroup of the kernel for single tokens would take: no look-up outside a sequence's row of the table,
-whatever the lengths, and no token left out that some row sees."""
+whatever the lengths, and no token left out that some row sees; windows of any size."""
 import os
 import shutil
 import subprocess
@@ -10,6 +10,7 @@ import pytest
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 PROGRAM = r"""
+#include <cstdint>
 #include <cstdio>
 #include <initializer_list>
 #include <set>
@@ -56,6 +57,16 @@ int main() {
               }
             }
         }
+  // windows up to the type's end mean what the widest that reaches any token means, also for rows in front of the first token
+  for (int64_t window : {(int64_t)1 << 31, ((int64_t)1 << 32) - 1, (int64_t)1 << 32, INT64_MAX - 100, INT64_MAX})
+    for (int64_t p : {-((int64_t)1 << 31), (int64_t)-1000, (int64_t)-70, (int64_t)-3, (int64_t)-1, (int64_t)0, (int64_t)5, ((int64_t)1 << 31) - 2}) {
+      const Span s = seen(p, 1000, true, cut_window(window));
+      const int64_t hi = p + 1 < 1000 ? p + 1 : 1000;
+      if (s.lo != 0 || s.hi != hi) { std::printf("window %lld at %lld: %lld .. %lld\n", (long long)window, (long long)p, (long long)s.lo, (long long)s.hi); bad = 1; }
+    }
+  for (int64_t window : {0, 1, 75, 0x7FFFFFFF})
+    if (cut_window(window) != window) bad = 1;
+  if (bad) return 1;
   std::puts("spans ok");
   return 0;
 }

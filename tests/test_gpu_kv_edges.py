@@ -31,3 +31,18 @@ def test_a_window_behind_the_tables_end_sees_nothing(dtype, new, group, dim, pag
     out = full(mpq.kv_attention(c.dev, b, q, window=window))
     assert not out[:new].any() and out[new:2 * new].any(axis=(1, 2)).all() and not out[3 * new - 1].any()
     check_attention(c, out, full(q), True, window, dim ** -0.5, dtype)
+
+
+@pytest.mark.parametrize("window", (2 ** 31, 2 ** 62, 2 ** 63 - 1))
+@pytest.mark.parametrize("new,heads", [(200, 1), (128, 16)])
+def test_a_window_of_any_size_is_none_when_it_reaches_everything(window, new, heads):
+    """Rows in front of the first token among them, in calls that either kernel takes."""
+    import torch
+    r = rng(new)
+    lengths = [40, new, 130, 5, 70, 300, 1, 2]
+    c, table = filled(r, 8, lengths, heads, 64, 16, 8, "bfloat16")
+    b = c.batch([new] * 8, lengths, table, new, 300)
+    q = dev(r.standard_normal((b.rows, heads, 64)), "bfloat16")
+    want = mpq.kv_attention(c.dev, b, q)
+    assert torch.equal(mpq.kv_attention(c.dev, b, q, window=window), want)
+    check_attention(c, full(want), full(q), True, 0, 0.125, "bfloat16")
