@@ -287,7 +287,9 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
     }
     e = __builtin_amdgcn_readfirstlane(e);
     v_next = e > v_next ? e : v_next;
-    const float l2 = any ? fmaxf(__builtin_amdgcn_logf(__builtin_ldexpf(mv_in, -v_next)), kLeast) : 0.0f;
+    // (a page of maximum 0 as one of the least factor: its probabilities vanish in fp16, 2^(kLag + kUp + kLeast) at most, and
+    // count in the sum)
+    const float l2 = any ? fmaxf(__builtin_amdgcn_logf(__builtin_ldexpf(mv_in, -v_next)), kLeast) : kLeast;
     const float inverse = __builtin_amdgcn_exp2f(-l2);
 #pragma unroll
     for (int u = 0; u < NP; ++u) {

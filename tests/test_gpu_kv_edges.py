@@ -46,3 +46,26 @@ def test_a_window_of_any_size_is_none_when_it_reaches_everything(window, new, he
     want = mpq.kv_attention(c.dev, b, q)
     assert torch.equal(mpq.kv_attention(c.dev, b, q, window=window), want)
     check_attention(c, full(want), full(q), True, 0, 0.125, "bfloat16")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("page", (16, 64))
+@pytest.mark.parametrize("new", (1, 128))
+def test_pages_whose_maximum_is_zero_whatever_their_codes(dtype, page, new):
+    """A caller's own cache, or one whose maxima were cleared: codes under a maximum of 0 are zeros (code * 0 / qmax), for
+    values as for keys, and their tokens keep their weight.  A sequence whose value maxima are all 0 gives 0."""
+    r = rng(page + new)
+    lengths = [256, 200, 300, 130, 128, 140, 257, 190]
+    c, table = filled(r, 8, lengths, 4, 64, page, 8, dtype)
+    for s, at, name in ((0, 0, "v"), (0, 128 // page, "v"), (1, 64 // page, "k"), (2, 192 // page, "v"), (2, 192 // page, "k"), (3, 0, "v")):
+        (c.dev.v_absmax if name == "v" else c.dev.k_absmax)[int(table[s, at])] = 0
+        c.host.absmax[name][table[s, at]] = 0
+    for on in table[4]:
+        c.dev.v_absmax[int(on)] = 0
+        c.host.absmax["v"][on] = 0
+    assert c.host.codes["v"][table[4, 0]].any()
+    b = c.batch([new] * 8, lengths, table, new, 300)
+    q = dev(r.standard_normal((b.rows, 8, 64)) * 2, dtype)
+    out = full(mpq.kv_attention(c.dev, b, q))
+    assert not out[4 * new:5 * new].any()
+    check_attention(c, out, full(q), True, 0, 0.125, dtype)
