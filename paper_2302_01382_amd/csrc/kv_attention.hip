@@ -231,7 +231,7 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
     int ve = v_exp;
 #pragma unroll
     for (int u = 0; u < NP; ++u)
-      if (mv_now[u] > 0.0f) {
+      if (mv_now[u] > 0.0f && mv_now[u] < __builtin_inff()) {
         const int e = __builtin_amdgcn_frexp_expf(mv_now[u]);
         ve = e > ve ? e : ve;
       }
@@ -251,7 +251,8 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
     f16x4 p[PT][NS];
 #pragma unroll
     for (int u = 0; u < NS; ++u) {
-      const float v = mv_now[u / (NS / NP)], f = v > 0.0f ? __builtin_ldexpf(v, kPBits - v_exp) : 0.0f;
+      // (a maximum of infinity as a factor that leaves a probability of 0 one: rows that see the page become NaN, others do not)
+      const float v = mv_now[u / (NS / NP)], f = v > 0.0f ? fminf(__builtin_ldexpf(v, kPBits - v_exp), __FLT_MAX__) : 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float w = __builtin_amdgcn_exp2f(x[u][e] - m_use);

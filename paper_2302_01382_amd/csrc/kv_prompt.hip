@@ -27,7 +27,7 @@
 
 namespace mpq {
 
-constexpr float kLag = 6.0f, kUp = 8.0f, kLeast = -60.0f;
+constexpr float kLag = 6.0f, kUp = 8.0f, kLeast = -60.0f, kMost = 1e30f;
 
 // Maxima in assembly: the compiler's would first quiet every operand that it has not seen quieted.
 __device__ __forceinline__ float max2(float a, float b) {
@@ -280,7 +280,9 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
   auto arrived = [&]() {
     mk_in = page_ok ? mk_in : -1.0f;
     const bool any = page_ok && mv_in > 0.0f;
-    int e = any ? __builtin_amdgcn_frexp_expf(mv_in) : v_next;
+    // (a maximum of infinity moves no exponent and gives a factor whose sum with minus infinity is minus infinity: rows that see
+    // the page become NaN, rows that do not see it keep their value)
+    int e = any && mv_in < __builtin_inff() ? __builtin_amdgcn_frexp_expf(mv_in) : v_next;
     if (!ONE) {
       e = max(e, __builtin_amdgcn_update_dpp(0, e, kQuadSwap1, 0xF, 0xF, true));
       e = max(e, __builtin_amdgcn_update_dpp(0, e, kQuadSwap2, 0xF, 0xF, true));
@@ -289,7 +291,7 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
     v_next = e > v_next ? e : v_next;
     // (a page of maximum 0 as one of the least factor: its probabilities vanish in fp16, 2^(kLag + kUp + kLeast) at most, and
     // count in the sum)
-    const float l2 = any ? fmaxf(__builtin_amdgcn_logf(__builtin_ldexpf(mv_in, -v_next)), kLeast) : kLeast;
+    const float l2 = any ? fminf(fmaxf(__builtin_amdgcn_logf(__builtin_ldexpf(mv_in, -v_next)), kLeast), kMost) : kLeast;
     const float inverse = __builtin_amdgcn_exp2f(-l2);
 #pragma unroll
     for (int u = 0; u < NP; ++u) {

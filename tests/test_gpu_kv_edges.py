@@ -69,3 +69,33 @@ def test_pages_whose_maximum_is_zero_whatever_their_codes(dtype, page, new):
     out = full(mpq.kv_attention(c.dev, b, q))
     assert not out[4 * new:5 * new].any()
     check_attention(c, out, full(q), True, 0, 0.125, dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", "kv")
+@pytest.mark.parametrize("page", (16, 64))
+@pytest.mark.parametrize("new,window", [(1, 0), (1, 40), (7, 0), (7, 40), (128, 0), (128, 40)])
+def test_an_infinite_page_spoils_the_rows_that_see_it(dtype, name, page, new, window):
+    """A token with an infinity leaves an infinite maximum on its page.  Rows that see the page become NaN; rows in front of it,
+    behind the window or of other heads keep their values, whatever tile or step they share with it."""
+    import torch
+    r = rng(page + new + window)
+    lengths = [256, 200, 300, 130, 128, 140, 257, 190]
+    c, table = filled(r, 8, lengths, 4, 64, page, 8, dtype)
+    b = c.batch([new] * 8, lengths, table, new, 300)
+    q = dev(r.standard_normal((b.rows, 8, 64)), dtype)
+    clean = mpq.kv_attention(c.dev, b, q, window=window)
+    bad = np.zeros((b.rows, 8), bool)
+    for s, at, h in ((0, 192 // page, 1), (1, 0, 0), (2, 2, 3), (4, 64 // page, 2), (6, 256 // page, 0), (7, 176 // page, 3)):
+        (c.dev.k_absmax if name == "k" else c.dev.v_absmax)[int(table[s, at]), h] = float("inf")
+        codes = c.dev.k_codes if name == "k" else c.dev.v_codes      # what append leaves under such a maximum
+        codes[int(table[s, at]), h] = 0
+        for i in range(new):
+            p = lengths[s] - new + i
+            if p >= at * page and (window == 0 or (at + 1) * page > p - window + 1):
+                bad[s * new + i, 2 * h:2 * h + 2] = True
+    got = mpq.kv_attention(c.dev, b, q, window=window)
+    t = torch.from_numpy(bad).cuda()
+    assert bad.any() and not bad.all() and got[t].isnan().all()
+    got[t] = clean[t]
+    check_attention(c, full(got), full(q), True, window, 0.125, dtype)
