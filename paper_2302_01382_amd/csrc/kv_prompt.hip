@@ -29,7 +29,9 @@ namespace mpq {
 
 constexpr float kLag = 6.0f, kUp = 8.0f, kLeast = -60.0f, kMost = 1e30f;
 
-// Maxima in assembly: the compiler's would first quiet every operand that it has not seen quieted.
+// Maxima in assembly: the compiler's would first quiet every operand that it has not seen quieted.  Its hazard pass does not look into
+// assembly, so that the waits around it are stated: results_ready between matrix steps and the maxima of their
+// results, two states between a maximum and a swap of lanes.
 __device__ __forceinline__ float max2(float a, float b) {
   float r;
   asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
@@ -42,10 +44,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 // max over the four lanes that share a row: lane & 15
 __device__ __forceinline__ float row_max(float v) {
+  asm("s_nop 1" : "+v"(v));
   auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
   v = max2(__builtin_bit_cast(float, (unsigned)a[0]), __builtin_bit_cast(float, (unsigned)a[1]));
+  asm("s_nop 1" : "+v"(v));
   auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
   return max2(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
+}
+
+// The results of matrix steps of four passes (16x16x32), for assembly to read: eight states behind the last of them.
+template <int NQ>
+__device__ __forceinline__ void results_ready(f32x4 (&sc)[2][NQ]) {
+  static_assert(NQ <= 2, "all of them in one block: what comes behind it has waited");
+  if constexpr (NQ == 1) asm volatile("s_nop 7" : "+v"(sc[0][0]), "+v"(sc[1][0]));
+  else asm volatile("s_nop 7" : "+v"(sc[0][0]), "+v"(sc[1][0]), "+v"(sc[0][1]), "+v"(sc[1][1]));
 }
 
 // this wave's LDS accesses are done, and so are everyone's (loads from memory stay in flight)
@@ -342,6 +354,7 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
         else vf[i + kAhead - NR] = read_v(i + kAhead - NR);
       }
       __builtin_amdgcn_sched_barrier(0);
+      results_ready<NQ>(sc);
       // logits over f; scalars: see kv_attention.hip
       float x[2][NQ][4];
 #pragma unroll
