@@ -14,10 +14,11 @@
 //
 // Precision: logits, maxima, sums and outputs are fp32.  q goes in as fp16 after a scaling by a power of two (its row's
 // largest entry to 2^14: bf16 and fp16 keep every bit down to 2^-28 of that entry), fp32 as two such terms (22 bits).
-// Probabilities, at most 1, go in as fp16 times 2^14: as one term for bf16 (2^-11, an eighth of the output's rounding), as two
-// for the others (with one, an fp16 output's distance to 64 bits went from 2.1e-4 to 3.1e-4; the step has room for the
-// products).  Values' maxima differ from page to page: probabilities carry them relative to a power of two that is
-// at least the largest maximum so far, an exact rescaling whenever it grows.
+// Probabilities, at most 1, go in as fp16 times 2^14, as two such terms: with one, an fp16 output's distance to 64 bits went from
+// 2.1e-4 to 3.1e-4, and a bf16 one, whose distance stays at 1.7e-3, differed from the output of fp32 products by 8.9e-4 of its power
+// instead of 6.3e-5 (64 sequences of up to 8192 tokens 151.3 -> 152.4 us with the second term).
+// Values' maxima differ from page to page: probabilities carry them relative to a power of two that is at least the largest
+// maximum so far, an exact rescaling whenever it grows.
 #include "kv_attn.hpp"
 
 namespace mpq {
@@ -30,7 +31,6 @@ constexpr int kPBits = 14;  // probabilities are multiplied by 2^14 before they 
 template <int T, int DH>
 struct AttnShape {
   static constexpr int QT = T == MPQ_F32 ? 2 : 1;   // fp16 terms of q
-  static constexpr int PT = T == MPQ_BF16 ? 1 : 2;  // ... of a probability
   static constexpr int TT = DH <= 2 ? 64 : 32;  // tokens per step
   static constexpr int NS = TT / 16;
   static constexpr int DP = DH * 64;
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
   using S = AttnShape<T, DH>;
   using E = Elem<T>;
   typedef typename E::type El;
-  constexpr int QT = S::QT, PT = S::PT, TT = S::TT, NS = S::NS, DP = S::DP, NP = ONE ? 1 : NS;
+  constexpr int QT = S::QT, TT = S::TT, NS = S::NS, DP = S::DP, NP = ONE ? 1 : NS;
   __shared__ float sm_m[NW][16], sm_l[NW][16];
   __shared__ __attribute__((aligned(16))) float sm_o[NW / 2][16][DP + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
       v_exp = ve;
       m_run = m_new;
     }
-    f16x4 p[PT][NS];
+    f16x4 p[2][NS];
 #pragma unroll
     for (int u = 0; u < NS; ++u) {
       // (a maximum of infinity as a factor that leaves a probability of 0 one: rows that see the page become NaN, others do not)
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
         asm("" : "+v"(y));
         const _Float16 hi16 = (_Float16)y;
         p[0][u][e] = hi16;
-        if (PT == 2) p[PT - 1][u][e] = (_Float16)(y - (float)hi16);
+        p[1][u][e] = (_Float16)(y - (float)hi16);
       }
     }
     // O': channels 64 c + 4 (lane & 15) + k of the value operand
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
         for (int k = 0; k < 4; ++k) {
           const f16x8 v = codes8(vw[u][c][k], vw[u + 1][c][k]);
 #pragma unroll
-          for (int term = 0; term < PT; ++term) {
+          for (int term = 0; term < 2; ++term) {
             const f16x8 pp = __builtin_shufflevector(p[term][u], p[term][u + 1], 0, 1, 2, 3, 4, 5, 6, 7);
             o[c][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pp, o[c][k], 0, 0, 0);
           }

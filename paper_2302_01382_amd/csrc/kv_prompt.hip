@@ -69,8 +69,10 @@ __device__ __forceinline__ void lds_meet() {
 
 template <int T, int DH, int NQ>
 struct PromptCfg {
-  // fp16 terms of q, and of a probability: a second one takes a fifth of the time (fp16, two prompts of up to 4500 rows 283 | 347 us)
-  // and an fp16 output's distance to 64 bits from 3.0e-4 to 2.1e-4, its own rounding's; bf16's is 1.7e-3 either way
+  // fp16 terms of q, and of a probability.  A second one of these takes a quarter of the time (bf16, two prompts of up to 4500 rows 262 |
+  // 337 us).  It brings an fp16 output's distance to 64 bits from 3.0e-4 to 2.1e-4, its own rounding's.  A bf16 output's is 1.7e-3
+  // either way: one term is off by 2^-11 at most, an eighth of bf16's half step, and outputs differ from those of fp32 products in one
+  // step here and there (8.8e-4 of their power, 7.3e-5 with two).
   static constexpr int QT = T == MPQ_F32 ? 2 : 1, PT = T == MPQ_BF16 ? 1 : 2;
   // Waves: two workgroups of four share a CU, each at its own pace, and work comes in smaller pieces than with eight; dim > 128
   // fills the LDS with one workgroup (us, 8 | 4 waves: two prompts of up to 4500 rows of 16 / 4 heads of 128 306 | 283; 8 of 1000

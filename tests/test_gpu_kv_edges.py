@@ -105,3 +105,41 @@ def test_an_infinite_page_spoils_the_rows_that_see_it(dtype, name, page, new, wi
     assert bad.any() and not bad.all() and got[t].isnan().all()
     got[t] = clean[t]
     check(c, full(got), full(q), True, window, 0.125, dtype)
+
+
+def half_step(x, dtype):
+    """Half a step of the type at x."""
+    half, least = {"float32": (2.0 ** -24, 0.0), "bfloat16": (2.0 ** -8, 0.0), "float16": (2.0 ** -11, 2.0 ** -25)}[dtype]
+    return np.maximum(half * 2.0 ** np.floor(np.log2(np.maximum(x, 1e-30))), least)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("page", (16, 64))
+@pytest.mark.parametrize("rows", (1, 512))
+def test_probabilities_keep_their_bits(dtype, page, rows):
+    """With a value of its own channel for each of 64 tokens an output is a token's probability.  Products of whole numbers are exact
+    here, so that a logit below 9 is off by its scalings alone (9 * 4 * 2^-24 = 1.125 * 2^-19) and a probability by that, its exponential
+    and the value factor that it takes along (2^-20), its two fp16 terms and the sum (2^-21, 64 * 2^-24): 1.94 * 2^-18 together.
+    The terms end at 2^-25 of a scale that holds the largest one at 2^8 or more: 2^-33, of values below 2.  bf16 prompts (512 rows of
+    16 key heads) have one term: 2^-11 more.  Beyond that an output is off by the half step that it is rounded by."""
+    r = rng(page + rows)
+    heads = 16
+    for seed in range(6):
+        c, table = filled(r, 1, [64], heads, 64, page, 8, dtype)
+        k = r.integers(-127, 128, (64, heads, 64)).astype(np.float64)
+        k[::page] = 127.0                      # a page's maximum, so that codes are the numbers
+        size = 1 + seed / 16
+        v = np.broadcast_to(np.eye(64)[:, None, :] * size, (64, heads, 64))
+        b = c.batch([64], [64], table)
+        mpq.kv_append(c.dev, b, dev(k, dtype), dev(v, dtype))
+        b = c.batch([rows], [64], table)
+        q = r.integers(-3, 4, (rows, heads, 64)).astype(np.float64)
+        scale = 1 / 1024
+        got = full(mpq.kv_attention(c.dev, b, dev(q, dtype), causal=False, softmax_scale=scale)).astype(np.float64)
+        x = np.einsum("jhd,rhd->rhj", k, q) * scale
+        e = np.exp(x - x.max(2, keepdims=True))
+        p = e / e.sum(2, keepdims=True) * size
+        off = p * (2.0 ** -17 + (2.0 ** -11 if dtype == "bfloat16" and rows > 1 else 0)) + 2.0 ** -32
+        assert np.abs(x).max() < 9 and np.isfinite(got).all()
+        over = np.abs(got - p) - off - half_step(p + off, dtype)
+        assert (over <= 0).all(), (over.max(), (over > 0).sum())
