@@ -143,3 +143,24 @@ def test_probabilities_keep_their_bits(dtype, page, rows):
         assert np.abs(x).max() < 9 and np.isfinite(got).all()
         over = np.abs(got - p) - off - half_step(p + off, dtype)
         assert (over <= 0).all(), (over.max(), (over > 0).sum())
+
+
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 90)])
+@pytest.mark.parametrize("seqs,heads,group,dim,page,new,held", [
+    (3, 1, 2, 64, 16, 1, 700), (2, 2, 4, 128, 64, 1, 300), (1, 1, 4, 128, 64, 1, 5000), (2, 1, 1, 256, 128, 20, 200),
+    (8, 4, 2, 64, 16, 128, 70), (8, 4, 2, 128, 64, 128, 30), (8, 4, 2, 80, 128, 64, 1500), (8, 16, 1, 256, 32, 128, 9)])
+def test_fp16_keeps_the_bits_of_its_type(causal, window, seqs, heads, group, dim, page, new, held):
+    """check_attention's bound with the two terms of an fp16 call's probabilities: 2^-22 of each, and 2^-33 absolutely (prompts; single
+    tokens 2^-39), so that the values' mean is off by 2 V 2^-22 and n 2^-32 V in place of 2 V 2^-12 and n 2^-38 V."""
+    r = rng(dim + page + new + window)
+    lengths = [new + held - 3 * s for s in range(seqs)]
+    c, table = filled(r, seqs, lengths, heads, dim, page, 8, "float16")
+    b = c.batch([new] * seqs, lengths, table, new, max(lengths))
+    q = dev(r.standard_normal((b.rows, heads * group, dim)) * 2, "float16")
+    got = full(mpq.kv_attention(c.dev, b, q, causal=causal, window=window))
+    want, logit, big = c.host.attention(c.starts, c.length, c.table, full(q), causal, window, dim ** -0.5)
+    n, u = max(lengths), 2.0 ** -24
+    e = logit * ((dim + 4) * u + 2.0 ** -21)
+    off = (2 * big * (2 * e + 2.0 ** -21 + (n / 4 + 64) * u + 2.0 ** -22) + n * 2.0 ** -32 * big)[..., None]
+    over = np.abs(got - want) - off - half_step(np.abs(want) + off, "float16")
+    assert np.isfinite(got).all() and (over <= 0).all(), over.max()
