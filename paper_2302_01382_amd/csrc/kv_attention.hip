@@ -45,6 +45,7 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
   typedef typename E::type El;
   constexpr int QT = S::QT, TT = S::TT, NS = S::NS, DP = S::DP, NP = ONE ? 1 : NS;
   __shared__ float sm_m[NW][16], sm_l[NW][16];
+  __shared__ int sm_e[NW];
   __shared__ __attribute__((aligned(16))) float sm_o[NW / 2][16][DP + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int r = lane & 15, quarter = lane >> 4;
@@ -292,14 +293,19 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
     sm_m[wave][r] = m_run;
     sm_l[wave][r] = l_run;
   }
+  if (lane == 0) sm_e[wave] = v_exp;
   __syncthreads();
   float m_all = sm_m[0][r];
+  int e_all = sm_e[0];  // shares are added in units of 2^e_all: they are as large as the sum then, whatever the values are
 #pragma unroll
-  for (int w = 1; w < NW; ++w) m_all = fmaxf(m_all, sm_m[w][r]);
+  for (int w = 1; w < NW; ++w) {
+    m_all = fmaxf(m_all, sm_m[w][r]);
+    e_all = max(e_all, sm_e[w]);
+  }
   const float m_use = m_all == -__builtin_inff() ? 0.0f : m_all;
   const float mine = __builtin_amdgcn_exp2f(m_run - m_use);
   const float qmax = (float)((1 << (a.c.bits - 1)) - 1);
-  const float f = l_run > 0.0f ? __builtin_ldexpf(mine, v_exp - kPBits) / qmax : 0.0f;
+  const float f = l_run > 0.0f ? __builtin_ldexpf(mine / qmax, v_exp - e_all - kPBits) : 0.0f;
 #pragma unroll
   for (int half = 1; half >= 0; --half) {  // the upper half of the waves leaves its share, the lower half adds its own
     if (wave / (NW / 2) == half) {
@@ -331,14 +337,16 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
     if (a.splits > 1) {
       *reinterpret_cast<f32x4*>(a.part_o + (slot * 16 + row) * D + d) = v;
       if (d == 0) {
-        a.part_ml[(slot * 16 + row) * 2] = top;
-        a.part_ml[(slot * 16 + row) * 2 + 1] = l;
+        float* part = a.part_mle + (slot * 16 + row) * 3;
+        part[0] = top;
+        part[1] = l;
+        part[2] = (float)e_all;
       }
       continue;
     }
     const unsigned token = (unsigned)at / group;
     El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + token) * a.o_ts + (int64_t)(h * a.group + (int)((unsigned)at - token * group)) * a.o_hs + d;
-    E::store4(to, l == 0.0f ? f32x4{0, 0, 0, 0} : v / l);  // (a row with a NaN in q has one in l)
+    E::store4(to, l == 0.0f ? f32x4{0, 0, 0, 0} : times_two_to(v / l, e_all));  // (a row with a NaN in q has one in l)
   }
 }
 
@@ -350,7 +358,7 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   using E = Elem<T>;
   typedef typename E::type El;
   __shared__ __attribute__((aligned(16))) float sm_o[kBlock * 4];
-  __shared__ float sm_l[kBlock], sm_m[kBlock / kWave];
+  __shared__ float sm_l[kBlock], sm_m[kBlock / kWave], sm_e[kBlock / kWave];
   const Digits g = digits(a.tile_rows, a.row_tiles, a.c.heads);
   const int row = (int)g.d[0], h = (int)g.d[2];
   const int64_t tile = g.d[1], s = g.d[3], slot = ((s * a.c.heads + h) * a.row_tiles + tile) * a.splits;
@@ -360,21 +368,30 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   if (at >= (int64_t)sq.n * a.group) return;
   const int D = a.c.dim, quads = D >> 2, parts = kBlock / quads;
   const int d = ((int)threadIdx.x % quads) * 4, part = (int)threadIdx.x / quads;
-  float top = -__builtin_inff();
-  for (int i = threadIdx.x; i < a.splits; i += kBlock) top = fmaxf(top, a.part_ml[((slot + i) * 16 + row) * 2]);
+  const float* ml = a.part_mle + (slot * 16 + row) * 3;  // of a split: 48 floats further
+  float top = -__builtin_inff(), exponent = -__builtin_inff();
+  for (int i = threadIdx.x; i < a.splits; i += kBlock) {
+    top = fmaxf(top, ml[i * 48]);
+    exponent = fmaxf(exponent, ml[i * 48 + 2]);
+  }
   top = wave_max(top);
-  if ((threadIdx.x & 63) == 0) sm_m[threadIdx.x >> 6] = top;
+  exponent = wave_max(exponent);
+  if ((threadIdx.x & 63) == 0) {
+    sm_m[threadIdx.x >> 6] = top;
+    sm_e[threadIdx.x >> 6] = exponent;
+  }
   __syncthreads();
   top = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
+  const int e_all = (int)fmaxf(fmaxf(sm_e[0], sm_e[1]), fmaxf(sm_e[2], sm_e[3]));
   const float use = top == -__builtin_inff() ? 0.0f : top;
   float l = 0.0f;
   f32x4 v = {0, 0, 0, 0};
   if (part < parts) {
 #pragma unroll 4
     for (int i = part; i < a.splits; i += parts) {
-      const float f = __builtin_amdgcn_exp2f(a.part_ml[((slot + i) * 16 + row) * 2] - use);
-      l += a.part_ml[((slot + i) * 16 + row) * 2 + 1] * f;
-      v += *reinterpret_cast<const f32x4*>(a.part_o + ((slot + i) * 16 + row) * D + d) * f;
+      const float f = __builtin_amdgcn_exp2f(ml[i * 48] - use);
+      l += ml[i * 48 + 1] * f;
+      v += *reinterpret_cast<const f32x4*>(a.part_o + ((slot + i) * 16 + row) * D + d) * __builtin_ldexpf(f, (int)ml[i * 48 + 2] - e_all);
     }
   }
   *reinterpret_cast<f32x4*>(sm_o + 4 * threadIdx.x) = v;
@@ -387,7 +404,7 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   }
   const unsigned group = (unsigned)a.group, token = (unsigned)at / group;
   El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + token) * a.o_ts + (int64_t)(h * a.group + (int)((unsigned)at - token * group)) * a.o_hs + d;
-  E::store4(to, l == 0.0f ? f32x4{0, 0, 0, 0} : v / l);  // (a row with a NaN in q has one in l)
+  E::store4(to, l == 0.0f ? f32x4{0, 0, 0, 0} : times_two_to(v / l, e_all));  // (a row with a NaN in q has one in l)
 }
 
 // Which kernel takes a call, in what pieces.  us on the device, prompt kernel | decode kernel (rows, heads x group, dim; nothing
@@ -438,7 +455,7 @@ static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int type
     p.splits = (int)(n < 1 ? 1 : n);
   }
   if (blocks_z(p.tiles * (p.splits > 16 ? p.splits : 16), 512) > 65535u) return MPQ_ERR_SHAPE;
-  p.ws_bytes = p.splits > 1 ? (size_t)p.tiles * p.splits * 16 * (c.dim + 2) * sizeof(float) : 0;
+  p.ws_bytes = p.splits > 1 ? (size_t)p.tiles * p.splits * 16 * (c.dim + 3) * sizeof(float) : 0;
   return MPQ_OK;
 }
 
@@ -500,7 +517,7 @@ extern "C" int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* b
              causal != 0, cut_window(window), softmax_scale, p.row_tiles, p.splits, p.tile_rows, nullptr, nullptr};
   if (p.splits > 1) {
     a.part_o = reinterpret_cast<float*>(ws);
-    a.part_ml = a.part_o + (size_t)p.tiles * p.splits * 16 * cache->dim;
+    a.part_mle = a.part_o + (size_t)p.tiles * p.splits * 16 * cache->dim;
   }
   hipStream_t st = (hipStream_t)stream;
   if (type == MPQ_F32) return launch_attention<MPQ_F32>(a, p, st);

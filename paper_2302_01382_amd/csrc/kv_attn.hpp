@@ -22,8 +22,8 @@ struct AttnArgs {
   int64_t row_tiles;  // tiles of 16 (row, query head) pairs per sequence and key head
   int splits;
   int tile_rows;      // of a tile that a sequence may have: 16 but where there is a single tile
-  float* part_o;      // splits > 1: [tile][split][16][dim], then
-  float* part_ml;     // [tile][split][16][2]
+  float* part_o;      // splits > 1: [tile][split][16][dim] in units of 2^exponent, then
+  float* part_mle;    // [tile][split][16][3]: maximum, sum, exponent
 };
 
 // defined in kv_prompt.hip: the most rows of a workgroup there, and the launch of wg_tiles row tiles of wg_rows (those, or for
@@ -71,6 +71,10 @@ __device__ __forceinline__ Digits digits(int64_t a, int64_t b, int64_t c) {
 
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
   return ((a | b) >> 32) == 0 ? (int64_t)((unsigned)a / (unsigned)b) : a / b;
+}
+
+__device__ __forceinline__ f32x4 times_two_to(f32x4 v, int e) {
+  return f32x4{__builtin_ldexpf(v.x, e), __builtin_ldexpf(v.y, e), __builtin_ldexpf(v.z, e), __builtin_ldexpf(v.w, e)};
 }
 
 __device__ __forceinline__ float across(float v, int mask) { return __shfl_xor(v, mask, 64); }

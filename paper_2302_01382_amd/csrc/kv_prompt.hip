@@ -464,7 +464,7 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
     l += across(l, 32);
     const int at = w0 + n * 16 + r;
     if (at >= nrows) continue;
-    const float f = l == 0.0f ? 0.0f : __builtin_ldexpf(1.0f / qmax, v_exp) * (a.splits > 1 ? __builtin_amdgcn_exp2f(-kUp) : 1.0f / l);
+    const float f = l == 0.0f ? 0.0f : 1.0f / qmax * (a.splits > 1 ? __builtin_amdgcn_exp2f(-kUp) : 1.0f / l);
     const int64_t slot = (pair * a.row_tiles + (at >> 4)) * a.splits + split;
     float* part = a.part_o + (slot * 16 + r) * D;
     const int i = at / group;
@@ -477,11 +477,13 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
         if (d >= D) continue;
         const f32x4 v = f32x4{o[n][4 * c][e], o[n][4 * c + 1][e], o[n][4 * c + 2][e], o[n][4 * c + 3][e]} * f;
         if (a.splits > 1) *reinterpret_cast<f32x4*>(part + d) = v;
-        else E::store4(to + d, v);
+        else E::store4(to + d, times_two_to(v, v_exp));
       }
     if (a.splits > 1 && quarter == 0) {
-      a.part_ml[(slot * 16 + r) * 2] = m_top[n] == -__builtin_inff() ? m_top[n] : m_use[n];
-      a.part_ml[(slot * 16 + r) * 2 + 1] = l * __builtin_amdgcn_exp2f(-kUp);
+      float* mle = a.part_mle + (slot * 16 + r) * 3;
+      mle[0] = m_top[n] == -__builtin_inff() ? m_top[n] : m_use[n];
+      mle[1] = l * __builtin_amdgcn_exp2f(-kUp);
+      mle[2] = (float)v_exp;
     }
   }
 }

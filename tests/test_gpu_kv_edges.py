@@ -164,3 +164,32 @@ def test_fp16_keeps_the_bits_of_its_type(causal, window, seqs, heads, group, dim
     off = (2 * big * (2 * e + 2.0 ** -21 + (n / 4 + 64) * u + 2.0 ** -22) + n * 2.0 ** -32 * big)[..., None]
     over = np.abs(got - want) - off - half_step(np.abs(want) + off, "float16")
     assert np.isfinite(got).all() and (over <= 0).all(), over.max()
+
+
+@pytest.mark.parametrize("dtype", ("float32", "bfloat16"))
+@pytest.mark.parametrize("size", (3e38, 1e-30, 1e-33, 2e-36))
+@pytest.mark.parametrize("seqs,heads,dim,page,new,held", [
+    (3, 1, 64, 16, 1, 700), (1, 1, 128, 64, 1, 5000), (2, 1, 256, 128, 20, 200), (8, 4, 64, 64, 128, 70), (8, 4, 128, 16, 64, 1500)])
+def test_values_at_the_ends_of_their_range(dtype, size, seqs, heads, dim, page, new, held):
+    """Single tokens and prompts, split and not: a weighted mean of values is no larger than they are and as precise, next to the
+    largest number of the type (sums pass it) and next to the smallest (a factor of the sums passes that).  An output of a bf16 call
+    may be one of its subnormals, of 2^-133, and an fp32 one of 2^-149: a half step of those more, 2^-134."""
+    import torch
+    r = rng(dim + page + new)
+    lengths = [new + held - 3 * s for s in range(seqs)]
+    c, table = filled(r, seqs, lengths, heads, dim, page, 8, dtype)
+    b = c.batch(lengths, lengths, table)
+    k = r.standard_normal((b.rows, heads, dim))
+    v = r.uniform(-1, 1, (b.rows, heads, dim)) + 0.5 * np.sign(r.standard_normal((1, heads, dim)))   # channels with a mean
+    v = (torch.from_numpy(v / 1.5).double() * size).to(getattr(torch, dtype)).cuda()
+    c.append(b, dev(k, dtype), v)
+    b = c.batch([new] * seqs, lengths, table, new, max(lengths))
+    q = dev(r.standard_normal((b.rows, heads * 2, dim)), dtype)
+    got = full(mpq.kv_attention(c.dev, b, q)).astype(np.float64)
+    want, logit, big = c.host.attention(c.starts, c.length, c.table, full(q), True, 0, dim ** -0.5)
+    n, u = max(lengths), 2.0 ** -24
+    e = logit * ((dim + 4) * u + 2.0 ** -21)
+    p = 2.0 ** -22 if dtype == "float32" else 2.0 ** -12
+    off = (2 * big * (2 * e + 2.0 ** -21 + (n / 4 + 64) * u + p) + n * 2.0 ** -32 * big)[..., None]
+    over = np.abs(got - want) - off - (2.0 ** -24 if dtype == "float32" else 2.0 ** -8) * (np.abs(want) + off) - 2.0 ** -134
+    assert np.isfinite(got).all() and (over <= 0).all(), (over / size).max()
