@@ -35,7 +35,6 @@ struct Elem<MPQ_F32> {
     const f32x4 a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  static __device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4_any*>(p); }
   static __device__ __forceinline__ void store4(float* p, f32x4 v) { *reinterpret_cast<f32x4_any*>(p) = v; }
   static __device__ __forceinline__ void store8(float* p, f32x8 v) {
     store4(p, __builtin_shufflevector(v, v, 0, 1, 2, 3));
@@ -47,9 +46,6 @@ struct Elem<MPQ_BF16> {
   typedef __bf16 type;
   static __device__ __forceinline__ f32x8 load8(const __bf16* p) {
     return __builtin_convertvector((bf16x8)*reinterpret_cast<const bf16x8_any*>(p), f32x8);
-  }
-  static __device__ __forceinline__ f32x4 load4(const __bf16* p) {
-    return __builtin_convertvector((bf16x4)*reinterpret_cast<const bf16x4_any*>(p), f32x4);
   }
   static __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
     *reinterpret_cast<bf16x4_any*>(p) = __builtin_convertvector(v, bf16x4);
@@ -63,9 +59,6 @@ struct Elem<MPQ_F16> {
   typedef _Float16 type;
   static __device__ __forceinline__ f32x8 load8(const _Float16* p) {
     return __builtin_convertvector((f16x8)*reinterpret_cast<const f16x8_any*>(p), f32x8);
-  }
-  static __device__ __forceinline__ f32x4 load4(const _Float16* p) {
-    return __builtin_convertvector((f16x4)*reinterpret_cast<const f16x4_any*>(p), f32x4);
   }
   static __device__ __forceinline__ void store4(_Float16* p, f32x4 v) {
     *reinterpret_cast<f16x4_any*>(p) = __builtin_convertvector(v, f16x4);
