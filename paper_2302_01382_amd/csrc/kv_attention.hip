@@ -483,6 +483,18 @@ static int launch_attention(const AttnArgs& a, const AttnPlan& p, hipStream_t st
   return launch_status();
 }
 
+// Whether two of the rows x heads pieces of dim elements share one: workgroups would write it at the same time.  Strides are not
+// negative and their products with rows and heads were looked at.
+static bool pieces_overlap(int64_t rows, int64_t row_stride, int64_t heads, int64_t head_stride, int dim) {
+  if ((rows > 1 && row_stride < dim) || (heads > 1 && head_stride < dim)) return true;
+  if (rows == 1 || heads == 1 || row_stride >= (heads - 1) * head_stride + dim || head_stride >= (rows - 1) * row_stride + dim) return false;
+  for (int64_t j = 1; j < heads; ++j) {  // heads between the rows: a row as near to j heads' distance as there is
+    const int64_t i = j * head_stride / row_stride, over = j * head_stride - i * row_stride;
+    if ((i < rows && over < dim) || (i + 1 < rows && row_stride - over < dim)) return true;
+  }
+  return false;
+}
+
 }  // namespace mpq
 
 using namespace mpq;
@@ -507,6 +519,7 @@ extern "C" int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* b
   if (mul_overflows(batch->rows, q_token_stride) || mul_overflows(batch->rows, out_token_stride) || mul_overflows(q_heads, q_head_stride) ||
       mul_overflows(q_heads, out_head_stride))
     return MPQ_ERR_SHAPE;
+  if (batch->rows > 0 && pieces_overlap(batch->rows, out_token_stride, q_heads, out_head_stride, cache->dim)) return MPQ_ERR_SHAPE;
   const uintptr_t el = (uintptr_t)(type_size(type) - 1);
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & el) return MPQ_ERR_ALIGN;
   if (p.tiles == 0) return MPQ_OK;
