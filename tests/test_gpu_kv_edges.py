@@ -193,3 +193,26 @@ def test_values_at_the_ends_of_their_range(dtype, size, seqs, heads, dim, page, 
     off = (2 * big * (2 * e + 2.0 ** -21 + (n / 4 + 64) * u + p) + n * 2.0 ** -32 * big)[..., None]
     over = np.abs(got - want) - off - (2.0 ** -24 if dtype == "float32" else 2.0 ** -8) * (np.abs(want) + off) - 2.0 ** -134
     assert np.isfinite(got).all() and (over <= 0).all(), (over / size).max()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("page", (16, 64, 128))
+@pytest.mark.parametrize("new", (1, 9, 128))
+def test_pages_behind_the_window_may_hold_anything(dtype, page, new):
+    """A server gives the pages that a window has left behind to other sequences, or never wrote them: their codes and maxima
+    (a NaN here) reach no row, also where a step's tokens lie on both sides of the window's beginning."""
+    import torch
+    r = rng(page + new)
+    window = 70
+    lengths = [256, 200, 300, 150, 141, 140, 257, 190]
+    c, table = filled(r, 8, lengths, 4, 64, page, 8, dtype)
+    b = c.batch([new] * 8, lengths, table, new, 300)
+    for s, n in enumerate(lengths):
+        for on in table[s, :max(n - new - window + 1, 0) // page]:
+            for t in (c.dev.k_absmax, c.dev.v_absmax):
+                t[int(on)] = float("nan")
+            for t in (c.dev.k_codes, c.dev.v_codes):
+                t[int(on)] = torch.randint(-128, 128, t[int(on)].shape, dtype=torch.int8, device="cuda")
+    assert c.dev.k_absmax[torch.from_numpy(table[2, :2]).cuda().long()].isnan().any() or page == 128 or new == 128
+    q = dev(r.standard_normal((b.rows, 8, 64)), dtype)
+    check(c, full(mpq.kv_attention(c.dev, b, q, window=window)), full(q), True, window, 0.125, dtype)
