@@ -15,8 +15,8 @@
 // by more.
 //
 // Two prompts of up to 4500 rows behind up to 1000 tokens, 16 query and 4 key heads of 128 channels in bf16: 262 us, 868
-// TFLOP/s of the pairs that the mask leaves.  Matrix steps take 32 % of the SIMDs' cycles, vector instructions (a third of them the
-// exponentials, a quarter the codes' way into fp16) 50 %, with two waves per SIMD that 220 registers leave room for; a sixth of the
+// TFLOP/s of the pairs that the mask leaves.  Matrix steps take 35 % of the SIMDs' cycles, vector instructions (a third of them the
+// exponentials, a quarter the codes' way into fp16) 55 %, with two waves per SIMD that 232 registers leave room for; a sixth of the
 // time is the last workgroups' alone.  Operands are read out of the LDS four reads ahead, the first values' under the softmax (282
 // with the compiler's one or two).  What did not help: the next keys' matrix steps between the exponentials (302 against
 // 302), two groups of waves that take turns with matrix steps and softmax behind barriers (327 against 304), s_setprio around
