@@ -489,11 +489,12 @@ int mpq_linear_tokens(const void* x, int x_type, int64_t M, int64_t N, int64_t K
  *     out = sum_j P_j V_j,  P = softmax over the visible j of softmax_scale * (q . K_j),  K, V = code * m / qmax_b;
  *   visible: j < kv_len and on a valid page; with `causal` also j <= p, and with window > 0 (causal only) j > p - window.
  *   A row that sees nothing gives 0.  q, out [rows][q_heads][dim] of `type`, dim contiguous, strides in
- *   elements (out's rows and heads may not overlap), max_new * q_heads / heads < 2^31.  Logits, statistics and sums in fp32.  What is multiplied: codes,
- *   exact; q as one fp16 term (bf16 and fp16: exact down to 2^-28 of the row's largest entry) or two (fp32: about 22
- *   bits), a row whose largest entry is below 2^-100 with fewer bits; probabilities as two fp16 terms (about 22
- *   bits), in bf16 calls of many rows as one (11 bits).  Values are summed relative to the largest page maximum that
- *   neighbouring rows (up to 128) see, to 2^-33 of it: pages whose values are smaller by many orders lose bits beside it.
+ *   elements (out's rows and heads may not overlap), max_new * q_heads / heads < 2^31.
+ *   Logits, statistics and sums in fp32.  What is multiplied: codes, exact; q as one fp16 term (bf16 and fp16: exact
+ *   down to 2^-28 of the row's largest entry) or two (fp32: about 22 bits), a row whose largest entry is below 2^-100
+ *   with fewer bits; probabilities as two fp16 terms (about 22 bits), in bf16 calls of many rows as one (11 bits).
+ *   Values are summed relative to the largest page maximum that neighbouring rows (up to 128) see, to 2^-33 of it: pages
+ *   whose values are smaller by many orders lose bits beside it.
  *   Workspace from the query, 16-byte aligned (0 where one workgroup takes a sequence's keys).
  * Errors (all three): MPQ_ERR_NULL, MPQ_ERR_SHAPE, MPQ_ERR_BITS, MPQ_ERR_ALIGN (codes, maxima, elements),
  *   MPQ_ERR_WORKSPACE.  rows = 0 or seqs = 0: nothing is launched. */

@@ -336,12 +336,7 @@ __global__ __launch_bounds__(NW * 64) void kv_attention_k(AttnArgs a) {
     if (at >= nrows) continue;
     if (a.splits > 1) {
       *reinterpret_cast<f32x4*>(a.part_o + (slot * 16 + row) * D + d) = v;
-      if (d == 0) {
-        float* part = a.part_mle + (slot * 16 + row) * 3;
-        part[0] = top;
-        part[1] = l;
-        part[2] = (float)e_all;
-      }
+      if (d == 0) a.part[slot * 16 + row] = Partial{top, l, (float)e_all};
       continue;
     }
     const unsigned token = (unsigned)at / group;
@@ -368,11 +363,12 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   if (at >= (int64_t)sq.n * a.group) return;
   const int D = a.c.dim, quads = D >> 2, parts = kBlock / quads;
   const int d = ((int)threadIdx.x % quads) * 4, part = (int)threadIdx.x / quads;
-  const float* ml = a.part_mle + (slot * 16 + row) * 3;  // of a split: 48 floats further
+  const Partial* of = a.part + slot * 16 + row;  // the row's in the first split; 16 to the next
   float top = -__builtin_inff(), exponent = -__builtin_inff();
   for (int i = threadIdx.x; i < a.splits; i += kBlock) {
-    top = fmaxf(top, ml[i * 48]);
-    exponent = fmaxf(exponent, ml[i * 48 + 2]);
+    const Partial x = of[(int64_t)i * 16];
+    top = fmaxf(top, x.m);
+    exponent = fmaxf(exponent, x.e);
   }
   top = wave_max(top);
   exponent = wave_max(exponent);
@@ -389,9 +385,10 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   if (part < parts) {
 #pragma unroll 4
     for (int i = part; i < a.splits; i += parts) {
-      const float f = __builtin_amdgcn_exp2f(ml[i * 48] - use);
-      l += ml[i * 48 + 1] * f;
-      v += *reinterpret_cast<const f32x4*>(a.part_o + ((slot + i) * 16 + row) * D + d) * __builtin_ldexpf(f, (int)ml[i * 48 + 2] - e_all);
+      const Partial x = of[(int64_t)i * 16];
+      const float f = __builtin_amdgcn_exp2f(x.m - use);
+      l += x.l * f;
+      v += *reinterpret_cast<const f32x4*>(a.part_o + ((slot + i) * 16 + row) * D + d) * __builtin_ldexpf(f, (int)x.e - e_all);
     }
   }
   *reinterpret_cast<f32x4*>(sm_o + 4 * threadIdx.x) = v;
@@ -455,7 +452,7 @@ static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int type
     p.splits = (int)(n < 1 ? 1 : n);
   }
   if (blocks_z(p.tiles * (p.splits > 16 ? p.splits : 16), 512) > 65535u) return MPQ_ERR_SHAPE;
-  p.ws_bytes = p.splits > 1 ? (size_t)p.tiles * p.splits * 16 * (c.dim + 3) * sizeof(float) : 0;
+  p.ws_bytes = p.splits > 1 ? (size_t)p.tiles * p.splits * 16 * (c.dim * sizeof(float) + sizeof(Partial)) : 0;
   return MPQ_OK;
 }
 
@@ -530,7 +527,7 @@ extern "C" int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* b
              causal != 0, cut_window(window), softmax_scale, p.row_tiles, p.splits, p.tile_rows, nullptr, nullptr};
   if (p.splits > 1) {
     a.part_o = reinterpret_cast<float*>(ws);
-    a.part_mle = a.part_o + (size_t)p.tiles * p.splits * 16 * cache->dim;
+    a.part = reinterpret_cast<Partial*>(a.part_o + (size_t)p.tiles * p.splits * 16 * cache->dim);
   }
   hipStream_t st = (hipStream_t)stream;
   if (type == MPQ_F32) return launch_attention<MPQ_F32>(a, p, st);

@@ -9,6 +9,10 @@ namespace mpq {
 typedef int v4i __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
+// of a split's row: maximum, sum, and the exponent of the power of two that its share of the output is in units of
+struct Partial {
+  float m, l, e;
+};
 struct AttnArgs {
   mpq_kv_cache c;
   mpq_kv_batch b;
@@ -22,8 +26,8 @@ struct AttnArgs {
   int64_t row_tiles;  // tiles of 16 (row, query head) pairs per sequence and key head
   int splits;
   int tile_rows;      // of a tile that a sequence may have: 16 but where there is a single tile
-  float* part_o;      // splits > 1: [tile][split][16][dim] in units of 2^exponent, then
-  float* part_mle;    // [tile][split][16][3]: maximum, sum, exponent
+  float* part_o;      // splits > 1: [tile][split][16][dim], then
+  Partial* part;      // [tile][split][16]
 };
 
 // defined in kv_prompt.hip: the most rows of a workgroup there, and the launch of wg_tiles row tiles of wg_rows (those, or for

@@ -479,12 +479,8 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
         if (a.splits > 1) *reinterpret_cast<f32x4*>(part + d) = v;
         else E::store4(to + d, times_two_to(v, v_exp));
       }
-    if (a.splits > 1 && quarter == 0) {
-      float* mle = a.part_mle + (slot * 16 + r) * 3;
-      mle[0] = m_top[n] == -__builtin_inff() ? m_top[n] : m_use[n];
-      mle[1] = l * __builtin_amdgcn_exp2f(-kUp);
-      mle[2] = (float)v_exp;
-    }
+    if (a.splits > 1 && quarter == 0)
+      a.part[slot * 16 + r] = Partial{m_top[n] == -__builtin_inff() ? m_top[n] : m_use[n], l * __builtin_amdgcn_exp2f(-kUp), (float)v_exp};
   }
 }
 

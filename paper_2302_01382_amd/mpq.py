@@ -1048,7 +1048,8 @@ def kv_attention_workspace_bytes(cache: KvCache, batch: KvBatch, dtype, q_heads)
 
 def kv_attention(cache: KvCache, batch: KvBatch, q, causal=True, window=0, softmax_scale=None, out=None, ws: Workspace = None):
     """Attention of q [rows, q_heads, dim] (any strides of tokens and heads) over the cache, q_heads a multiple of the cache's
-    heads.  softmax_scale: 1 / sqrt(dim) where not given.  Returns the output, [rows, q_heads, dim] of q's type."""
+    heads.  softmax_scale: 1 / sqrt(dim) where not given.  Returns the output, [rows, q_heads, dim] of q's type (out, whose rows
+    and heads may have any strides that do not overlap); rows that belong to no sequence are left as they were."""
     t, q_ts, q_hs, heads = _kv_rows(cache, batch, q, None, "q")
     stream = _here(q)
     if out is None:
