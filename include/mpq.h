@@ -524,6 +524,82 @@ int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int t
                      int64_t window, void* out, int64_t out_token_stride, int64_t out_head_stride, void* ws,
                      size_t ws_bytes, void* stream);
 
+/* ==== a step of drafted tokens ====================================================================
+ * A served model whose next tokens another, smaller one has drafted runs all of them at once: through its layers, over the
+ * cache, and into the probabilities by which they are kept or dropped.  A single token is a draft of one.  These calls
+ * complete the step; weights and cache are those of the calls above, types those of mpq_type. */
+
+/* ---- a linear layer whose 4-bit weights have a step per group of input channels ---------------------
+ * y_out[m][n] = act(sum over groups g of w_scale[n][g] * sum over k in g of w_q[n][k] * x[m][k]), rounded once to y_type; act one of
+ * mpq_act, the input as it is (not quantized).
+ * x          [M x K] of x_type, K contiguous, rows x_stride elements apart (x_stride >= K).
+ * w_q        two's-complement nibbles [N x K/2], the even channel in the low half (packed4_out of mpq_fake_quant; the weights seen as
+ *            [N * K/group x group] with MPQ_PER_ROW give codes and maxima of such groups); any alignment.
+ * group      32, 64 or 128; K a multiple of it.   w_scale  [N x K/group] of scale_type, dense.
+ * y_out      [M x N] of y_type, dense.
+ * Products are exact and sums in fp32 (a group's about -24 times the sum of its x, which is added in again: intermediate values are up
+ * to 31 |x| summed); where such a value passes fp32's range, and for an x that is not finite, results are infinite or NaN.
+ * Made for few rows, whose time is that of reading the weights; more go in blocks of 64, each of which reads the weights.
+ * Errors: MPQ_ERR_NULL, MPQ_ERR_SHAPE (dims, stride, group, an unknown type or act), MPQ_ERR_ALIGN (elements).  M = 0: nothing is
+ * launched. */
+int mpq_linear_groups(const void* x, int x_type, int64_t M, int64_t N, int64_t K, int64_t x_stride, const uint8_t* w_q, int group,
+                      const void* w_scale, int scale_type, int act, int y_type, void* y_out, void* stream);
+
+/* ---- queries and keys between that layer and the cache: a norm per head and the rotation by position --------
+ * For each row i and each of its heads x (dim channels) of q and of k:
+ *   y[d] = x[d] / sqrt(mean over d of x[d]^2 + eps) * weight[d]   (y = x where the weight is NULL; q and k have one each)
+ *   the first 2 * pairs channels in pairs (a, b) become (a cos t - b sin t, b cos t + a sin t), t = positions[i] * frequencies[j] for
+ *   pair j: channels j and j + pairs (MPQ_ROTATE_HALVES) or 2 j and 2 j + 1 (MPQ_ROTATE_PAIRS); the others stay y
+ * Whole turns of t are dropped in 64 bits, so that far positions keep their angle; everything else is fp32, rounded once.
+ * q, k       [rows][q_heads][dim], [rows][k_heads][dim] of `type`, dim contiguous, strides in elements; outputs likewise, their rows and
+ *            heads may not overlap.  An output may be its input (the same address and strides: in place), else it may not overlap
+ *            any input.  q_heads or k_heads may be 0 (pointers are not looked at then).
+ * dim        a multiple of 16, at most 256.   pairs  a multiple of 4, 0 .. dim / 2 (0: positions and frequencies may be NULL).
+ * positions  device int32[rows] (negative: backwards).   frequencies  device float[pairs], radians per position.
+ * weights    device float[dim], 4-byte aligned, nullable.   eps  at least FLT_MIN, finite.
+ * Squares are summed in fp32: a head whose sum is beyond its range gives NaN.
+ * Errors: MPQ_ERR_NULL, MPQ_ERR_SHAPE, MPQ_ERR_ALIGN.  rows = 0 or no heads: nothing is launched. */
+enum mpq_rotate { MPQ_ROTATE_HALVES = 0, MPQ_ROTATE_PAIRS = 1 };
+int mpq_rotate_heads(int type, int64_t rows, int dim, const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
+                     const void* k, int64_t k_token_stride, int64_t k_head_stride, int k_heads, const int32_t* positions,
+                     const float* frequencies, int pairs, int layout, const float* q_weight, const float* k_weight, float eps,
+                     void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* k_out, int64_t k_out_token_stride,
+                     int64_t k_out_head_stride, void* stream);
+
+/* ---- attention of a tree of drafted tokens over the cache ----------------------------------------------
+ * mpq_kv_attention with another mask: a sequence's n rows are its drafted tokens, appended as its last n tokens in any order that a
+ * tree has.  Row i of the call (i - starts[s] of its sequence) sees every token before the drafted ones, and drafted token j of its
+ * sequence where bit j % 64 of tree[i][j / 64] is set -- for a tree: itself and its ancestors (their positions repeat along the
+ * branches; rotations are the caller's, mpq_rotate_heads).
+ * tree       device int64 [rows][tree_words], 8-byte aligned, bits in words from the lowest.  tree_words at least 1 (else
+ *            MPQ_ERR_SHAPE): drafted tokens behind the last word are not seen; bits behind a sequence's last drafted token do not matter.
+ * Everything else, and what is rounded, as mpq_kv_attention without a window.  Tokens that are kept are appended again, in a row, behind
+ * what the sequence held before. */
+size_t mpq_kv_attention_tree_workspace_bytes(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, int q_heads);
+int mpq_kv_attention_tree(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, const void* q, int64_t q_token_stride,
+                          int64_t q_head_stride, int q_heads, float softmax_scale, const int64_t* tree, int tree_words, void* out,
+                          int64_t out_token_stride, int64_t out_head_stride, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- log probabilities of given tokens, with entropy and the most probable alternatives ---------------------
+ * For each row of logits x and p = softmax(scale * x):
+ *   logprob_out[row] = log p[tokens[row]]; minus infinity for a token outside 0 .. vocab - 1
+ *   entropy_out[row] = -sum p log p (terms of p = 0 are 0)
+ *   top_index_out[row][i], top_logprob_out[row][i], i < top: the tokens of the largest logits in descending order, the lower index
+ *   first where they are equal, and their log p; where fewer than top logits are above minus infinity, -1 and minus infinity
+ * A row of nothing but minus infinity has no distribution: NaN, as a row with a NaN or with plus infinity has (whose indices are of
+ * the logits that are not NaN).
+ * logits     [rows x vocab] of `type`, vocab contiguous, rows row_stride elements apart (row_stride >= vocab); vocab at most 2^22.
+ * scale      of the logits (1 / temperature): positive, finite.
+ * tokens     device int32[rows].  Outputs float [rows], float [rows], float and int32 [rows x top].  Nullable: logprob_out (then tokens
+ *            too) and entropy_out; with top = 0 the last two.  top 0 .. 32, at least one output.
+ * Sums in fp32 of exponentials relative to the row's maximum; logits are not rounded.
+ * Workspace from the query, 16-byte aligned (0 where a workgroup takes a row).  Errors: MPQ_ERR_NULL, MPQ_ERR_SHAPE, MPQ_ERR_ALIGN,
+ * MPQ_ERR_WORKSPACE.  rows = 0: nothing is launched. */
+size_t mpq_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int type, int top);
+int mpq_token_logprobs(const void* logits, int type, int64_t rows, int64_t vocab, int64_t row_stride, float scale,
+                       const int32_t* tokens, float* logprob_out, float* entropy_out, int top, float* top_logprob_out,
+                       int32_t* top_index_out, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- measurement aid (not part of the method) --------------------------------------------------
  * Launches a kernel that does nothing but issue the int8 matrix instructions of the GEMM kernels (16x16x64; one
  * workgroup of eight waves per CU, 32 x iters instructions per wave) on operand registers filled once from

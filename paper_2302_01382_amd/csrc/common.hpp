@@ -65,8 +65,9 @@ inline int allow_lds(const void* kern, int bytes, std::atomic<unsigned>* done, i
 
 // defined in hutchinson.hip: allows its kernels the LDS they need on the current device (mpq_init)
 int prepare_hutchinson();
-// ... and in kv_prompt.hip
+// ... and in kv_prompt.hip, kv_tree_wide.hip
 int prepare_prompt();
+int prepare_tree_wide();
 
 // defined in qgemm.hip: the host-side argument checks of mpq_qgemm_act / mpq_qgemm_score, for callers
 // that must validate several layers before their first launch
@@ -82,6 +83,18 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 inline bool mul_overflows(int64_t a, int64_t b) {
   int64_t r;
   return __builtin_mul_overflow(a, b, &r) || r > (int64_t)1 << 46;  // 2^46 elements: 256 TiB fp32
+}
+
+// Whether two of the rows x heads pieces of dim elements share one: workgroups would write it at the same time.  Strides are not
+// negative and their products with rows and heads were looked at.
+inline bool pieces_overlap(int64_t rows, int64_t row_stride, int64_t heads, int64_t head_stride, int dim) {
+  if ((rows > 1 && row_stride < dim) || (heads > 1 && head_stride < dim)) return true;
+  if (rows == 1 || heads == 1 || row_stride >= (heads - 1) * head_stride + dim || head_stride >= (rows - 1) * row_stride + dim) return false;
+  for (int64_t j = 1; j < heads; ++j) {  // heads between the rows: a row as near to j heads' distance as there is
+    const int64_t i = j * head_stride / row_stride, over = j * head_stride - i * row_stride;
+    if ((i < rows && over < dim) || (i + 1 < rows && row_stride - over < dim)) return true;
+  }
+  return false;
 }
 
 inline int64_t channels(int gran, int64_t rows, int64_t cols) {

@@ -457,6 +457,12 @@ static int plan_attention(const mpq_kv_cache& c, const mpq_kv_batch& b, int type
 }
 
 template <int T>
+static int join(const AttnArgs& a, int64_t tiles, hipStream_t st) {
+  kv_attention_join_k<T><<<wide_grid(tiles * a.tile_rows, kBlock), kBlock, 0, st>>>(a);
+  return launch_status();
+}
+
+template <int T>
 static int launch_attention(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   const int dh = a.c.dim <= 64 ? 1 : a.c.dim <= 128 ? 2 : 4;
   const bool one = a.c.page >= (dh <= 2 ? 64 : 32);
@@ -476,20 +482,24 @@ static int launch_attention(const AttnArgs& a, const AttnPlan& p, hipStream_t st
   }
   const int rc = p.wg_tiles > 0 ? launch_prompt(T, a, p.wg_tiles, p.wg_rows, false, st) : launch_status();
   if (rc != MPQ_OK || p.splits == 1) return rc;
-  kv_attention_join_k<T><<<wide_grid(p.tiles * p.tile_rows, kBlock), kBlock, 0, st>>>(a);
-  return launch_status();
+  return join<T>(a, p.tiles, st);
 }
 
-// Whether two of the rows x heads pieces of dim elements share one: workgroups would write it at the same time.  Strides are not
-// negative and their products with rows and heads were looked at.
-static bool pieces_overlap(int64_t rows, int64_t row_stride, int64_t heads, int64_t head_stride, int dim) {
-  if ((rows > 1 && row_stride < dim) || (heads > 1 && head_stride < dim)) return true;
-  if (rows == 1 || heads == 1 || row_stride >= (heads - 1) * head_stride + dim || head_stride >= (rows - 1) * row_stride + dim) return false;
-  for (int64_t j = 1; j < heads; ++j) {  // heads between the rows: a row as near to j heads' distance as there is
-    const int64_t i = j * head_stride / row_stride, over = j * head_stride - i * row_stride;
-    if ((i < rows && over < dim) || (i + 1 < rows && row_stride - over < dim)) return true;
-  }
-  return false;
+int launch_join(int type, const AttnArgs& a, int64_t tiles, hipStream_t st) {
+  if (type == MPQ_F32) return join<MPQ_F32>(a, tiles, st);
+  return type == MPQ_BF16 ? join<MPQ_BF16>(a, tiles, st) : join<MPQ_F16>(a, tiles, st);
+}
+
+int check_rows(const mpq_kv_cache& cache, const mpq_kv_batch& batch, int type, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+               int q_heads, const void* out, int64_t out_token_stride, int64_t out_head_stride) {
+  if (q_token_stride < 0 || q_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0) return MPQ_ERR_SHAPE;
+  if (mul_overflows(batch.rows, q_token_stride) || mul_overflows(batch.rows, out_token_stride) || mul_overflows(q_heads, q_head_stride) ||
+      mul_overflows(q_heads, out_head_stride))
+    return MPQ_ERR_SHAPE;
+  if (batch.rows > 0 && pieces_overlap(batch.rows, out_token_stride, q_heads, out_head_stride, cache.dim)) return MPQ_ERR_SHAPE;
+  const uintptr_t el = (uintptr_t)(type_size(type) - 1);
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & el) return MPQ_ERR_ALIGN;
+  return MPQ_OK;
 }
 
 }  // namespace mpq
@@ -512,13 +522,8 @@ extern "C" int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* b
   rc = plan_attention(*cache, *batch, type, q_heads, p);
   if (rc != MPQ_OK) return rc;
   if (window < 0 || (window > 0 && !causal) || !(softmax_scale == softmax_scale) || __builtin_isinf(softmax_scale)) return MPQ_ERR_SHAPE;
-  if (q_token_stride < 0 || q_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0) return MPQ_ERR_SHAPE;
-  if (mul_overflows(batch->rows, q_token_stride) || mul_overflows(batch->rows, out_token_stride) || mul_overflows(q_heads, q_head_stride) ||
-      mul_overflows(q_heads, out_head_stride))
-    return MPQ_ERR_SHAPE;
-  if (batch->rows > 0 && pieces_overlap(batch->rows, out_token_stride, q_heads, out_head_stride, cache->dim)) return MPQ_ERR_SHAPE;
-  const uintptr_t el = (uintptr_t)(type_size(type) - 1);
-  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & el) return MPQ_ERR_ALIGN;
+  rc = check_rows(*cache, *batch, type, q, q_token_stride, q_head_stride, q_heads, out, out_token_stride, out_head_stride);
+  if (rc != MPQ_OK) return rc;
   if (p.tiles == 0) return MPQ_OK;
   if (!q || !out) return MPQ_ERR_NULL;
   if (p.ws_bytes > 0 && (!ws || ws_bytes < p.ws_bytes)) return MPQ_ERR_WORKSPACE;

@@ -30,12 +30,34 @@ struct AttnArgs {
   Partial* part;      // [tile][split][16]
 };
 
+// which of a sequence's own rows a row sees: bits [rows][words]
+struct TreeMask {
+  const uint64_t* bits;
+  int words;
+};
+
 // defined in kv_prompt.hip: the most rows of a workgroup there, and the launch of wg_tiles row tiles of wg_rows (those, or for
 // dim <= 128 also 64) per sequence and key head
 int prompt_rows(int type, int dim);
 int launch_prompt(int type, const AttnArgs& a, int64_t wg_tiles, int wg_rows, bool prepare_only, hipStream_t st);
 
+// defined in kv_attention.hip: joins the splits of `tiles` tiles; the checks of the attention's own tensors but for NULL
+int launch_join(int type, const AttnArgs& a, int64_t tiles, hipStream_t st);
+int check_rows(const mpq_kv_cache& cache, const mpq_kv_batch& batch, int type, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+               int q_heads, const void* out, int64_t out_token_stride, int64_t out_head_stride);
+// defined in kv_tree_wide.hip, as launch_prompt
+int launch_tree_wide(int type, const AttnArgs& a, const TreeMask& tree, int64_t wg_tiles, int wg_rows, hipStream_t st);
+
 #if defined(__HIPCC__)
+
+// 64 bits of a row of a tree from bit `at` on: ones before its first drafted token, zeros behind its words
+__device__ __forceinline__ uint64_t tree_bits(const TreeMask& tree, int64_t row, int64_t at) {
+  const uint64_t* words = tree.bits + row * tree.words;
+  const int64_t w = at >> 6;
+  const int shift = (int)(at & 63);
+  auto word = [&](int64_t i) { return i < 0 ? ~(uint64_t)0 : i < tree.words ? words[i] : (uint64_t)0; };
+  return shift ? word(w) >> shift | word(w + 1) << (64 - shift) : word(w);
+}
 
 // four codes -> fp16: the byte code + 128 as the low bits of 1024 + u, less 1152 (both exact)
 __device__ __forceinline__ void codes4(int w, f16x2& lo, f16x2& hi) {

@@ -1,0 +1,29 @@
+// kv_tree_wide.hip -- attention of a tree of drafted tokens where a sequence brings many rows: the prompt's kernel (kv_prompt.hpp)
+// with the tree's bits as its mask.
+#include "kv_prompt.hpp"
+
+namespace mpq {
+
+template <int T, int DH, int NQ, bool ONE>
+__global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) void kv_tree_wide_k(AttnArgs a, int64_t wg_tiles, TreeMask tree) {
+  prompt_rows_body<T, DH, NQ, ONE, true>(a, wg_tiles, tree);
+}
+
+struct TreeKernels {
+  typedef void (*Kern)(AttnArgs, int64_t, TreeMask);
+  TreeMask tree;
+  template <int T, int DH, int NQ, bool ONE>
+  static Kern kernel() { return kv_tree_wide_k<T, DH, NQ, ONE>; }
+  int launch(Kern k, dim3 grid, int threads, int lds, hipStream_t st, const AttnArgs& a, int64_t wg_tiles) const {
+    k<<<grid, threads, lds, st>>>(a, wg_tiles, tree);
+    return launch_status();
+  }
+};
+
+int launch_tree_wide(int type, const AttnArgs& a, const TreeMask& tree, int64_t wg_tiles, int wg_rows, hipStream_t st) {
+  return prompt_launch(TreeKernels{tree}, type, a, wg_tiles, wg_rows, false, st);
+}
+
+int prepare_tree_wide() { return prompt_prepare<TreeKernels>(); }
+
+}  // namespace mpq

@@ -498,7 +498,9 @@ extern "C" int mpq_init(void) {
     if (rc != MPQ_OK) return rc;
   }
   const int rc = prepare_hutchinson();
-  return rc == MPQ_OK ? prepare_prompt() : rc;
+  if (rc != MPQ_OK) return rc;
+  const int prompt = prepare_prompt();
+  return prompt == MPQ_OK ? prepare_tree_wide() : prompt;
 }
 
 extern "C" size_t mpq_qgemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int w_storage_bits) {

@@ -25,6 +25,6 @@ const char* mpq_strerror(int status) {
 
 int mpq_last_hip_error(void) { return mpq::g_last_hip_error; }
 
-int mpq_version(void) { return 103; }  // 1.3: the serving calls
+int mpq_version(void) { return 104; }  // 1.4: a step of drafted tokens
 
 }  // extern "C"

@@ -31,6 +31,8 @@ EXPORTS = [
     "mpq_fake_quant_scales", "mpq_scale_grad_workspace_bytes", "mpq_scale_grad", "mpq_scale_sgd_step", "mpq_qgemm_act", "mpq_qgemm_act_codes",
     "mpq_token_quant", "mpq_qgemm_tokens", "mpq_linear_tokens_workspace_bytes", "mpq_linear_tokens",
     "mpq_kv_append", "mpq_kv_gather", "mpq_kv_attention_workspace_bytes", "mpq_kv_attention",
+    "mpq_linear_groups", "mpq_rotate_heads", "mpq_kv_attention_tree_workspace_bytes", "mpq_kv_attention_tree",
+    "mpq_token_logprobs_workspace_bytes", "mpq_token_logprobs",
     "mpq_diag_mfma_operand_bytes", "mpq_diag_mfma_rate", "mpq_diag_sweep_alu_rate", "mpq_fake_quant_step", "mpq_stack_evaluate_workspace_bytes", "mpq_stack_evaluate", "mpq_rademacher", "mpq_hutchinson_quad_workspace_bytes", "mpq_hutchinson_quad", "mpq_hutchinson_quad_signs",
 ]
 
@@ -121,6 +123,15 @@ def lib():
         L.mpq_kv_attention_workspace_bytes.restype = sz
         L.mpq_kv_attention_workspace_bytes.argtypes = [vp, vp, ci, ci]
         L.mpq_kv_attention.argtypes = [vp, vp, ci, vp, i64, i64, ci, C.c_float, ci, i64, vp, i64, i64, vp, sz, vp]
+        L.mpq_linear_groups.argtypes = [vp, ci, i64, i64, i64, i64, vp, ci, vp, ci, ci, ci, vp, vp]
+        L.mpq_rotate_heads.argtypes = [ci, i64, ci, vp, i64, i64, ci, vp, i64, i64, ci, vp, vp, ci, ci, vp, vp, C.c_float, vp, i64, i64, vp,
+                                       i64, i64, vp]
+        L.mpq_kv_attention_tree_workspace_bytes.restype = sz
+        L.mpq_kv_attention_tree_workspace_bytes.argtypes = [vp, vp, ci, ci]
+        L.mpq_kv_attention_tree.argtypes = [vp, vp, ci, vp, i64, i64, ci, C.c_float, vp, ci, vp, i64, i64, vp, sz, vp]
+        L.mpq_token_logprobs_workspace_bytes.restype = sz
+        L.mpq_token_logprobs_workspace_bytes.argtypes = [i64, i64, ci, ci]
+        L.mpq_token_logprobs.argtypes = [vp, ci, i64, i64, i64, C.c_float, vp, vp, vp, ci, vp, vp, vp, sz, vp]
         L.mpq_rademacher.argtypes = [C.c_uint64, C.c_uint64, i64, i64, vp, vp]
         L.mpq_hutchinson_quad_workspace_bytes.argtypes = [i64, i64, i64]
         L.mpq_hutchinson_quad_workspace_bytes.restype = C.c_size_t
@@ -857,7 +868,7 @@ def _scratch(ws, nbytes, x):
 def _rows2d(x):
     """(rows, columns, elements between rows) of a 2-D tensor whose columns are contiguous."""
     shape, stride = x.shape, x.stride()
-    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1 and shape[0] > 0):
         raise ValueError("expected a 2-D tensor with contiguous rows")
     M, K = shape
     return M, K, stride[0] if M > 1 else K
@@ -1065,3 +1076,160 @@ def kv_attention(cache: KvCache, batch: KvBatch, q, causal=True, window=0, softm
                               cache.dim ** -0.5 if softmax_scale is None else float(softmax_scale), int(bool(causal)), int(window),
                               out.data_ptr(), o_ts, o_hs, wp, wn, stream), "mpq_kv_attention")
     return out
+
+
+# ---------------------------------------------------------------------------------------------
+# A step of drafted tokens: what it needs besides the calls above.
+ROTATE_HALVES, ROTATE_PAIRS = 0, 1
+
+
+def group_quant(w, group):
+    """Eq. 1 at 4 bits with a maximum per `group` neighbouring input channels of w, float32 [N, K]: (nibbles uint8 [N, K / 2],
+    steps float32 [N, K / group]), the weights of linear_groups."""
+    if w.dim() != 2 or group not in (32, 64, 128) or w.shape[1] % group:
+        raise ValueError("expected [N, K] with K a multiple of a group of 32, 64 or 128")
+    N, K = w.shape
+    parts = w.contiguous().view(N * (K // group), group)
+    absmax = calibrate_absmax(parts, PER_ROW)
+    _, _, packed = fake_quant(parts, absmax, 4, PER_ROW, want_y=False, want_packed4=True)
+    return packed.view(N, K // 2), scale_from_absmax(absmax, 4).view(N, K // group)
+
+
+def linear_groups(x, w_q, w_scale, act=ACT_NONE, dtype=None, y=None):
+    """A linear layer whose 4-bit weights have a step per group of input channels: x [M, K] (float32, bfloat16 or float16, rows
+    contiguous), w_q uint8 [N, K / 2], w_scale [N, K / group] of any of those types, group 32, 64 or 128.  Returns Y [M, N] of `dtype`
+    (x's where neither it nor y is given)."""
+    t = ty = _type(x.dtype)
+    M, K, stride = _rows2d(x)
+    stream = _here(x, w_q, w_scale, y)
+    shape, groups = w_q.shape, w_scale.shape
+    N = shape[0]
+    if len(shape) != 2 or shape[1] * 2 != K or not w_q.is_contiguous() or w_q.element_size() != 1:
+        raise ValueError("expected contiguous weight codes of shape [N, K / 2]")
+    if len(groups) != 2 or groups[0] != N or groups[1] == 0 or K % groups[1] or not w_scale.is_contiguous():
+        raise ValueError("expected contiguous weight steps of shape [N, K / group]")
+    if y is not None:
+        dtype = dtype or y.dtype
+        _dense(y, dtype, (M, N), "y")
+    if dtype is not None and dtype != x.dtype:
+        ty = _type(dtype)
+    if y is None:
+        y = x.new(M, N) if ty == t else x.new_empty((M, N), dtype=dtype)
+    _check(lib().mpq_linear_groups(x.data_ptr(), t, M, N, K, stride, w_q.data_ptr(), K // groups[1], w_scale.data_ptr(), _type(w_scale.dtype),
+                                   int(act), ty, y.data_ptr(), stream), "mpq_linear_groups")
+    return y
+
+
+def _heads(x, rows, dim, what):
+    """(heads, elements between rows, elements between heads) of a tensor [rows, heads, dim]."""
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or shape[0] != rows or shape[2] != dim or stride[2] != 1:
+        raise ValueError("%s: expected [%d, heads, %d] with contiguous channels" % (what, rows, dim))
+    return shape[1], stride[0], stride[1]
+
+
+def rotate_heads(q, k, positions, frequencies, q_weight=None, k_weight=None, eps=1e-6, layout=ROTATE_HALVES, q_out=None, k_out=None):
+    """A norm per head (where there is a weight, float32 [dim]) and the rotation by position of q and k, [rows, heads, dim] with any
+    strides of rows and heads; either may be None.  positions int32 [rows]; frequencies float32, one per rotated pair of channels.  Returns
+    (q_out, k_out), dense where not given; q_out may be q and k_out k (in place)."""
+    torch = _torch()
+    some = q if q is not None else k
+    if some is None or some.dim() != 3:
+        raise ValueError("expected q or k, [rows, heads, dim]")
+    rows, dim, dtype = some.shape[0], some.shape[2], some.dtype
+    t = _type(dtype)
+    stream = _here(q, k, positions, frequencies, q_weight, k_weight, q_out, k_out)
+    args, outs = [], []
+    for x, out, weight, what in ((q, q_out, q_weight, "q"), (k, k_out, k_weight, "k")):
+        if weight is not None:
+            _dense(weight, torch.float32, (dim,), what + "_weight")
+        if x is None:
+            if out is not None or weight is not None:
+                raise ValueError("%s_out and %s_weight go with %s" % (what, what, what))
+            args.append((None, 0, 0, 0, None, 0, 0, None))
+            outs.append(None)
+            continue
+        heads, ts, hs = _heads(x, rows, dim, what)
+        if out is None:
+            out = x.new(rows, heads, dim)
+        out_heads, o_ts, o_hs = _heads(out, rows, dim, what + "_out")
+        if x.dtype != dtype or out.dtype != dtype or out_heads != heads:
+            raise ValueError("q, k and their outputs have one type, an output its input's heads")
+        args.append((x.data_ptr(), ts, hs, heads, out.data_ptr(), o_ts, o_hs, None if weight is None else weight.data_ptr()))
+        outs.append(out)
+    pairs = 0 if frequencies is None else frequencies.numel()
+    if pairs:
+        _dense(frequencies, torch.float32, (pairs,), "frequencies")
+        _dense(positions, torch.int32, (rows,), "positions")
+    (qp, q_ts, q_hs, q_n, qo, qo_ts, qo_hs, qw), (kp, k_ts, k_hs, k_n, ko, ko_ts, ko_hs, kw) = args
+    _check(lib().mpq_rotate_heads(t, rows, dim, qp, q_ts, q_hs, q_n, kp, k_ts, k_hs, k_n, positions.data_ptr() if pairs else None,
+                                  frequencies.data_ptr() if pairs else None, pairs, int(layout), qw, kw, float(eps), qo, qo_ts, qo_hs, ko,
+                                  ko_ts, ko_hs, stream), "mpq_rotate_heads")
+    return tuple(outs)
+
+
+def tree_bits(parents):
+    """The bits that kv_attention_tree reads, of one sequence's drafted tokens (a host function): parents[i] is the drafted token that
+    token i continues, or -1 where it continues the sequence; a token comes behind its parent.  Returns int64 [tokens, words] on the
+    host; sequences' bits are laid one after the other (those of fewer words filled up with zeros)."""
+    seen = []
+    for i, p in enumerate(parents):
+        if not -1 <= p < i:
+            raise ValueError("token %d continues %d, which does not come before it" % (i, p))
+        seen.append(1 << i | (seen[p] if p >= 0 else 0))
+    words = max(1, (len(seen) + 63) // 64)
+    signed = lambda w: w - (w >> 63 << 64)  # noqa: E731
+    return _torch().tensor([[signed(b >> 64 * w & (1 << 64) - 1) for w in range(words)] for b in seen], dtype=_torch().int64).view(-1, words)
+
+
+def kv_attention_tree_workspace_bytes(cache: KvCache, batch: KvBatch, dtype, q_heads) -> int:
+    return int(lib().mpq_kv_attention_tree_workspace_bytes(cache.ref, batch.ref, _type(dtype), q_heads))
+
+
+def kv_attention_tree(cache: KvCache, batch: KvBatch, q, tree, softmax_scale=None, out=None, ws: Workspace = None):
+    """kv_attention for rows that are drafted tokens: a row sees every token before its sequence's rows, and of those rows the ones
+    whose bits are set in tree, int64 [rows, words] on the device (tree_bits makes them).  Other arguments and the result as
+    kv_attention."""
+    t, q_ts, q_hs, heads = _kv_rows(cache, batch, q, None, "q")
+    stream = _here(q, tree)
+    if tree.dim() != 2:
+        raise ValueError("tree: expected [rows, words]")
+    _dense(tree, _torch().int64, (batch.rows, tree.shape[1]), "tree")
+    if out is None:
+        out = q.new(batch.rows, heads, cache.dim)
+        o_ts, o_hs = heads * cache.dim, cache.dim
+    else:
+        to, o_ts, o_hs, _ = _kv_rows(cache, batch, out, heads, "out")
+        if to != t:
+            raise ValueError("q and out have one type")
+    c = lib()
+    wp, wn, _alive = _scratch(ws, c.mpq_kv_attention_tree_workspace_bytes(cache.ref, batch.ref, t, heads), q)
+    _check(c.mpq_kv_attention_tree(cache.ref, batch.ref, t, q.data_ptr(), q_ts, q_hs, heads,
+                                   cache.dim ** -0.5 if softmax_scale is None else float(softmax_scale), tree.data_ptr(), tree.shape[1],
+                                   out.data_ptr(), o_ts, o_hs, wp, wn, stream), "mpq_kv_attention_tree")
+    return out
+
+
+def token_logprobs_workspace_bytes(rows, vocab, dtype, top=0) -> int:
+    return int(lib().mpq_token_logprobs_workspace_bytes(rows, vocab, _type(dtype), top))
+
+
+def token_logprobs(logits, tokens=None, top=0, scale=1.0, want_entropy=True, ws: Workspace = None):
+    """Of each row of logits [rows, vocab] (float32, bfloat16 or float16, rows contiguous) under softmax(scale * logits): the log probability
+    of tokens (int32 [rows]), the entropy, and the log probabilities and indices of the `top` (up to 32) most probable tokens.  Returns
+    (logprob float32 [rows] | None, entropy float32 [rows] | None, top_logprob float32 [rows, top] | None, top_index int32 [rows, top]
+    | None)."""
+    torch = _torch()
+    t = _type(logits.dtype)
+    rows, vocab, stride = _rows2d(logits)
+    stream = _here(logits, tokens)
+    if tokens is not None:
+        _dense(tokens, torch.int32, (rows,), "tokens")
+    new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=logits.device)  # noqa: E731
+    logprob, entropy = None if tokens is None else new(rows), new(rows) if want_entropy else None
+    best, index = (new(rows, top), torch.empty((rows, top), dtype=torch.int32, device=logits.device)) if top > 0 else (None, None)
+    c = lib()
+    wp, wn, _alive = _scratch(ws, c.mpq_token_logprobs_workspace_bytes(rows, vocab, t, int(top)), logits)
+    _check(c.mpq_token_logprobs(logits.data_ptr(), t, rows, vocab, stride, float(scale), _ptr(tokens), _ptr(logprob), _ptr(entropy),
+                                int(top), _ptr(best), _ptr(index), wp, wn, stream), "mpq_token_logprobs")
+    return logprob, entropy, best, index
