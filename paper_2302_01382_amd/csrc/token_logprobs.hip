@@ -1,7 +1,7 @@
 // token_logprobs.hip -- log probabilities of given tokens, entropy and the most probable alternatives, from one read of the logits.
 //
-// With m the row's largest logit, d = x - m, l = sum e^(scale d), w = sum scale d e^(scale d):
-//   log p_t = scale (x_t - m) - log l,   entropy = log l - w / l.
+// With m the row's largest logit, d = scale log2(e) (x - m), l = sum 2^d and w = sum d 2^d:
+//   ln p_t = scale (x_t - m) - ln l,   entropy = ln l - ln 2 w / l.
 // A workgroup holds a piece of a row in registers, so that the maximum is known before the first exponential and nothing is
 // rescaled in the loop.  The largest `top` of a piece: of the 64 maxima of what the four threads of a lane number hold, the
 // top-th largest is a bound that at least `top` values reach and few more do; those are listed, and a value's place in the order is
@@ -14,6 +14,8 @@ namespace mpq {
 constexpr int kMostTop = 32, kPieceThreads = 256, kListed = 1024, kJoinListed = 4096;
 constexpr int64_t kMostVocab = 1 << 22;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// 2^-200 is 0 in fp32: as the least exponent it leaves minus infinity a product of 0
+constexpr float kLeast = -200.0f;
 
 struct Piece {
   float m, l, w;
@@ -37,16 +39,18 @@ struct LogprobArgs {
 // a before b: the larger value, the lower index where they are equal
 __device__ __forceinline__ bool before(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
 
-// what a row's outputs are made of, but for the alternatives: by one thread
+__device__ __forceinline__ float at_least(float d) { return __builtin_elementwise_maximum(d, kLeast); }  // (a NaN stays one)
+
+// what a row's outputs are made of, but for the alternatives: by one thread; ln l
 template <int T>
 __device__ __forceinline__ float finish_row(const LogprobArgs& a, int64_t row, float m, float l, float w) {
-  const float log_l = logf(l);
-  if (a.entropy) a.entropy[row] = m == -__builtin_inff() ? __builtin_nanf("") : log_l - w / l;
+  const float log_l = m == -__builtin_inff() ? __builtin_nanf("") : logf(l);
+  if (a.entropy) a.entropy[row] = log_l - w / l * kLn2;
   if (a.logprob) {
     const int t = a.tokens[row];
-    float y = -__builtin_inff();
-    if (t >= 0 && t < a.vocab) y = (float)reinterpret_cast<const typename Elem<T>::type*>(a.logits)[row * a.stride + t];
-    a.logprob[row] = m == -__builtin_inff() ? __builtin_nanf("") : a.scale * (y - m) - log_l;
+    float x = -__builtin_inff();
+    if (t >= 0 && t < a.vocab) x = (float)reinterpret_cast<const typename Elem<T>::type*>(a.logits)[row * a.stride + t];
+    a.logprob[row] = __builtin_fmaf(a.scale, x - m, -log_l);
   }
   return log_l;
 }
@@ -71,24 +75,40 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
   if (row >= a.rows) return;
   const El* x = reinterpret_cast<const El*>(a.logits) + row * a.stride;
   const int vocab = (int)a.vocab, first = piece * (kPieceThreads * 8 * V);
-  float v[V][8];
+  float v[V][8], most[V];  // most: of each vector
+  if (first + kPieceThreads * 8 * V <= vocab) {  // uniform
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const f32x8 y = E::load8(x + first + (i * kPieceThreads + tid) * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = y[e];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int at = first + (i * kPieceThreads + tid) * 8;
+      f32x8 y;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = -__builtin_inff();
+      if (at + 8 <= vocab) {
+        y = E::load8(x + at);
+      } else if (at < vocab) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+          if (at + e < vocab) y[e] = (float)x[at + e];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = y[e];
+    }
+  }
   float mine = -__builtin_inff();
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int at = first + (i * kPieceThreads + tid) * 8;
-    if (at + 8 <= vocab) {
-      const f32x8 y = E::load8(x + at);
+    most[i] = v[i][0];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = y[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = at + e < vocab ? (float)x[at + e] : -__builtin_inff();
-    }
+    for (int e = 1; e < 8; ++e) most[i] = fmaxf(most[i], v[i][e]);
+    mine = fmaxf(mine, most[i]);
   }
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mine = fmaxf(mine, v[i][e]);
   lane_max[wave][lane] = mine;
   const float of_wave = wave_max(mine);
   if (lane == 0) sm_m[wave] = of_wave;
@@ -99,16 +119,15 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
   }
   __syncthreads();
   const float m = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
-  const float m_use = m == -__builtin_inff() ? 0.0f : m;
+  const float m_use = m == -__builtin_inff() ? 0.0f : m, c = a.scale * kLog2e;
   float l = 0.0f, w = 0.0f;
-  const float c = a.scale * kLog2e;  // d, and with it w, in units of log 2
 #pragma unroll
   for (int i = 0; i < V; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float d = (v[i][e] - m_use) * c, p = __builtin_amdgcn_exp2f(d);
+      const float d = at_least((v[i][e] - m_use) * c), p = __builtin_amdgcn_exp2f(d);
       l += p;
-      w = __builtin_fmaf(p, fmaxf(d, -__FLT_MAX__), w);  // (minus infinity has a p of 0; a NaN has one of NaN)
+      w = __builtin_fmaf(p, d, w);
     }
   l = wave_sum(l);
   w = wave_sum(w);
@@ -117,36 +136,39 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
     sm_w[wave] = w;
   }
   if (a.top > 0 && wave == 0) {
-    // the top-th largest of the 64 maxima: its bits from the highest down, of a key that orders like the value
+    // the top-th largest of the 64 maxima: its upper 16 bits from the highest down, of a key that orders like the value
     const float of_lane = fmaxf(fmaxf(lane_max[0][lane], lane_max[1][lane]), fmaxf(lane_max[2][lane], lane_max[3][lane]));
     const unsigned u = (unsigned)bits_from_f(of_lane), key = u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
     unsigned at_least = 0;
 #pragma unroll 1
-    for (unsigned bit = 0x80000000u; bit; bit >>= 1)
+    for (unsigned bit = 0x80000000u; bit > 0x8000u; bit >>= 1)
       if (__popcll(__ballot(key >= (at_least | bit))) >= a.top) at_least |= bit;
-    if (lane == 0) bound = f_from_bits((int)(at_least & 0x80000000u ? at_least ^ 0x80000000u : ~at_least));
+    // (at least the lowest number, so that minus infinity stays below it; keys below that one are of minus infinity or NaN)
+    if (lane == 0) bound = at_least & 0x80000000u ? f_from_bits((int)(at_least ^ 0x80000000u)) : at_least < 0x00800000u ? -__FLT_MAX__ : f_from_bits((int)~at_least);
   }
   __syncthreads();
   l = (sm_l[0] + sm_l[1]) + (sm_l[2] + sm_l[3]);
-  w = ((sm_w[0] + sm_w[1]) + (sm_w[2] + sm_w[3])) * kLn2;
+  w = (sm_w[0] + sm_w[1]) + (sm_w[2] + sm_w[3]);
   if (tid == 0) {
     if (a.pieces > 1) a.piece[b] = Piece{m, l, w};
     else sm_log = finish_row<T>(a, row, m, l, w);
   }
   if (a.top == 0) return;
   const float low = bound;
-  if (mine >= low && mine > -__builtin_inff()) {
+  if (mine >= low) {
 #pragma unroll
-    for (int i = 0; i < V; ++i)
+    for (int i = 0; i < V; ++i) {
+      if (!(most[i] >= low)) continue;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (v[i][e] >= low && v[i][e] > -__builtin_inff()) {
+        if (v[i][e] >= low) {
           const int k = atomicAdd(&count, 1);  // (any order: places go by value and index)
           if (k < kListed) {
             listed[k] = v[i][e];
             listed_at[k] = first + (i * kPieceThreads + tid) * 8 + e;
           }
         }
+    }
   }
   __syncthreads();
   const int n = count;
@@ -162,29 +184,28 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
       }
     }
   } else {
-    // one at a time: the first in order behind the last one taken
+    // one at a time, read again: the first in order behind the last one taken
+    const int end = first + kPieceThreads * 8 * V < vocab ? first + kPieceThreads * 8 * V : vocab;
     float last = __builtin_inff();
     int last_at = -1;
     for (int k = 0; k < a.top; ++k) {
       float y = -__builtin_inff();
       int at = 0x7FFFFFFF;
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int here = first + (i * kPieceThreads + tid) * 8 + e;
-          if (v[i][e] > -__builtin_inff() && before(last, last_at, v[i][e], here) && before(v[i][e], here, y, at)) {
-            y = v[i][e];
-            at = here;
-          }
+#pragma unroll 1
+      for (int here = first + tid; here < end; here += kPieceThreads) {
+        const float z = (float)x[here];
+        if (z >= low && before(last, last_at, z, here) && before(z, here, y, at)) {
+          y = z;
+          at = here;
         }
-      const float most = wave_max(y);
-      int low_at = y == most ? at : 0x7FFFFFFF;
+      }
+      const float top = wave_max(y);
+      int low_at = y == top ? at : 0x7FFFFFFF;
 #pragma unroll
       for (int s = 1; s < 64; s <<= 1) low_at = min(low_at, __shfl_xor(low_at, s, 64));
       __syncthreads();
       if (lane == 0) {
-        listed[wave] = most;
+        listed[wave] = top;
         listed_at[wave] = low_at;
       }
       __syncthreads();
@@ -210,7 +231,7 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
       a.best[b * a.top + tid] = out[tid];
       a.best_at[b * a.top + tid] = out_at[tid];
     } else {
-      a.top_logprob[row * a.top + tid] = out_at[tid] < 0 ? -__builtin_inff() : a.scale * (out[tid] - m_use) - sm_log;
+      a.top_logprob[row * a.top + tid] = out_at[tid] < 0 ? -__builtin_inff() : __builtin_fmaf(a.scale, out[tid] - m, -sm_log);
       a.top_index[row * a.top + tid] = out_at[tid];
     }
   }
@@ -227,17 +248,14 @@ __global__ __launch_bounds__(kWave) void token_logprobs_join_k(LogprobArgs a) {
   float m = -__builtin_inff();
   for (int i = lane; i < a.pieces; i += kWave) m = fmaxf(m, piece[i].m);
   m = wave_max(m);
-  const float m_use = m == -__builtin_inff() ? 0.0f : m;
+  const float m_use = m == -__builtin_inff() ? 0.0f : m, c = a.scale * kLog2e;
   float l = 0.0f, w = 0.0f;
   for (int i = lane; i < a.pieces; i += kWave) {
+    // 2^(d + d') = 2^d 2^d', and (d + d') 2^(d + d') likewise; a piece of nothing has l of 0, or of NaN
     const Piece p = piece[i];
-    if (p.m == -__builtin_inff()) {  // (sums of nothing; of a piece of NaN, NaN)
-      l += p.l;
-      continue;
-    }
-    const float d = fmaxf(a.scale * (p.m - m_use), -__FLT_MAX__), f = __builtin_amdgcn_exp2f(d * kLog2e);
-    l += p.l * f;
-    w += __builtin_fmaf(f * d, p.l, p.w * f);
+    const float d = at_least((p.m - m_use) * c), f = __builtin_amdgcn_exp2f(d);
+    l = __builtin_fmaf(p.l, f, l);
+    w = __builtin_fmaf(f, __builtin_fmaf(p.l, d, p.w), w);
   }
   l = wave_sum(l);
   w = wave_sum(w);
@@ -286,7 +304,7 @@ __global__ __launch_bounds__(kWave) void token_logprobs_join_k(LogprobArgs a) {
     for (int s = 1; s < 64; s <<= 1) low = min(low, __shfl_xor(low, s, 64));
     const bool any = low != 0x7FFFFFFF;
     if (lane == 0) {
-      a.top_logprob[row * a.top + k] = any ? a.scale * (most - m_use) - log_l : -__builtin_inff();
+      a.top_logprob[row * a.top + k] = any ? __builtin_fmaf(a.scale, most - m, -log_l) : -__builtin_inff();
       a.top_index[row * a.top + k] = any ? low : -1;
     }
     if (any && at == low) {  // (an index is in one piece)

@@ -19,6 +19,8 @@ def check(got, x, tokens, top, scale):
     the sum l by rel = 7 u spread + 115 u, spread = sum p |d|.  sum p |d| itself by u (7 bend + 120), relative, bend = sum p d^2 / spread.  So
       log p = d - log l: rel + 3 u |d| + 3 u |log l| + u;   entropy = log l + spread: rel (1 + spread) + spread u (7 bend + 123) + 3 u |log l|."""
     want, want_h, want_top, want_index, spread, bend = drafts.token_logprobs(x, tokens, top, scale)
+    with np.errstate(over="ignore"):
+        want, want_top = want.astype(np.float32).astype(np.float64), want_top.astype(np.float32).astype(np.float64)   # (u more)
     logprob, entropy, best, index = (host(t) for t in got)
     log_l = np.maximum(want_h - spread, 0)
     rel = U * (7 * spread + 115)
@@ -122,6 +124,25 @@ def test_large_values_and_scales():
         if size == 3e38:
             y = np.clip(y, -1.6e38, 1.6e38)      # (differences stay within the range)
         check(mpq.token_logprobs(dev(y), dev(tokens, "int32"), 4, scale), y, tokens, 4, scale)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", (700, 30000))
+def test_rows_of_the_lowest_value(dtype, vocab):
+    """Masks of the type's lowest value: behind them a row of nothing else is even, and one of a few others is those."""
+    import torch
+    r = rng(vocab)
+    low = torch.finfo(getattr(torch, dtype)).min
+    x = rows(r, 5, vocab, dtype)
+    x[0] = low
+    x[1, 5:] = low
+    x[2] = -low
+    x[3, ::2] = -INF
+    x[3, 1::2] = low
+    tokens = r.integers(0, vocab, 5).astype(np.int32)
+    for scale in (1.0, 0.5, 2.0):
+        # (with scale 2 an exponent of the lowest value passes the range: none of it is left, as in the reference)
+        check(mpq.token_logprobs(x, dev(tokens, "int32"), 7, scale), full(x), tokens, 7, scale)
 
 
 def test_strides_outputs_and_the_last_vocabulary():
