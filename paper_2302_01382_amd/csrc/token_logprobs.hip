@@ -11,11 +11,13 @@
 
 namespace mpq {
 
-constexpr int kMostTop = 32, kPieceThreads = 256, kListed = 1024, kJoinListed = 4096;
+constexpr int kMostTop = 32, kPieceThreads = 256, kListed = 1024;
 constexpr int64_t kMostVocab = 1 << 22;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // 2^-200 is 0 in fp32: as the least exponent it leaves minus infinity a product of 0
 constexpr float kLeast = -200.0f;
+
+typedef unsigned long long Key;
 
 struct Piece {
   float m, l, w;
@@ -32,12 +34,45 @@ struct LogprobArgs {
   int32_t* top_index;
   int pieces;
   Piece* piece;       // pieces > 1: [row][piece], then
-  float* best;        // [row][piece][top], and
-  int32_t* best_at;   // likewise: -1 where there is none
+  Key* best;          // [row][piece][top]
 };
 
-// a before b: the larger value, the lower index where they are equal
-__device__ __forceinline__ bool before(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
+// A logit and its index as a number that is the larger the earlier it comes: by value, the lower index first where they are equal (-0
+// and 0 are).  0 is none.
+__device__ __forceinline__ unsigned order_of(float x) {
+  const unsigned u = (unsigned)bits_from_f(x + 0.0f);
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(unsigned order) {
+  return f_from_bits((int)(order & 0x80000000u ? order ^ 0x80000000u : ~order));
+}
+__device__ __forceinline__ Key key_of(float x, int index) { return (Key)order_of(x) << 32 | (unsigned)~index; }
+__device__ __forceinline__ float value_of(Key k) { return value_of((unsigned)(k >> 32)); }
+__device__ __forceinline__ int index_of(Key k) { return (int)~(unsigned)k; }
+
+// An order that at least `top` of what 64 lanes hold reaches, from the lanes' largest: the upper half of the top-th largest, its bits from the
+// highest down; at least that of the lowest number, so that minus infinity and none stay below.
+__device__ __forceinline__ unsigned bound_of(unsigned largest, int top) {
+  unsigned least = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const unsigned with = least | 1u << bit;
+    least = __popcll(__ballot(largest >= with)) >= top ? with : least;
+  }
+  return max(least, 0x00800000u);
+}
+
+// The first `top` of n keys, in order, to out (those behind the last are 0): a key's place is the number of larger ones.  All threads;
+// keys are there and out is cleared already.
+__device__ __forceinline__ void place_keys(const Key* keys, int n, int top, Key* out) {
+  for (int k = threadIdx.x; k < n; k += kPieceThreads) {
+    const Key mine = keys[k];
+    int place = 0;
+#pragma unroll 8
+    for (int o = 0; o < n; ++o) place += keys[o] > mine;
+    if (place < top && mine) out[place] = mine;
+  }
+}
 
 __device__ __forceinline__ float at_least(float d) { return __builtin_elementwise_maximum(d, kLeast); }  // (a NaN stays one)
 
@@ -55,6 +90,11 @@ __device__ __forceinline__ float finish_row(const LogprobArgs& a, int64_t row, f
   return log_l;
 }
 
+__device__ __forceinline__ void store_top(const LogprobArgs& a, int64_t row, int i, Key k, float m, float log_l) {
+  a.top_logprob[row * a.top + i] = k ? __builtin_fmaf(a.scale, value_of(k) - m, -log_l) : -__builtin_inff();
+  a.top_index[row * a.top + i] = k ? index_of(k) : -1;
+}
+
 // V: vectors of eight values that a thread holds.  grid: row * pieces + piece
 template <int T, int V>
 __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a) {
@@ -63,12 +103,8 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
   constexpr int NW = kPieceThreads / kWave;
   __shared__ float sm_m[NW], sm_l[NW], sm_w[NW], sm_log;
   __shared__ float lane_max[NW][kWave];
-  __shared__ float bound;
   __shared__ int count;
-  __shared__ float listed[kListed];
-  __shared__ int listed_at[kListed];
-  __shared__ float out[kMostTop];
-  __shared__ int out_at[kMostTop];
+  __shared__ Key listed[kListed], out[kMostTop];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t b = block_index(), row = b / a.pieces;
   const int piece = (int)(b - row * a.pieces);
@@ -113,10 +149,7 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
   const float of_wave = wave_max(mine);
   if (lane == 0) sm_m[wave] = of_wave;
   if (tid == 0) count = 0;
-  if (tid < kMostTop) {
-    out[tid] = -__builtin_inff();
-    out_at[tid] = -1;
-  }
+  if (tid < kMostTop) out[tid] = 0;
   __syncthreads();
   const float m = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
   const float m_use = m == -__builtin_inff() ? 0.0f : m, c = a.scale * kLog2e;
@@ -135,183 +168,150 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
     sm_l[wave] = l;
     sm_w[wave] = w;
   }
-  if (a.top > 0 && wave == 0) {
-    // the top-th largest of the 64 maxima: its upper 16 bits from the highest down, of a key that orders like the value
-    const float of_lane = fmaxf(fmaxf(lane_max[0][lane], lane_max[1][lane]), fmaxf(lane_max[2][lane], lane_max[3][lane]));
-    const unsigned u = (unsigned)bits_from_f(of_lane), key = u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
-    unsigned at_least = 0;
-#pragma unroll 1
-    for (unsigned bit = 0x80000000u; bit > 0x8000u; bit >>= 1)
-      if (__popcll(__ballot(key >= (at_least | bit))) >= a.top) at_least |= bit;
-    // (at least the lowest number, so that minus infinity stays below it; keys below that one are of minus infinity or NaN)
-    if (lane == 0) bound = at_least & 0x80000000u ? f_from_bits((int)(at_least ^ 0x80000000u)) : at_least < 0x00800000u ? -__FLT_MAX__ : f_from_bits((int)~at_least);
+  float low = 0.0f;
+  if (a.top > 0) {
+    low = value_of(bound_of(order_of(fmaxf(fmaxf(lane_max[0][lane], lane_max[1][lane]), fmaxf(lane_max[2][lane], lane_max[3][lane]))), a.top));
+    if (mine >= low) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (!(most[i] >= low)) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (v[i][e] >= low) {
+            const int k = atomicAdd(&count, 1);  // (any order: places go by value and index)
+            if (k < kListed) listed[k] = key_of(v[i][e], first + (i * kPieceThreads + tid) * 8 + e);
+          }
+      }
+    }
   }
   __syncthreads();
-  l = (sm_l[0] + sm_l[1]) + (sm_l[2] + sm_l[3]);
-  w = (sm_w[0] + sm_w[1]) + (sm_w[2] + sm_w[3]);
   if (tid == 0) {
+    l = (sm_l[0] + sm_l[1]) + (sm_l[2] + sm_l[3]);
+    w = (sm_w[0] + sm_w[1]) + (sm_w[2] + sm_w[3]);
     if (a.pieces > 1) a.piece[b] = Piece{m, l, w};
     else sm_log = finish_row<T>(a, row, m, l, w);
   }
   if (a.top == 0) return;
-  const float low = bound;
-  if (mine >= low) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (!(most[i] >= low)) continue;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (v[i][e] >= low) {
-          const int k = atomicAdd(&count, 1);  // (any order: places go by value and index)
-          if (k < kListed) {
-            listed[k] = v[i][e];
-            listed_at[k] = first + (i * kPieceThreads + tid) * 8 + e;
-          }
-        }
-    }
-  }
-  __syncthreads();
   const int n = count;
   if (n <= kListed) {
-    for (int k = tid; k < n; k += kPieceThreads) {
-      const float y = listed[k];
-      const int at = listed_at[k];
-      int place = 0;
-      for (int o = 0; o < n; ++o) place += before(listed[o], listed_at[o], y, at);
-      if (place < a.top) {
-        out[place] = y;
-        out_at[place] = at;
-      }
-    }
+    place_keys(listed, n, a.top, out);
   } else {
-    // one at a time, read again: the first in order behind the last one taken
+    // too many share the bound: one at a time, read again, the largest key below the last one taken
     const int end = first + kPieceThreads * 8 * V < vocab ? first + kPieceThreads * 8 * V : vocab;
-    float last = __builtin_inff();
-    int last_at = -1;
+    Key last = ~(Key)0;
     for (int k = 0; k < a.top; ++k) {
-      float y = -__builtin_inff();
-      int at = 0x7FFFFFFF;
+      Key best = 0;
 #pragma unroll 1
       for (int here = first + tid; here < end; here += kPieceThreads) {
         const float z = (float)x[here];
-        if (z >= low && before(last, last_at, z, here) && before(z, here, y, at)) {
-          y = z;
-          at = here;
-        }
+        const Key key = z >= low ? key_of(z, here) : 0;
+        if (key < last && key > best) best = key;
       }
-      const float top = wave_max(y);
-      int low_at = y == top ? at : 0x7FFFFFFF;
 #pragma unroll
-      for (int s = 1; s < 64; s <<= 1) low_at = min(low_at, __shfl_xor(low_at, s, 64));
-      __syncthreads();
-      if (lane == 0) {
-        listed[wave] = top;
-        listed_at[wave] = low_at;
+      for (int s = 1; s < 64; s <<= 1) {
+        const Key other = __shfl_xor(best, s, 64);
+        best = other > best ? other : best;
       }
       __syncthreads();
-      y = listed[0];
-      at = listed_at[0];
+      if (lane == 0) listed[wave] = best;
+      __syncthreads();
+      last = listed[0];
 #pragma unroll
-      for (int o = 1; o < NW; ++o)
-        if (before(listed[o], listed_at[o], y, at)) {
-          y = listed[o];
-          at = listed_at[o];
-        }
-      last = y;
-      last_at = at;
-      if (tid == 0) {
-        out[k] = y;
-        out_at[k] = at;
-      }
+      for (int o = 1; o < NW; ++o) last = listed[o] > last ? listed[o] : last;
+      if (tid == 0) out[k] = last;
     }
   }
   __syncthreads();
   if (tid < a.top) {
-    if (a.pieces > 1) {
-      a.best[b * a.top + tid] = out[tid];
-      a.best_at[b * a.top + tid] = out_at[tid];
-    } else {
-      a.top_logprob[row * a.top + tid] = out_at[tid] < 0 ? -__builtin_inff() : __builtin_fmaf(a.scale, out[tid] - m, -sm_log);
-      a.top_index[row * a.top + tid] = out_at[tid];
-    }
+    if (a.pieces > 1) a.best[b * a.top + tid] = out[tid];
+    else store_top(a, row, tid, out[tid], m, sm_log);
   }
 }
 
-// Joins a row's pieces: a wave per row.  The pieces' lists are in order, so that the next alternative is the first of their heads.
+// Joins a row's pieces: a workgroup per row.  The alternatives are among the pieces' own, found as they were found in a piece.
 template <int T>
-__global__ __launch_bounds__(kWave) void token_logprobs_join_k(LogprobArgs a) {
-  extern __shared__ int lds[];  // of each piece, how many of its list were taken; the lists where they fit
-  const int lane = threadIdx.x;
+__global__ __launch_bounds__(kPieceThreads) void token_logprobs_join_k(LogprobArgs a) {
+  constexpr int NW = kPieceThreads / kWave;
+  __shared__ float sm_m[NW], sm_l[NW], sm_w[NW], sm_log;
+  __shared__ unsigned lane_max[NW][kWave];
+  __shared__ int count;
+  __shared__ Key listed[kListed], out[kMostTop];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = block_index();
   if (row >= a.rows) return;
   const Piece* piece = a.piece + row * a.pieces;
-  float m = -__builtin_inff();
-  for (int i = lane; i < a.pieces; i += kWave) m = fmaxf(m, piece[i].m);
+  const int entries = a.pieces * a.top;
+  const Key* best = a.best + row * entries;
+  const bool all = entries <= kPieceThreads;  // few enough to be listed as they are
+  Key first = tid < entries ? best[tid] : 0;
+  Piece p = tid < a.pieces ? piece[tid] : Piece{-__builtin_inff(), 0.0f, 0.0f};
+  float m = p.m;
+  unsigned mine = (unsigned)(first >> 32);
+  for (int i = tid + kPieceThreads; i < a.pieces; i += kPieceThreads) m = fmaxf(m, piece[i].m);
+  if (!all)
+    for (int i = tid + kPieceThreads; i < entries; i += kPieceThreads) mine = max(mine, (unsigned)(best[i] >> 32));
   m = wave_max(m);
+  if (lane == 0) sm_m[wave] = m;
+  lane_max[wave][lane] = mine;
+  if (tid == 0) count = 0;
+  if (tid < kMostTop) out[tid] = 0;
+  if (all) listed[tid] = first;
+  __syncthreads();
+  m = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
   const float m_use = m == -__builtin_inff() ? 0.0f : m, c = a.scale * kLog2e;
   float l = 0.0f, w = 0.0f;
-  for (int i = lane; i < a.pieces; i += kWave) {
+  for (int i = tid; i < a.pieces; i += kPieceThreads) {
     // 2^(d + d') = 2^d 2^d', and (d + d') 2^(d + d') likewise; a piece of nothing has l of 0, or of NaN
-    const Piece p = piece[i];
+    if (i != tid) p = piece[i];
     const float d = at_least((p.m - m_use) * c), f = __builtin_amdgcn_exp2f(d);
     l = __builtin_fmaf(p.l, f, l);
     w = __builtin_fmaf(f, __builtin_fmaf(p.l, d, p.w), w);
   }
   l = wave_sum(l);
   w = wave_sum(w);
-  float log_l = 0.0f;
-  if (lane == 0) log_l = finish_row<T>(a, row, m, l, w);
-  if (a.top == 0) return;
-  log_l = __shfl(log_l, 0, 64);
-  const int entries = a.pieces * a.top;
-  const float* best = a.best + row * entries;
-  const int32_t* best_at = a.best_at + row * entries;
-  int* head = lds;
-  for (int i = lane; i < a.pieces; i += kWave) head[i] = 0;
-  if (entries <= kJoinListed) {
-    int *to_at = lds + a.pieces, *to = to_at + entries;
-    for (int i = lane; i < entries; i += kWave) {
-      to[i] = bits_from_f(best[i]);
-      to_at[i] = best_at[i];
+  if (lane == 0) {
+    sm_l[wave] = l;
+    sm_w[wave] = w;
+  }
+  int n = entries;
+  if (!all) {
+    const unsigned low = bound_of(max(max(lane_max[0][lane], lane_max[1][lane]), max(lane_max[2][lane], lane_max[3][lane])), a.top);
+    for (int i = tid; i < entries; i += kPieceThreads) {
+      const Key k = best[i];
+      if ((unsigned)(k >> 32) < low) continue;
+      const int at = atomicAdd(&count, 1);
+      if (at < kListed) listed[at] = k;
     }
-    best = reinterpret_cast<float*>(to);
-    best_at = to_at;
   }
   __syncthreads();
-  // the first of the heads of the lane's pieces, looked for again only where it was taken
-  float y;
-  int at, of;
-  auto look = [&]() {
-    y = -__builtin_inff();
-    at = 0x7FFFFFFF;
-    for (int i = lane; i < a.pieces; i += kWave) {
-      const int h = head[i];
-      if (h >= a.top) continue;
-      const float z = best[i * a.top + h];
-      const int z_at = best_at[i * a.top + h];
-      if (z_at >= 0 && before(z, z_at, y, at)) {
-        y = z;
-        at = z_at;
-        of = i;
-      }
-    }
-  };
-  look();
-  for (int k = 0; k < a.top; ++k) {
-    const float most = wave_max(y);
-    int low = y == most ? at : 0x7FFFFFFF;
+  if (tid == 0) sm_log = finish_row<T>(a, row, m, (sm_l[0] + sm_l[1]) + (sm_l[2] + sm_l[3]), (sm_w[0] + sm_w[1]) + (sm_w[2] + sm_w[3]));
+  if (a.top == 0) return;
+  if (!all) n = count;
+  if (n <= kListed) {
+    place_keys(listed, n, a.top, out);
+  } else {
+    // too many share the bound: one at a time, the largest key below the last one taken
+    Key last = ~(Key)0;
+    for (int k = 0; k < a.top; ++k) {
+      Key most = 0;
+      for (int i = tid; i < entries; i += kPieceThreads)
+        if (best[i] < last && best[i] > most) most = best[i];
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) low = min(low, __shfl_xor(low, s, 64));
-    const bool any = low != 0x7FFFFFFF;
-    if (lane == 0) {
-      a.top_logprob[row * a.top + k] = any ? __builtin_fmaf(a.scale, most - m, -log_l) : -__builtin_inff();
-      a.top_index[row * a.top + k] = any ? low : -1;
-    }
-    if (any && at == low) {  // (an index is in one piece)
-      head[of] += 1;
-      look();
+      for (int s = 1; s < 64; s <<= 1) {
+        const Key other = __shfl_xor(most, s, 64);
+        most = other > most ? other : most;
+      }
+      __syncthreads();
+      if (lane == 0) listed[wave] = most;
+      __syncthreads();
+      last = listed[0];
+#pragma unroll
+      for (int o = 1; o < NW; ++o) last = listed[o] > last ? listed[o] : last;
+      if (tid == 0) out[k] = last;
     }
   }
+  __syncthreads();
+  if (tid < a.top) store_top(a, row, tid, out[tid], m, sm_log);
 }
 
 struct LogprobPlan {
@@ -339,8 +339,7 @@ static int launch_logprobs(const LogprobArgs& a, const LogprobPlan& p, hipStream
   else token_logprobs_k<T, 8><<<grid, kPieceThreads, 0, st>>>(a);
   const int rc = launch_status();
   if (rc != MPQ_OK || a.pieces == 1) return rc;
-  const int lists = a.pieces * a.top <= kJoinListed ? a.pieces * a.top : 0;
-  token_logprobs_join_k<T><<<wide_grid(a.rows, kWave), kWave, (a.pieces + 2 * lists) * sizeof(int), st>>>(a);
+  token_logprobs_join_k<T><<<wide_grid(a.rows, kPieceThreads), kPieceThreads, 0, st>>>(a);
   return launch_status();
 }
 
@@ -370,11 +369,10 @@ extern "C" int mpq_token_logprobs(const void* logits, int type, int64_t rows, in
   if (p.ws_bytes > 0 && (!ws || ws_bytes < p.ws_bytes)) return MPQ_ERR_WORKSPACE;
   if (p.ws_bytes > 0 && !aligned16(ws)) return MPQ_ERR_ALIGN;
   LogprobArgs a{logits, rows, vocab, row_stride, scale, tokens, logprob_out, entropy_out, top, top_logprob_out, top_index_out, p.pieces,
-                nullptr, nullptr, nullptr};
+                nullptr, nullptr};
   if (p.pieces > 1) {
-    a.piece = reinterpret_cast<Piece*>(ws);
-    a.best = reinterpret_cast<float*>(a.piece + rows * p.pieces);
-    a.best_at = reinterpret_cast<int32_t*>(a.best + rows * p.pieces * top);
+    a.best = reinterpret_cast<Key*>(ws);
+    a.piece = reinterpret_cast<Piece*>(a.best + rows * p.pieces * top);
   }
   hipStream_t st = (hipStream_t)stream;
   if (type == MPQ_F32) return launch_logprobs<MPQ_F32>(a, p, st);

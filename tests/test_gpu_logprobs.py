@@ -77,6 +77,14 @@ def test_equal_logits(n, vocab):
         check(mpq.token_logprobs(dev(x), dev(tokens, "int32"), 32), x, tokens, 32, 1.0)
 
 
+def test_equal_logits_of_many_pieces():
+    """More equal alternatives than the join lists at once."""
+    x = np.zeros((1, 2 ** 21 + 9), np.float32)
+    x[0, 12345] = 1.0
+    tokens = np.array([2 ** 21], np.int32)
+    check(mpq.token_logprobs(dev(x), dev(tokens, "int32"), 32), x, tokens, 32, 1.0)
+
+
 @pytest.mark.parametrize("n,vocab", [(3, 500), (1, 40000), (530, 9000)])
 def test_tokens_that_are_ruled_out(n, vocab):
     r = rng(vocab)
