@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_join_k(LogprobAr
   const Piece* piece = a.piece + row * a.pieces;
   const int entries = a.pieces * a.top;
   const Key* best = a.best + row * entries;
-  const bool all = entries <= kPieceThreads;  // few enough to be listed as they are
+  const bool all = entries <= kWave;  // few enough to be listed as they are (32 x 8 of them 10.3 us with, 8 without a bound)
   Key first = tid < entries ? best[tid] : 0;
   Piece p = tid < a.pieces ? piece[tid] : Piece{-__builtin_inff(), 0.0f, 0.0f};
   float m = p.m;
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_join_k(LogprobAr
   lane_max[wave][lane] = mine;
   if (tid == 0) count = 0;
   if (tid < kMostTop) out[tid] = 0;
-  if (all) listed[tid] = first;
+  if (all && tid < kWave) listed[tid] = first;
   __syncthreads();
   m = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
   const float m_use = m == -__builtin_inff() ? 0.0f : m, c = a.scale * kLog2e;
@@ -321,8 +321,13 @@ struct LogprobPlan {
 static int plan_logprobs(int64_t rows, int64_t vocab, int type, int top, LogprobPlan& p) {
   if (!known_type(type) || rows < 0 || vocab <= 0 || vocab > kMostVocab || top < 0 || top > kMostTop) return MPQ_ERR_SHAPE;
   auto pieces = [&](int vectors) { return (vocab + kPieceThreads * 8 * vectors - 1) / (kPieceThreads * 8 * vectors); };
-  p.vectors = 8;
-  while (p.vectors > 1 && (rows * pieces(p.vectors) < 2 * kNumCU || pieces(p.vectors / 2) == 1)) p.vectors /= 2;
+  // One piece, the smallest that takes the row, spares the join's launch (us on the device, one piece | several; the host saves 4 more: 1 x
+  // 10000 6.1 | 6.6, 100 x 16000 fp32 7.0 | 9.1, 4000 x 10000 fp32 35 | 40).  Else eight vectors a thread where that makes many rounds of the
+  // chip, so that loads overlap with other workgroups' arithmetic, else fewer (2 | 4 | 8 vectors: 2500 x 65536 bf16 92 | 75 | 71, 190 x 100003
+  // fp32 24.2 | 23.1 | 24.0, 256 x 32768 12.8 | 12.6 | 12.8, 16 x 50000 fp32 8.0 | 8.7 | 9.4, 1 x 131072 9.1 | 9.6 | 10.4).
+  p.vectors = 1;
+  while (p.vectors < 8 && pieces(p.vectors) > 1) p.vectors *= 2;
+  if (pieces(8) > 1) p.vectors = rows * pieces(8) >= 8 * kNumCU ? 8 : rows * pieces(4) >= 4 * kNumCU ? 4 : 2;
   p.pieces = (int)pieces(p.vectors);
   if (mul_overflows(rows, (int64_t)p.pieces * (kMostTop + 4))) return MPQ_ERR_SHAPE;
   p.ws_bytes = p.pieces > 1 ? (size_t)rows * p.pieces * (sizeof(Piece) + (size_t)top * 8) : 0;
