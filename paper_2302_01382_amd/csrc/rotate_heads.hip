@@ -23,6 +23,22 @@ struct RotateArgs {
   float eps;
 };
 
+// sum over each aligned group of LPH lanes
+template <int LPH>
+__device__ __forceinline__ float head_sum(float v) {
+  v += dpp<kQuadSwap1>(v);
+  if (LPH >= 4) v += dpp<kQuadSwap2>(v);
+  if (LPH >= 8) v += dpp<kRowHalfMirror>(v);
+  if (LPH >= 16) v += dpp<kRowMirror>(v);
+  if (LPH == 32) v += __shfl_xor(v, 16, 64);
+  return v;
+}
+
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)v), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
 // LPH: lanes of a head, dim / 8 rounded up to a power of two.  NEIGHBOURS: pairs are channels 2 j and 2 j + 1.
 template <int T, int LPH, bool NEIGHBOURS>
 __global__ __launch_bounds__(kBlock) void rotate_heads_k(RotateArgs a) {
@@ -31,78 +47,88 @@ __global__ __launch_bounds__(kBlock) void rotate_heads_k(RotateArgs a) {
   constexpr int HPW = kWave / LPH;
   const int lane = threadIdx.x & 63, u = lane % LPH;
   const int64_t wave = block_index() * (kBlock / kWave) + (threadIdx.x >> 6);
-  const int64_t row = wave / a.per_row;
+  const int64_t row = uniform(wave / a.per_row);
   if (row >= a.rows) return;  // uniform over the wave
   const bool real = u < a.dim / 8, turns = u < a.pairs / 4;
   // the lane's channels: four from `first` on and four from `second` on
-  const int first = NEIGHBOURS || !turns ? 8 * u : 4 * u, second = NEIGHBOURS || !turns ? first + 4 : first + a.pairs;
-  float c[4], s[4];
+  const bool together = NEIGHBOURS || !turns;
+  const int first = together ? 8 * u : 4 * u, second = together ? first + 4 : first + a.pairs;
+  // groups of HPW heads, q's before k's: which a group is of, and where it lies, is the same for the whole wave
+  const int of_q = (a.heads[0] + HPW - 1) / HPW, groups = of_q + (a.heads[1] + HPW - 1) / HPW;
+  const int g0 = __builtin_amdgcn_readfirstlane((int)(wave - row * a.per_row)) * a.run, g1 = g0 + a.run < groups ? g0 + a.run : groups;
+  const int sub = lane / LPH;
+  auto load = [&](int g) {
+    const int which = g < of_q ? 0 : 1, head = (which ? g - of_q : g) * HPW;
+    f32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (real && head + sub < a.heads[which]) {
+      const El* from = reinterpret_cast<const El*>(a.in[which]) + row * a.in_ts[which] + head * a.in_hs[which] + sub * a.in_hs[which];
+      if (NEIGHBOURS) v = E::load8(from + first);
+      else v = __builtin_shufflevector(E::load4(from + first), E::load4(from + second), 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    return v;
+  };
+  f32x8 next = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (g0 < g1) next = load(g0);
+  f32x8 weight[2];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    c[j] = 1.0f;
-    s[j] = 0.0f;
-  }
-  if (turns) {
+  for (int i = 0; i < 2; ++i)
+    if (a.weight[i] && real)
+      weight[i] = __builtin_shufflevector(Elem<MPQ_F32>::load4(a.weight[i] + first), Elem<MPQ_F32>::load4(a.weight[i] + second), 0, 1, 2, 3, 4, 5, 6, 7);
+  // a cosine and a sine of every pair, made by one lane each (two where there are more than 64), and handed to the lanes that turn the pair
+  float c[4], s[4];
+  if (a.pairs > 0) {
+    constexpr int EACH = LPH > 16 ? 2 : 1;
     const double position = (double)a.positions[row] * 0.15915494309189535;  // 1 / (2 pi)
+    float cs[EACH], sn[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int j = lane + 64 * i;
+      const double t = j < a.pairs ? position * (double)a.frequencies[j] : 0.0;
+      sincospif(2.0f * (float)(t - __builtin_rint(t)), &sn[i], &cs[i]);
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const double t = position * (double)a.frequencies[4 * u + j];
-      sincospif(2.0f * (float)(t - __builtin_rint(t)), &s[j], &c[j]);
+      const int from = 4 * u + j;
+      c[j] = __shfl(cs[0], from & 63, 64);
+      s[j] = __shfl(sn[0], from & 63, 64);
+      if (EACH == 2) {
+        const float c1 = __shfl(cs[EACH - 1], from & 63, 64), s1 = __shfl(sn[EACH - 1], from & 63, 64);
+        c[j] = from < 64 ? c[j] : c1;
+        s[j] = from < 64 ? s[j] : s1;
+      }
     }
   }
-  const int heads = a.heads[0] + a.heads[1];
   const float one_of = 1.0f / (float)a.dim;
-  int h = (int)(wave - row * a.per_row) * a.run * HPW + lane / LPH;
-  for (int g = 0; g < a.run; ++g, h += HPW) {
-    const int which = h < a.heads[0] ? 0 : 1;
-    const int64_t head = h - (which ? a.heads[0] : 0);
-    const bool mine = real && h < heads;
-    f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-    if (mine) {
-      const El* from = reinterpret_cast<const El*>(a.in[which]) + row * a.in_ts[which] + head * a.in_hs[which];
-      x = E::load4(from + first);
-      y = E::load4(from + second);
-    }
-    const float* weight = a.weight[which];
-    float sum = 0.0f;
+  for (int g = g0; g < g1; ++g) {
+    const int which = g < of_q ? 0 : 1, head = (which ? g - of_q : g) * HPW;
+    f32x8 x = next;
+    if (g + 1 < g1) next = load(g + 1);
+    if (a.weight[which]) {
+      float sum = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(x[e], x[e], __builtin_fmaf(y[e], y[e], sum));
-#pragma unroll
-    for (int m = 1; m < LPH; m <<= 1) sum += __shfl_xor(sum, m, 64);
-    if (!mine) continue;
-    if (weight) {
-      const float mean = __builtin_fmaf(sum, one_of, a.eps);
+      for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
+      const float mean = __builtin_fmaf(head_sum<LPH>(sum), one_of, a.eps);
       float r = __builtin_amdgcn_rsqf(mean);  // (to one step; the line below to about half of one)
       r = __builtin_fmaf(0.5f * r, __builtin_fmaf(-mean * r, r, 1.0f), r);
-      x = x * r * Elem<MPQ_F32>::load4(weight + first);
-      y = y * r * Elem<MPQ_F32>::load4(weight + second);
+      x = x * r * (which ? weight[1] : weight[0]);
     }
     if (turns) {
-      f32x4 p, q;
-      if (NEIGHBOURS) {
-        p = f32x4{x[0], x[2], y[0], y[2]};
-        q = f32x4{x[1], x[3], y[1], y[3]};
-      } else {
-        p = x;
-        q = y;
-      }
-      f32x4 v, w;
+      constexpr int STEP = NEIGHBOURS ? 2 : 1, OTHER = NEIGHBOURS ? 1 : 4;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = __builtin_fmaf(p[e], c[e], -(q[e] * s[e]));
-        w[e] = __builtin_fmaf(q[e], c[e], p[e] * s[e]);
-      }
-      if (NEIGHBOURS) {
-        x = f32x4{v[0], w[0], v[1], w[1]};
-        y = f32x4{v[2], w[2], v[3], w[3]};
-      } else {
-        x = v;
-        y = w;
+      for (int j = 0; j < 4; ++j) {
+        const float p = x[STEP * j], q = x[STEP * j + OTHER];
+        x[STEP * j] = __builtin_fmaf(p, c[j], -(q * s[j]));
+        x[STEP * j + OTHER] = __builtin_fmaf(q, c[j], p * s[j]);
       }
     }
-    El* to = reinterpret_cast<El*>(a.out[which]) + row * a.out_ts[which] + head * a.out_hs[which];
-    E::store4(to + first, x);
-    E::store4(to + second, y);
+    if (!real || head + sub >= a.heads[which]) continue;
+    El* to = reinterpret_cast<El*>(a.out[which]) + row * a.out_ts[which] + head * a.out_hs[which] + sub * a.out_hs[which];
+    if (NEIGHBOURS) {
+      E::store8(to + first, x);
+    } else {
+      E::store4(to + first, __builtin_shufflevector(x, x, 0, 1, 2, 3));
+      E::store4(to + second, __builtin_shufflevector(x, x, 4, 5, 6, 7));
+    }
   }
 }
 
@@ -117,9 +143,11 @@ static int launch(RotateArgs& a, int layout, hipStream_t st) {
   const int units = a.dim / 8;
   int lanes = 2;
   while (lanes < units) lanes *= 2;
-  const int per_wave = kWave / lanes, groups = (a.heads[0] + a.heads[1] + per_wave - 1) / per_wave;
+  const int per_wave = kWave / lanes, groups = (a.heads[0] + per_wave - 1) / per_wave + (a.heads[1] + per_wave - 1) / per_wave;
+  // Groups to a wave: all of a row's, which share its angles, halved while there are not four waves to a SIMD (us, two | four | eight | sixteen
+  // to a SIMD: 997 x 40 x 128 bf16 8.5 | 8.0 | 8.8 | 8.8, 4000 x 24 x 64 fp32 13.2 | 12.4 | 13.4 | 13.4, 12289 x 40 x 128 fp16 55 | 56 | 56 | 54).
   a.run = groups;
-  while (a.run > 1 && a.rows * ((groups + a.run - 1) / a.run) < 4 * 2 * kNumCU) a.run = (a.run + 1) / 2;
+  while (a.run > 1 && a.rows * ((groups + a.run - 1) / a.run) < 16 * kNumCU) a.run = (a.run + 1) / 2;
   a.per_row = (groups + a.run - 1) / a.run;
   const dim3 grid = wide_grid((a.rows * a.per_row + 3) / 4, kBlock);
   switch (lanes) {
@@ -166,7 +194,7 @@ extern "C" int mpq_rotate_heads(int type, int64_t rows, int dim, const void* q, 
   if (pairs > 0 && (!positions || !frequencies)) return MPQ_ERR_NULL;
   for (int i = 0; i < 2; ++i)
     if (a.heads[i] > 0 && (!a.in[i] || !a.out[i])) return MPQ_ERR_NULL;
-  if (blocks_z(rows * (((int64_t)q_heads + k_heads + 1) / 2), kBlock) > 65535u) return MPQ_ERR_SHAPE;
+  if (blocks_z(rows * ((int64_t)q_heads + k_heads), kBlock) > 65535u) return MPQ_ERR_SHAPE;
   hipStream_t st = (hipStream_t)stream;
   if (type == MPQ_F32) return launch<MPQ_F32>(a, layout, st);
   if (type == MPQ_BF16) return launch<MPQ_BF16>(a, layout, st);
