@@ -1,19 +1,23 @@
 // linear_groups.hip -- a linear layer of few rows whose 4-bit weights have a step per group of 32, 64 or 128 input channels.
 //
-// y[m][n] = act(sum_g s[n][g] sum_{k in g} c[n][k] x[m][k]).  The weights are read once and meet at most 64 rows, so that their bytes
-// bound it.  No LDS tiles: a lane loads 16 bytes, 32 codes, of a weight row; the waves of a workgroup deal out k in steps of 256 (a
-// whole cache line of a weight row) and their sums meet in LDS, in a fixed order.
+// y[m][n] = act(sum_g s[n][g] sum_{k in g} c[n][k] x[m][k]).  The weights are read once and meet at most 64 rows at a time, so that their bytes
+// bound it while there are few rows (1 x 4096 x 12288, fp16 steps: 26 MB in 8.4 us, of which a launch takes 2.6; a kernel that only reads
+// so many in the same way takes 5.3), and with many the rows, which every workgroup reads out of the L2 (61 x 4096 x 11008, groups of
+// 32: 21.6 us for 230 workgroups' 115 MB of x and 27 MB of weights).
+// A lane loads 16 bytes, 32 codes, of a weight row; the waves of a workgroup take an eighth of k each and their sums meet in LDS, in a
+// fixed order.
 //
 // The product runs on v_mfma_f32_16x16x32 in the rows' own 16-bit type (rows x times codes): bf16 and fp16 hold x and codes exactly.
 // fp32 rows go in as three bf16 terms, 24 bits.  Both types take a code's four bits as they are: u = code + 8 in the mantissa of 16,
-// which makes 16 + u = code + 24, one shift and one three-operand logic instruction for two codes.  The 24 comes off again in the same sums: they
-// start from -24 times the sum of the group's x, a matrix step with a constant operand that all channels share.  A sum's rounding is that
-// of terms up to 24 / 4 times as large as without it, 2^-21 of them.
+// which makes 16 + u = code + 24, one shift and one three-operand logic instruction for two codes.  The 24 comes off again in the same sums:
+// -24 times the sum of the group's x is a matrix step with a constant operand, which all channels share.  A sum's rounding is that of terms up to
+// 24 / 4 times as large as without it, 2^-21 of them.
 //
 // A group's sum has to hold that group alone, and a matrix step adds up the k of four quarters of the wave.  A lane's 16 bytes are
-// 32 neighbouring codes: for groups of 128, whose four quarters are one group, operand c is dword c of every lane and x is read to
-// match; for 64 and 32 the quarters exchange their dwords, four swaps for four dwords, after which step c has 32 neighbouring k.
+// 32 neighbouring codes: the quarters exchange their dwords, four swaps for four dwords, after which dword c has 32 neighbouring k.
 #include "qgemm_dma.hpp"
+
+#include <type_traits>
 
 namespace mpq {
 
@@ -23,11 +27,11 @@ struct GroupsArgs {
   const uint8_t* w;
   const void* scale;
   int64_t M, N;
-  int K, act, y_type;
+  int K, scale_type, act, y_type;
   void* y;
 };
 
-constexpr int kGroupWaves = 8, kGroupThreads = kGroupWaves * 64, kGroupStep = 256;
+constexpr int kGroupWaves = 8, kGroupThreads = kGroupWaves * 64;
 
 template <int T>
 struct Operand {  // bf16, also for the terms of fp32
@@ -66,6 +70,27 @@ __device__ __forceinline__ v4i pair_up(v4i v) {
              (int)__builtin_amdgcn_perm((unsigned)v.w, (unsigned)v.y, 0x05040100u), (int)__builtin_amdgcn_perm((unsigned)v.w, (unsigned)v.y, 0x07060302u)};
 }
 
+// eight values of x as they are loaded, and as operands
+template <int T>
+struct Values {
+  typedef v4i type;
+  static __device__ __forceinline__ v4i load(const typename Elem<T>::type* p) { return *reinterpret_cast<const v4i_byte*>(p); }
+  static __device__ __forceinline__ void split(v4i v, v4i (&term)[1]) { term[0] = pair_up(v); }
+};
+template <>
+struct Values<MPQ_F32> {
+  typedef f32x8 type;
+  static __device__ __forceinline__ f32x8 load(const float* p) { return Elem<MPQ_F32>::load8(p); }
+  static __device__ __forceinline__ void split(f32x8 v, v4i (&term)[3]) {
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+      const bf16x8 top = __builtin_convertvector(v, bf16x8);
+      term[t] = pair_up(__builtin_bit_cast(v4i, top));
+      v -= __builtin_convertvector(top, f32x8);
+    }
+  }
+};
+
 // Dword d of quarter c becomes dword c of quarter d.
 __device__ __forceinline__ v4i exchange(v4i v) {
   const auto a = __builtin_amdgcn_permlane32_swap((unsigned)v.x, (unsigned)v.z, false, false);
@@ -75,25 +100,154 @@ __device__ __forceinline__ v4i exchange(v4i v) {
   return v4i{(int)c[0], (int)c[1], (int)d[0], (int)d[1]};
 }
 
-template <int S>
-__device__ __forceinline__ float step_at(const void* p, int64_t i) {
-  return (float)reinterpret_cast<const typename Elem<S>::type*>(p)[i];
+// COUNT neighbouring steps of 4 or 2 bytes, at any address that one may have
+template <bool WIDE, int COUNT>
+struct Steps {
+  typedef typename std::conditional<WIDE, float, unsigned short>::type El;
+  typedef El Raw __attribute__((ext_vector_type(COUNT)));
+  typedef El RawAny __attribute__((ext_vector_type(COUNT), aligned(sizeof(El))));
+  Raw v;
+  __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const RawAny*>(reinterpret_cast<const El*>(p) + at); }
+  // the second half takes the first one's place
+  __device__ __forceinline__ void turn() {
+#pragma unroll
+    for (int i = 0; i < COUNT / 2; ++i) v[i] = v[i + COUNT / 2];
+  }
+  // bf16: all bits set where the 2 bytes are one, else none (a choice in bits: at a branch the compiler would keep everything in registers)
+  __device__ __forceinline__ float get(int i, unsigned bf16) const {
+    if constexpr (WIDE) return v[i];
+    else return f_from_bits((int)(((unsigned)v[i] << 16 & bf16) | ((unsigned)bits_from_f((float)__builtin_bit_cast(_Float16, (unsigned short)v[i])) & ~bf16)));
+  }
+};
+
+// A row tile's sums of the waves, in a fixed order, to y: lane (channel, rows 4 q .. 4 q + 3).
+template <int NT>
+__device__ __forceinline__ void store_tile(const GroupsArgs& p, f32x4 (*red)[NT][64], const f32x4 (&total)[NT], int64_t m0, int rows, int64_t n0) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) red[wave][j][lane] = total[j];
+  __syncthreads();
+  for (int t = threadIdx.x; t < NT * 64; t += kGroupThreads) {
+    const int j = t >> 6, l = t & 63;
+    f32x4 sum = red[0][j][l];
+#pragma unroll
+    for (int v = 1; v < kGroupWaves; ++v) sum += red[v][j][l];
+    const int64_t n = n0 + j * 16 + (l & 15);
+    if (n >= p.N) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int m = 4 * (l >> 4) + e;
+      if (m >= rows) continue;
+      const float y = apply_act(sum[e], p.act);
+      const int64_t to = (m0 + m) * p.N + n;
+      if (p.y_type == MPQ_F32) reinterpret_cast<float*>(p.y)[to] = y;
+      else reinterpret_cast<unsigned short*>(p.y)[to] = to_half(y, p.y_type == MPQ_BF16);
+    }
+  }
 }
 
-// T: type of x, S: of the steps, G: group.  A workgroup takes NT x 16 output channels and MT x 16 rows.
-// grid: x channels, y blocks of rows
-template <int T, int S, int G, int MT, int NT>
-__global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p) {
+// What the two kernels share: the sums of 64 k, `half` of a step of 128, times their groups' steps to the totals.  `term` holds x of 32 k as
+// operands, of MT row tiles; from: -24 times the sums of its x.  Groups of 128 are summed over both halves.
+template <int T, int MT, int NT, int G>
+struct HalfSums {
   using O = Operand<T>;
-  using E = Elem<T>;
-  typedef typename E::type El;
-  constexpr int NW = kGroupWaves, TERMS = O::TERMS;
-  __shared__ f32x4 red[NW][NT][64];
+  static constexpr int PER = G / 32;
+  f32x4 from[MT], part[PER > 1 ? NT : 1][MT];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      from[i] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < (PER > 1 ? NT : 1); ++j) part[j][i] = f32x4{0, 0, 0, 0};
+    }
+  }
+  // c: 0 or 1, of the half
+  __device__ __forceinline__ void add32(const v4i (&term)[MT][O::TERMS], const unsigned (&w)[NT], int c) {
+    const v4i minus = {(int)O::MINUS, (int)O::MINUS, (int)O::MINUS, (int)O::MINUS};
+    const bool fresh = PER == 1 || (PER == 2 && c == 0);
+#pragma unroll
+    for (int t = 0; t < O::TERMS; ++t)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) from[i] = O::mfma(term[i][t], minus, fresh && t == 0 ? f32x4{0, 0, 0, 0} : from[i]);
+    if constexpr (PER > 1) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const v4i codes = codes_operand<T>(w[j]);
+#pragma unroll
+        for (int t = 0; t < O::TERMS; ++t)
+#pragma unroll
+          for (int i = 0; i < MT; ++i) part[j][i] = O::mfma(term[i][t], codes, fresh && t == 0 ? f32x4{0, 0, 0, 0} : part[j][i]);
+      }
+    }
+  }
+  // groups of 32: the product itself, from `from` on
+  __device__ __forceinline__ void product(const v4i (&term)[MT][O::TERMS], unsigned w) {
+    const v4i codes = codes_operand<T>(w);
+#pragma unroll
+    for (int t = 0; t < O::TERMS; ++t)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) part[0][i] = O::mfma(term[i][t], codes, t == 0 ? from[i] : part[0][i]);
+  }
+  __device__ __forceinline__ void scale(f32x4 (&total)[MT][NT], int j, float step) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        total[i][j][e] = __builtin_fmaf(PER > 1 ? part[PER > 1 ? j : 0][i][e] + from[i][e] : part[0][i][e], step, total[i][j][e]);
+  }
+  // term_of(c, term), dword c of a half's codes w[j][c], step_of(j, c): of tile j, of the group that ends with c; there: matrix steps of
+  // the half, 1 or 2; last: whether a group of 128 ends
+  template <typename TermOf, typename WOf, typename StepOf>
+  __device__ __forceinline__ void add(f32x4 (&total)[MT][NT], int there, bool last, TermOf&& term_of, WOf&& w_of, StepOf&& step_of) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      if (c >= there) break;  // uniform
+      __builtin_amdgcn_sched_barrier(0);  // (matrix steps stay apart: drawn into one another they would not fit the registers)
+      v4i term[MT][O::TERMS];
+      term_of(c, term);
+      unsigned w[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[j] = w_of(j, c);
+      add32(term, w, c);
+      if constexpr (PER == 1) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          product(term, w[j]);
+          scale(total, j, step_of(j, c));
+        }
+      }
+      if (PER == 2 && c == 1) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) scale(total, j, step_of(j, 0));
+      }
+    }
+    if (PER == 4 && last) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) scale(total, j, step_of(j, 0));
+      clear();
+    }
+  }
+};
+
+// T: type of x, WIDE: steps of 4 bytes, G: group.  A workgroup takes NT x 16 output channels and MT x 16 rows, each wave an eighth of k.
+// A wave's rows of x come 64 k at a time, whole cache lines, through registers into LDS of its own, from where a lane reads its row's operands:
+// read straight as operands, 16 rows of 64 bytes a time, a line came twice (64 x 4096 x 11008, groups of 128: 55 us with a channel tile to a
+// workgroup, 30 so, 20 with three).
+// grid: x channels, y blocks of rows
+template <int T, bool WIDE, int G, int MT, int NT>
+__global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p) {
+  typedef typename Elem<T>::type El;
+  constexpr int NW = kGroupWaves, TERMS = Operand<T>::TERMS, STEP = 128, OF_STEP = STEP / G;  // groups of a step
+  constexpr int CH = 64 * (int)sizeof(El) / 16;            // chunks of 16 bytes of a row and 64 k
+  constexpr int LOADS = MT * 16 * CH / 64;                 // a lane's
+  constexpr int STAGE = NW * MT * 16 * CH, RED = NW * NT * 64;
+  __shared__ v4i lds[STAGE > RED ? STAGE : RED];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int r = lane & 15, q = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * (16 * NT), m0 = (int64_t)blockIdx.y * (16 * MT);
   const int K = p.K, groups = K / G;
   const int rows = (int)(p.M - m0 < 16 * MT ? p.M - m0 : 16 * MT);
+  const unsigned bf16_steps = p.scale_type == MPQ_BF16 ? ~0u : 0u;
   // channels and rows past the edge re-read the last one; never stored
   const uint8_t* w_row[NT];
   int64_t s_row[NT];
@@ -103,133 +257,310 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
     w_row[j] = p.w + n * (K >> 1);
     s_row[j] = n * groups;
   }
-  const El* x_row[MT];
+  // the lane's loads of x: row and chunk
+  const El* x_row[LOADS];
+  v4i* own = lds + wave * (MT * 16 * CH);
+  int put[LOADS];
+  constexpr int EL = 16 / (int)sizeof(El);
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = i * 16 + r;
-    x_row[i] = reinterpret_cast<const El*>(p.x) + (m0 + (m < rows ? m : rows - 1)) * p.x_stride;
+  for (int i = 0; i < LOADS; ++i) {
+    const int row = (i * 64 + lane) / CH, chunk = lane % CH;
+    x_row[i] = reinterpret_cast<const El*>(p.x) + (m0 + (row < rows ? row : rows - 1)) * p.x_stride + chunk * EL;
+    put[i] = row * CH + (chunk ^ (row >> 1 & 7));  // (so that 16 rows' reads of one chunk fall into different banks)
   }
+  auto read = [&](int i, int chunk) {
+    const int row = i * 16 + r;
+    return own[row * CH + (chunk ^ (row >> 1 & 7))];
+  };
+
+  // Whole steps of the wave, neighbours.  What comes next is requested while this is multiplied, without a branch: behind one the compiler
+  // does not know what is in flight, and waits for everything.
+  const int whole = K / STEP, s0 = (int)((int64_t)whole * wave / NW), s1 = (int)((int64_t)whole * (wave + 1) / NW);
   f32x4 total[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) total[i][j] = f32x4{0, 0, 0, 0};
-
-  const int steps = (K + kGroupStep - 1) / kGroupStep;
-  constexpr int PER = G / 32;  // matrix steps of a group
-  const v4i minus = {(int)O::MINUS, (int)O::MINUS, (int)O::MINUS, (int)O::MINUS};
-  for (int s = wave; s < steps; s += NW) {
-    v4i w[NT][2];
+  v4i x[LOADS], w[NT], w_next[NT];
+  Steps<WIDE, OF_STEP> sc[NT], sc_next[NT];
+  HalfSums<T, MT, NT, G> sums;
+  sums.clear();
+  auto request_x = [&](int k) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      // a lane's 32 codes lie in the row or behind it, as a whole; those behind are not multiplied
-      const int k = s * kGroupStep + 128 * half + 32 * q, at = k < K ? k : K - 32;
+    for (int i = 0; i < LOADS; ++i) x[i] = *reinterpret_cast<const v4i_byte*>(x_row[i] + k);
+  };
+  auto stage = [&]() {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) w[j][half] = *reinterpret_cast<const v4i_byte*>(w_row[j] + (at >> 1));
+    for (int i = 0; i < LOADS; ++i) own[put[i]] = x[i];
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  auto term_of = [&](int c, v4i (&term)[MT][TERMS]) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int chunk = c * (CH / 2) + q * (CH / 8);
+      if constexpr (T == MPQ_F32) {
+        const f32x4 a = __builtin_bit_cast(f32x4, read(i, chunk)), b = __builtin_bit_cast(f32x4, read(i, chunk + 1));
+        Values<T>::split(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), term[i]);
+      } else {
+        Values<T>::split(read(i, chunk), term[i]);
+      }
     }
+  };
+  auto w_of = [&](int j, int c) { return (unsigned)w[j][c]; };
+  auto step_of = [&](int j, int c) { return sc[j].get(G == 32 ? c : 0, bf16_steps); };
+  // the other half's codes and steps take the first one's place
+  auto turn = [&]() {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int k1 = s * kGroupStep + 128 * half;
-      if (G < 128) {
+    for (int j = 0; j < NT; ++j) {
+      w[j] = v4i{w[j].z, w[j].w, 0, 0};
+      sc[j].turn();
+    }
+  };
+  if (s0 < s1) {
+    request_x(s0 * STEP);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) w[j][half] = exchange(w[j][half]);
+    for (int j = 0; j < NT; ++j) {
+      w[j] = *reinterpret_cast<const v4i_byte*>(w_row[j] + ((s0 * STEP + 32 * q) >> 1));
+      sc[j].load(p.scale, s_row[j] + s0 * OF_STEP);
+    }
+#pragma unroll 1
+    for (int s = s0; s < s1; ++s) {
+      const int then = s + 1 < s1 ? s + 1 : s;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        w[j] = exchange(w[j]);
+        w_next[j] = *reinterpret_cast<const v4i_byte*>(w_row[j] + ((then * STEP + 32 * q) >> 1));
+        sc_next[j].load(p.scale, s_row[j] + then * OF_STEP);
+      }
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        stage();
+        request_x(half == 0 ? s * STEP + 64 : then * STEP);
+        sums.add(total, 2, half == 1, term_of, w_of, step_of);
+        turn();
       }
 #pragma unroll
-      for (int c0 = 0; c0 < 4; c0 += PER) {
-        const int g = (k1 + 32 * c0) / G;
-        if (g >= groups) break;  // uniform
-        v4i x[PER][MT][TERMS];
-        f32x4 from[MT];  // -24 times the sum of the group's x
-#pragma unroll
-        for (int i = 0; i < MT; ++i) from[i] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int c = 0; c < PER; ++c) {
-          const El* chunk[MT];
-#pragma unroll
-          for (int i = 0; i < MT; ++i) chunk[i] = x_row[i] + k1 + (G < 128 ? 32 * (c0 + c) + 8 * q : 32 * q + 8 * c);
-#pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            if constexpr (T == MPQ_F32) {
-              f32x8 v = E::load8(chunk[i]);
-#pragma unroll
-              for (int t = 0; t < TERMS; ++t) {
-                const bf16x8 top = __builtin_convertvector(v, bf16x8);
-                x[c][i][t] = pair_up(__builtin_bit_cast(v4i, top));
-                v -= __builtin_convertvector(top, f32x8);
-              }
-            } else {
-              x[c][i][0] = pair_up(*reinterpret_cast<const v4i_byte*>(chunk[i]));
-            }
-#pragma unroll
-            for (int t = 0; t < TERMS; ++t) from[i] = O::mfma(x[c][i][t], minus, from[i]);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          f32x4 part[MT];
-#pragma unroll
-          for (int i = 0; i < MT; ++i) part[i] = from[i];
-#pragma unroll
-          for (int c = 0; c < PER; ++c) {
-            const v4i codes = codes_operand<T>((unsigned)w[j][half][c0 + c]);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-              for (int t = 0; t < TERMS; ++t) part[i] = O::mfma(x[c][i][t], codes, part[i]);
-          }
-          const float sw = step_at<S>(p.scale, s_row[j] + g);
-#pragma unroll
-          for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) total[i][j][e] = __builtin_fmaf(part[i][e], sw, total[i][j][e]);
-        }
+      for (int j = 0; j < NT; ++j) {
+        w[j] = w_next[j];
+        sc[j] = sc_next[j];
       }
     }
   }
-  // the waves' sums, a row tile at a time: lane (channel r, rows 4 q .. 4 q + 3)
+  if (G < 128 && whole * STEP < K && wave == NW - 1) {  // the rest of the row: one to three matrix steps
+    // a lane's 32 codes, and its chunk of x, lie in the row or behind it, as a whole; those behind are not multiplied
+    const int k = whole * STEP, there = (K - k) / 32, at = k + 32 * q;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      w[j] = exchange(*reinterpret_cast<const v4i_byte*>(w_row[j] + ((at < K ? at : K - 32) >> 1)));
+#pragma unroll
+      for (int g = 0; g < OF_STEP; ++g) {
+        Steps<WIDE, 1> one;
+        one.load(p.scale, s_row[j] + (whole * OF_STEP + g < groups ? whole * OF_STEP + g : groups - 1));
+        sc[j].v[g] = one.v[0];
+      }
+    }
+#pragma unroll 1
+    for (int half = 0; 2 * half < there; ++half) {
+      const int first = lane % CH * EL, here = k + 64 * half;
+      request_x(here + first < K ? here : K - EL - first);
+      stage();
+      sums.add(total, there - 2 * half, false, term_of, w_of, step_of);
+      turn();
+    }
+  }
+  __syncthreads();  // the waves' sums go where x was
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     if (i) __syncthreads();
-#pragma unroll
-    for (int j = 0; j < NT; ++j) red[wave][j][lane] = total[i][j];
-    __syncthreads();
-    for (int t = threadIdx.x; t < NT * 64; t += kGroupThreads) {
-      const int j = t >> 6, l = t & 63;
-      f32x4 sum = red[0][j][l];
-#pragma unroll
-      for (int v = 1; v < NW; ++v) sum += red[v][j][l];
-      const int64_t n = n0 + j * 16 + (l & 15);
-      if (n >= p.N) continue;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int m = i * 16 + 4 * (l >> 4) + e;
-        if (m >= rows) continue;
-        const float y = apply_act(sum[e], p.act);
-        const int64_t to = (m0 + m) * p.N + n;
-        if (p.y_type == MPQ_F32) reinterpret_cast<float*>(p.y)[to] = y;
-        else reinterpret_cast<unsigned short*>(p.y)[to] = to_half(y, p.y_type == MPQ_BF16);
-      }
-    }
+    store_tile<NT>(p, reinterpret_cast<f32x4(*)[NT][64]>(lds), total[i], m0 + 16 * i, rows - 16 * i, n0);
   }
 }
 
-template <int T, int S, int G>
+// Few rows: x as a whole in LDS, as operands, and the steps of the workgroup's channels, which lie together in memory, beside it.  Read
+// straight as operands, x would come with 16 times the loads that it is long, and steps in pieces of 2 bytes a line: a CU has a line from the L2 in
+// four clocks at best, and its lines bound it (1 x 4096 x 12288, fp16 steps, groups of 128: 12.2 us so).
+// Four units of 128 k of a wave are in flight, and once they have arrived the next four.  LDS: [row][k / 8][term], rows 64 bytes apart
+// modulo 256; [channel][group].
+constexpr int kUnits = 4, kFewRows = 8;
+__host__ __device__ inline int x_row_chunks(int K, int terms) {
+  const int n = K / 8 * terms;
+  return n + (4 - n % 16 + 16) % 16;
+}
+// steps from a channel to the next there: 16 bytes further where channels are whole pieces of 16, so that 16 of them fall into different banks
+__host__ __device__ inline int step_row_length(int groups, int step_size) { return groups * step_size % 16 ? groups : groups + 16 / step_size; }
+// bytes of LDS of a call: x, whose place the waves' sums take, and steps; the latter alone
+inline int few_steps_bytes(int64_t K, int group, int step_size) { return (16 * step_row_length((int)(K / group), step_size) * step_size + 15) / 16 * 16; }
+inline int64_t few_bytes(int64_t M, int64_t K, int terms, int group, int step_size) {
+  if (M > kFewRows || K > (1 << 16)) return 1 << 30;
+  const int64_t x = M * x_row_chunks((int)K, terms) * 16, red = kGroupWaves * 1024;
+  return (x > red ? x : red) + few_steps_bytes(K, group, step_size);
+}
+template <int T, bool WIDE, int G>
+__global__ __launch_bounds__(kGroupThreads) void linear_groups_few_k(GroupsArgs p, int x_bytes) {
+  constexpr int NT = 1;
+  typedef typename Elem<T>::type El;
+  typedef typename Steps<WIDE, 1>::El StepEl;
+  constexpr int NW = kGroupWaves, TERMS = Operand<T>::TERMS, UNIT = 128, OF_UNIT = UNIT / G;
+  extern __shared__ v4i few_lds[];
+  StepEl* steps = reinterpret_cast<StepEl*>(reinterpret_cast<char*>(few_lds) + x_bytes);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane((int)(tid >> 6));
+  const int r = lane & 15, q = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
+  const int K = p.K, groups = K / G, rows = (int)p.M, row_chunks = x_row_chunks(K, TERMS), per_row = K / 8, chunks = rows * per_row;
+  const unsigned bf16_steps = p.scale_type == MPQ_BF16 ? ~0u : 0u;
+  // this thread's first pieces of x and of the steps are requested before the weights, and stored behind their request
+  auto load_x = [&](int i, int& to) {
+    const int row = rows == 1 ? 0 : i / per_row, chunk = i - row * per_row;
+    to = row * row_chunks + chunk * TERMS;
+    return Values<T>::load(reinterpret_cast<const El*>(p.x) + row * p.x_stride + chunk * 8);
+  };
+  auto store_x = [&](typename Values<T>::type v, int to) {
+    v4i term[TERMS];
+    Values<T>::split(v, term);
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) few_lds[to + t] = term[t];
+  };
+  const int channels = (int)(p.N - n0 < 16 * NT ? p.N - n0 : 16 * NT);
+  const StepEl* step_from = reinterpret_cast<const StepEl*>(p.scale) + n0 * groups;
+  constexpr int SE = 16 / (int)sizeof(StepEl);
+  const int step_count = channels * groups, step_chunks = step_count / SE;
+  int x_to = 0;
+  typename Values<T>::type x_first = typename Values<T>::type{};
+  v4i s_first = {0, 0, 0, 0};
+  if (tid < chunks) x_first = load_x(tid, x_to);
+  if (tid < step_chunks) s_first = *reinterpret_cast<const v4i_byte*>(step_from + tid * SE);
+  // channels past the edge re-read the last one; never stored
+  const uint8_t* w_row[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) w_row[j] = p.w + (n0 + (j * 16 + r < channels ? j * 16 + r : channels - 1)) * (K >> 1) + 16 * q;
+  const int whole = K / UNIT, s0 = (int)((int64_t)whole * wave / NW), s1 = (int)((int64_t)whole * (wave + 1) / NW);
+  v4i w[kUnits][NT], w_next[kUnits][NT];
+  auto request = [&](v4i (&to)[kUnits][NT], int s) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int at = s + u < s1 ? s + u : s1 - 1;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) to[u][j] = *reinterpret_cast<const v4i_byte*>(w_row[j] + at * (UNIT / 2));
+    }
+  };
+  if (s0 < s1) request(w, s0);
+  if (tid < chunks) store_x(x_first, x_to);
+  const int row_length = step_row_length(groups, sizeof(StepEl));
+  auto store_steps = [&](v4i v, int i) {
+    if (row_length != groups) i += i / (groups / SE);
+    reinterpret_cast<v4i*>(steps)[i] = v;
+  };
+  if (tid < step_chunks) store_steps(s_first, tid);
+#pragma unroll 1
+  for (int i = tid + kGroupThreads; i < chunks; i += kGroupThreads) {
+    int to;
+    const auto v = load_x(i, to);
+    store_x(v, to);
+  }
+#pragma unroll 1
+  for (int i = tid + kGroupThreads; i < step_chunks; i += kGroupThreads) store_steps(*reinterpret_cast<const v4i_byte*>(step_from + i * SE), i);
+  if (tid < step_count - step_chunks * SE) steps[step_chunks * SE + tid] = step_from[step_chunks * SE + tid];
+  __syncthreads();
+  const v4i* x_row = few_lds + (r < rows ? r : 0) * row_chunks + q * TERMS;  // (rows past the edge: never stored)
+  f32x4 total[1][NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) total[0][j] = f32x4{0, 0, 0, 0};
+  HalfSums<T, 1, NT, G> sums;
+  sums.clear();
+  int step_row[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) step_row[j] = (j * 16 + r < channels ? j * 16 + r : channels - 1) * row_length;
+  auto unit = [&](v4i (&codes)[NT], int s, int there) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) codes[j] = exchange(codes[j]);
+    const v4i* x = x_row + s * (UNIT / 8) * TERMS;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (2 * half >= there) break;  // uniform
+      sums.add(total, there - 2 * half, half == 1, [&](int c, v4i (&term)[1][TERMS]) {
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) term[0][t] = x[(8 * half + 4 * c) * TERMS + t];
+      }, [&](int j, int c) { return (unsigned)codes[j][2 * half + c]; }, [&](int j, int c) {
+        Steps<WIDE, 1> one;
+        one.v[0] = steps[step_row[j] + s * OF_UNIT + (G == 32 ? 2 * half + c : G == 64 ? half : 0)];
+        return one.get(0, bf16_steps);
+      });
+    }
+  };
+  // (the last units apart, so that the loop needs no branch around its requests)
+  int s = s0;
+#pragma unroll 1
+  for (; s + kUnits < s1; s += kUnits) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(w[u][j]));  // here they have arrived: a wait further down would be one for the next as well
+    request(w_next, s + kUnits);
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) unit(w[u], s + u, 4);
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[u][j] = w_next[u][j];
+  }
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) {
+    if (s + u >= s1) break;  // uniform
+    unit(w[u], s + u, 4);
+  }
+  if (G < 128 && whole * UNIT < K && wave == NW - 1) {  // the rest of the row: one to three matrix steps
+    // a lane's 32 codes lie in the row or behind it, as a whole; those behind are not multiplied
+    const int at = whole * UNIT + 32 * q;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) w[0][j] = *reinterpret_cast<const v4i_byte*>(w_row[j] - 16 * q + ((at < K ? at : K - 32) >> 1));
+    unit(w[0], whole, (K - whole * UNIT) / 32);
+  }
+  __syncthreads();  // the waves' sums go where x was
+  store_tile<NT>(p, reinterpret_cast<f32x4(*)[NT][64]>(few_lds), total[0], 0, rows, n0);
+}
+
+// Channel tiles per workgroup: what makes the bytes that a CU loads smallest, its workgroups' weights and rows.
+static int channel_tiles(int mt, const GroupsArgs& p, int el) {
+  int best = 1;
+  double least = 0;
+  for (int nt = 1; nt <= 3; ++nt) {
+    const int64_t workgroups = (p.N + 16 * nt - 1) / (16 * nt), rounds = (workgroups * ((p.M + 16 * mt - 1) / (16 * mt)) + kNumCU - 1) / kNumCU;
+    const double bytes = (double)rounds * (nt * 16 * 0.5 + (p.M < 16 * mt ? p.M : 16 * mt) * el);
+    if (nt == 1 || bytes < least) { least = bytes; best = nt; }
+  }
+  return best;
+}
+
+template <int T, bool WIDE, int G, int MT>
 static int go(const GroupsArgs& p, hipStream_t st) {
-  const int64_t row_tiles = (p.M + 15) / 16;
-  const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)((p.M + 63) / 64));
-  if (row_tiles == 1) linear_groups_k<T, S, G, 1, 1><<<grid, kGroupThreads, 0, st>>>(p);
-  else if (row_tiles == 2) linear_groups_k<T, S, G, 2, 1><<<grid, kGroupThreads, 0, st>>>(p);
-  else linear_groups_k<T, S, G, 4, 1><<<grid, kGroupThreads, 0, st>>>(p);
+  const int nt = channel_tiles(MT, p, T == MPQ_F32 ? 4 : 2);
+  const dim3 grid((unsigned)((p.N + 16 * nt - 1) / (16 * nt)), (unsigned)((p.M + 16 * MT - 1) / (16 * MT)));
+  if (nt == 1) linear_groups_k<T, WIDE, G, MT, 1><<<grid, kGroupThreads, 0, st>>>(p);
+  else if (nt == 2) linear_groups_k<T, WIDE, G, MT, 2><<<grid, kGroupThreads, 0, st>>>(p);
+  else linear_groups_k<T, WIDE, G, MT, 3><<<grid, kGroupThreads, 0, st>>>(p);
   return launch_status();
 }
-template <int T, int S>
+template <int T, bool WIDE, int G>
+static int go_rows(const GroupsArgs& p, hipStream_t st) {
+  constexpr int TERMS = Operand<T>::TERMS, SIZE = WIDE ? 4 : 2;
+  const int64_t few = few_bytes(p.M, p.K, TERMS, G, SIZE);
+  if (few <= 65536) {
+    linear_groups_few_k<T, WIDE, G><<<(unsigned)((p.N + 15) / 16), kGroupThreads, (int)few, st>>>(p, (int)few - few_steps_bytes(p.K, G, SIZE));
+    return launch_status();
+  }
+  if (p.M <= 16) return go<T, WIDE, G, 1>(p, st);
+  if (p.M <= 32 || T == MPQ_F32) return go<T, WIDE, G, 2>(p, st);
+  return go<T, WIDE, G, T == MPQ_F32 ? 2 : 4>(p, st);
+}
+template <int T, bool WIDE>
 static int go_group(const GroupsArgs& p, int group, hipStream_t st) {
-  return group == 32 ? go<T, S, 32>(p, st) : group == 64 ? go<T, S, 64>(p, st) : go<T, S, 128>(p, st);
+  return group == 32 ? go_rows<T, WIDE, 32>(p, st) : group == 64 ? go_rows<T, WIDE, 64>(p, st) : go_rows<T, WIDE, 128>(p, st);
 }
 template <int T>
-static int go_type(const GroupsArgs& p, int group, int scale_type, hipStream_t st) {
-  if (scale_type == MPQ_F32) return go_group<T, MPQ_F32>(p, group, st);
-  return scale_type == MPQ_BF16 ? go_group<T, MPQ_BF16>(p, group, st) : go_group<T, MPQ_F16>(p, group, st);
+static int go_type(const GroupsArgs& p, int group, hipStream_t st) {
+  return p.scale_type == MPQ_F32 ? go_group<T, true>(p, group, st) : go_group<T, false>(p, group, st);
 }
 
 }  // namespace mpq
@@ -249,8 +580,8 @@ extern "C" int mpq_linear_groups(const void* x, int x_type, int64_t M, int64_t N
   if (reinterpret_cast<uintptr_t>(y_out) & (uintptr_t)(type_size(y_type) - 1)) return MPQ_ERR_ALIGN;
   if (M == 0) return MPQ_OK;
   if (!x || !w_q || !w_scale || !y_out) return MPQ_ERR_NULL;
-  const GroupsArgs p{x, x_stride, w_q, w_scale, M, N, (int)K, act, y_type, y_out};
+  const GroupsArgs p{x, x_stride, w_q, w_scale, M, N, (int)K, scale_type, act, y_type, y_out};
   hipStream_t st = (hipStream_t)stream;
-  if (x_type == MPQ_F32) return go_type<MPQ_F32>(p, group, scale_type, st);
-  return x_type == MPQ_BF16 ? go_type<MPQ_BF16>(p, group, scale_type, st) : go_type<MPQ_F16>(p, group, scale_type, st);
+  if (x_type == MPQ_F32) return go_type<MPQ_F32>(p, group, st);
+  return x_type == MPQ_BF16 ? go_type<MPQ_BF16>(p, group, st) : go_type<MPQ_F16>(p, group, st);
 }
