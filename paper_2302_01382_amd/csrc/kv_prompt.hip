@@ -10,6 +10,8 @@ __global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) v
 
 struct PromptKernels {
   typedef void (*Kern)(AttnArgs, int64_t);
+  template <int T, int DH, int NQ>
+  using Cfg = PromptCfg<T, DH, NQ>;
   template <int T, int DH, int NQ, bool ONE>
   static Kern kernel() { return kv_prompt_k<T, DH, NQ, ONE>; }
   static int launch(Kern k, dim3 grid, int threads, int lds, hipStream_t st, const AttnArgs& a, int64_t wg_tiles) {

@@ -69,7 +69,8 @@ __device__ __forceinline__ void lds_meet() {
   asm volatile("" ::: "memory");
 }
 
-template <int T, int DH, int NQ>
+// SINGLE: one LDS stage, which leaves room for a third workgroup on a CU
+template <int T, int DH, int NQ, bool SINGLE = false>
 struct PromptCfg {
   // fp16 terms of q, and of a probability.  A second one of these takes a quarter of the time (bf16, two prompts of up to 4500 rows 262 |
   // 337 us).  It brings an fp16 output's distance to 64 bits from 3.0e-4 to 2.1e-4, its own rounding's.  A bf16 output's is 1.7e-3
@@ -83,7 +84,7 @@ struct PromptCfg {
   static constexpr int NW = DH == 4 ? 8 : 4, THREADS = NW * 64;
   static constexpr int ROWS = NW * 16 * NQ;                 // rows of a workgroup
   static constexpr int K_BYTES = 64 * DH * 128, STAGE = 2 * K_BYTES;
-  static constexpr int LDS_BYTES = 2 * STAGE;
+  static constexpr int LDS_BYTES = SINGLE ? STAGE : 2 * STAGE;
   static constexpr int NK = 256 * DH / THREADS, NV = NK;    // chunks per thread and step: 16 bytes of keys; twice 8 of values
 };
 
@@ -91,9 +92,9 @@ struct PromptCfg {
 // short sequences; then splits; row tiles last, the last ones -- under a causal mask the longest -- first.
 // ONE: a page holds at least a step's tokens, which then lie on one page.
 // TREE: of a sequence's own rows, its last tokens, a row sees those that its bits name.
-template <int T, int DH, int NQ, bool ONE, bool TREE>
+template <int T, int DH, int NQ, bool ONE, bool TREE, bool SINGLE = false>
 __device__ __forceinline__ void prompt_rows_body(const AttnArgs& a, int64_t wg_tiles, const TreeMask& tree) {
-  using C = PromptCfg<T, DH, NQ>;
+  using C = PromptCfg<T, DH, NQ, SINGLE>;
   using E = Elem<T>;
   typedef typename E::type El;
   constexpr int QT = C::QT, PT = C::PT, TT = 64;
@@ -456,7 +457,8 @@ __device__ __forceinline__ void prompt_rows_body(const AttnArgs& a, int64_t wg_t
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    stage = (unsigned)C::STAGE - stage;
+    if (SINGLE) lds_meet();
+    else stage = (unsigned)C::STAGE - stage;
     if (more) store(stage);
     if (more) arrived();
     lds_meet();
@@ -493,7 +495,7 @@ __device__ __forceinline__ void prompt_rows_body(const AttnArgs& a, int64_t wg_t
 // K: the kernels, and what they take besides the call and its tiles
 template <typename K, int T, int DH, int NQ>
 static int prompt_go(const K& k, const AttnArgs& a, int64_t wg_tiles, bool prepare_only, hipStream_t st) {
-  using C = PromptCfg<T, DH, NQ>;
+  using C = typename K::template Cfg<T, DH, NQ>;
   using Kern = typename K::Kern;
   static const Kern kerns[2] = {K::template kernel<T, DH, NQ, false>(), K::template kernel<T, DH, NQ, true>()};
   static std::atomic<unsigned> done[kMaxDevices];

@@ -14,7 +14,7 @@ constexpr int kTreeBits = 14;  // probabilities are multiplied by 2^14 before th
 template <int DH, int MT>
 struct TreeShape {
   static constexpr int TT = DH * MT <= 2 ? 64 : 32;  // tokens per step
-  static constexpr int NW = DH * MT <= 4 ? 8 : 4;    // waves
+  static constexpr int NW = DH < 4 ? 8 : 4;            // waves (dim > 128: shares of eight pass the LDS)
 };
 
 __device__ __forceinline__ v4i stream_codes(const int8_t* p) {
@@ -348,7 +348,70 @@ __global__ __launch_bounds__((TreeShape<DH, MT>::NW * 64)) void kv_tree_k(AttnAr
   }
 }
 
-// How a call is cut up.
+// Joins the splits of a row, a wave per row: its lanes over groups of four channels and, as many as are left, over the splits.  For few splits
+// of many rows, where a workgroup per row (kv_attention_join_k) is mostly the launching of workgroups: 9984 rows of two splits of 128
+// channels 18.6 us there.
+// grid: (((sequence * heads + head) * row_tiles + tile) * tile_rows + row) / 4
+template <int T>
+__global__ __launch_bounds__(kBlock) void kv_tree_join_k(AttnArgs a) {
+  using E = Elem<T>;
+  typedef typename E::type El;
+  const int lane = threadIdx.x & 63;
+  const uint64_t wave = (uint64_t)block_index() * 4 + (uint64_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const Digits g = wave >> 32 == 0 ? split_digits<unsigned>((unsigned)wave, (unsigned)a.tile_rows, (unsigned)a.row_tiles, (unsigned)a.c.heads)
+                                   : split_digits<uint64_t>(wave, (uint64_t)a.tile_rows, (uint64_t)a.row_tiles, (uint64_t)a.c.heads);
+  const int row = (int)g.d[0], h = (int)g.d[2];
+  const int64_t tile = g.d[1], s = g.d[3], slot = ((s * a.c.heads + h) * a.row_tiles + tile) * a.splits;
+  if (s >= a.b.seqs) return;
+  const Sequence sq = sequence(a.b, a.c.page, (int)s);
+  const int64_t at = tile * 16 + row;
+  if (at >= (int64_t)sq.n * a.group) return;
+  const int D = a.c.dim, quads = D >> 2, parts = kWave / quads, d = lane % quads * 4, part = lane / quads;
+  const Partial* of = a.part + slot * 16 + row;  // the row's in the first split; 16 to the next
+  float top = -__builtin_inff(), exponent = -__builtin_inff();
+  for (int i = lane; i < a.splits; i += kWave) {
+    const Partial x = of[(int64_t)i * 16];
+    top = fmaxf(top, x.m);
+    exponent = fmaxf(exponent, x.e);
+  }
+  top = wave_max(top);
+  const int e_all = (int)wave_max(exponent);
+  const float use = top == -__builtin_inff() ? 0.0f : top;
+  float l = 0.0f;
+  f32x4 v = {0, 0, 0, 0};
+  if (part < parts) {
+#pragma unroll 4
+    for (int i = part; i < a.splits; i += parts) {
+      const Partial x = of[(int64_t)i * 16];
+      const float f = __builtin_amdgcn_exp2f(x.m - use);
+      l += x.l * f;
+      v += *reinterpret_cast<const f32x4*>(a.part_o + ((slot + i) * 16 + row) * D + d) * __builtin_ldexpf(f, (int)x.e - e_all);
+    }
+  }
+  f32x4 sum = v;
+  float l_all = l;
+  for (int i = 1; i < parts; ++i) {  // in a fixed order
+    const int from = (lane + i * quads) & 63;
+    l_all += __shfl(l, from, 64);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += __shfl(v[e], from, 64);
+  }
+  if (part > 0) return;
+  const unsigned group = (unsigned)a.group, token = (unsigned)at / group;
+  El* to = reinterpret_cast<El*>(a.out) + (sq.row0 + token) * a.o_ts + (int64_t)(h * a.group + (int)((unsigned)at - token * group)) * a.o_hs + d;
+  E::store4(to, l_all == 0.0f ? f32x4{0, 0, 0, 0} : times_two_to(sum / l_all, e_all));  // (a row with a NaN in q has one in l)
+}
+
+// Which kernel takes a call, in what pieces: up to 32 rows (row, query head pairs of a key head) the one here, with one or two tiles and splits
+// that fill the chip once; more in the wide kernel, in pieces of 64 rows of which three workgroups share a CU, of 128 from 129 rows on; few
+// rows over short sequences here, where a workgroup's latency counts.  us on the device, bf16, pages of 64 (sequences x drafted
+// tokens behind held, key heads x group, dim; one tile | two tiles | pieces of 64 | of 128, each with its best number of splits):
+// 1 x 3 behind 60000 8x4 128 fp16 33 | 35 | 44 | 69, 32 x 5 behind 4000 8x4 128 74 | 59 | 65 | -, 1 x 5 behind 32000 28 | 27 | 30 | 39, 8 x 7 behind 8000 43 |
+// 39 | 40 | -, 32 x 30 behind 1000 12x1 64 28 | 26 | 24 | 33 -- 4 x 16 behind 8000 8x4 128 41 | 38 | 31 | 36, 24 x 13 behind 8000 171 | 149 | 88 | 138, the
+// same behind 4000 in fp32 - | 91 | 73 | -, 4 x 30 behind 8000 62 | 59 | 42 | 43, 16 x 60 behind 2000 8x8 128 - | - | 84 | 87, 1 x 61 behind 65500 8x4 128 fp16
+// 434 | 349 | 147 | 126, 2 x 10 behind 16000 2x7 256 41 | 48 | - | 35 -- 1 x 60 behind 400 12x1 64 6.9 | 9.8 | 10.3 | -, 2 x 100 behind 300 8x4 128 18.5 |
+// 14.6 | 17.2 | 23.  (Four tiles here, which need 480 registers: 24 x 13 behind 8000 196.)  Splits: 4 x 16 behind 8000 in pieces of 64, 8 | 16 | 32:
+// 33 | 31 | 38; 24 x 13 behind 8000, 2 | 4 | 8: 118 | 88 | 110.
 struct TreePlan {
   int64_t row_tiles, tiles, wg_tiles;
   int mt, splits, tile_rows;
@@ -369,19 +432,20 @@ static int plan_tree(const mpq_kv_cache& c, const mpq_kv_batch& b, int type, int
   p.ws_bytes = 0;
   if (p.tiles == 0) return MPQ_OK;
   const int64_t room = (int64_t)b.table_pages * c.page, len = b.max_len < room ? b.max_len : room;
-  const int dh = c.dim <= 64 ? 1 : c.dim <= 128 ? 2 : 4;
-  p.mt = p.row_tiles == 1 ? 1 : p.row_tiles == 2 || dh == 4 ? 2 : 4;
+  // a workgroup's row tiles here; few, short sequences' rows spread over the chip
+  const bool narrow = c.dim <= 128;
+  p.mt = p.row_tiles == 1 || !narrow || (len <= 768 && pair_rows > 32 && p.tiles <= kNumCU) ? 1 : 2;
   p.wg_tiles = (p.row_tiles + p.mt - 1) / p.mt;
-  const int64_t want = kNumCU / (p.wg_tiles * pairs), most_splits = len <= 768 ? 1 : (len + 255) / 256;
-  int64_t splits = want < most_splits ? want : most_splits;
-  if (pair_rows > 64) {
+  const int64_t units = p.wg_tiles * pairs;
+  int64_t splits = kNumCU / units, most_splits = len <= 768 ? 1 : (len + 255) / 256;
+  if (pair_rows > 32 && !(len <= 768 && units <= kNumCU)) {
     const int wide = prompt_rows(type, c.dim);
-    const int64_t units = (pair_rows + wide - 1) / wide * pairs;
-    const int64_t cut = (c.dim <= 128 ? 2 : 1) * kNumCU / units, most_cut = len < 768 ? 1 : len / 768;
-    splits = units > kNumCU / 2 ? 1 : cut < most_cut ? cut : most_cut;
-    p.wide_rows = splits == 1 && units <= 2 * kNumCU && c.dim <= 128 ? 64 : wide;
+    p.wide_rows = narrow && pair_rows <= 128 ? 64 : wide;
     p.wg_tiles = (pair_rows + p.wide_rows - 1) / p.wide_rows;
+    splits = (!narrow ? 1 : p.wide_rows == 64 ? 3 : 2) * kNumCU / (p.wg_tiles * pairs);
+    most_splits = len < 1000 ? 1 : len / 500;
   }
+  splits = splits < most_splits ? splits : most_splits;
   p.splits = (int)(splits < 1 ? 1 : splits);
   if (blocks_z(p.tiles * (p.splits > 16 ? p.splits : 16), 512) > 65535u) return MPQ_ERR_SHAPE;
   p.ws_bytes = p.splits > 1 ? (size_t)p.tiles * p.splits * 16 * (c.dim * sizeof(float) + sizeof(Partial)) : 0;
@@ -398,11 +462,10 @@ static int go(const AttnArgs& a, const TreeMask& tree, int64_t wg_tiles, hipStre
 }
 template <int T, int DH>
 static int go_tiles(const AttnArgs& a, const TreeMask& tree, const TreePlan& p, hipStream_t st) {
-  if (p.mt == 1) return go<T, DH, 1>(a, tree, p.wg_tiles, st);
   if constexpr (DH < 4) {
-    if (p.mt == 4) return go<T, DH, 4>(a, tree, p.wg_tiles, st);
+    if (p.mt == 2) return go<T, DH, 2>(a, tree, p.wg_tiles, st);
   }
-  return go<T, DH, 2>(a, tree, p.wg_tiles, st);
+  return go<T, DH, 1>(a, tree, p.wg_tiles, st);
 }
 template <int T>
 static int launch_tree(const AttnArgs& a, const TreeMask& tree, const TreePlan& p, hipStream_t st) {
@@ -410,7 +473,10 @@ static int launch_tree(const AttnArgs& a, const TreeMask& tree, const TreePlan& 
   if (p.wide_rows > 0) rc = launch_tree_wide(T, a, tree, p.wg_tiles, p.wide_rows, st);
   else if (a.c.dim <= 64) rc = go_tiles<T, 1>(a, tree, p, st);
   else rc = a.c.dim <= 128 ? go_tiles<T, 2>(a, tree, p, st) : go_tiles<T, 4>(a, tree, p, st);
-  return rc != MPQ_OK || p.splits == 1 ? rc : launch_join(T, a, p.tiles, st);
+  if (rc != MPQ_OK || p.splits == 1) return rc;
+  if (p.splits > 16) return launch_join(T, a, p.tiles, st);
+  kv_tree_join_k<T><<<wide_grid((p.tiles * p.tile_rows + 3) / 4, kBlock), kBlock, 0, st>>>(a);
+  return launch_status();
 }
 
 }  // namespace mpq

@@ -4,13 +4,16 @@
 
 namespace mpq {
 
+constexpr bool kSingle(int dh, int nq) { return dh <= 2 && nq == 1; }
 template <int T, int DH, int NQ, bool ONE>
-__global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : 2) void kv_tree_wide_k(AttnArgs a, int64_t wg_tiles, TreeMask tree) {
-  prompt_rows_body<T, DH, NQ, ONE, true>(a, wg_tiles, tree);
+__global__ __launch_bounds__((PromptCfg<T, DH, NQ>::THREADS), DH == 4 ? 1 : kSingle(DH, NQ) && T != MPQ_F32 ? 3 : 2) void kv_tree_wide_k(AttnArgs a, int64_t wg_tiles, TreeMask tree) {
+  prompt_rows_body<T, DH, NQ, ONE, true, kSingle(DH, NQ)>(a, wg_tiles, tree);
 }
 
 struct TreeKernels {
   typedef void (*Kern)(AttnArgs, int64_t, TreeMask);
+  template <int T, int DH, int NQ>
+  using Cfg = PromptCfg<T, DH, NQ, kSingle(DH, NQ)>;
   TreeMask tree;
   template <int T, int DH, int NQ, bool ONE>
   static Kern kernel() { return kv_tree_wide_k<T, DH, NQ, ONE>; }
