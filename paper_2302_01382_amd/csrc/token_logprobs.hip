@@ -3,15 +3,15 @@
 // With m the row's largest logit, d = scale log2(e) (x - m), l = sum 2^d and w = sum d 2^d:
 //   ln p_t = scale (x_t - m) - ln l,   entropy = ln l - ln 2 w / l.
 // A workgroup holds a piece of a row in registers, so that the maximum is known before the first exponential and nothing is
-// rescaled in the loop.  The largest `top` of a piece: of the 64 maxima of what the four threads of a lane number hold, the
+// rescaled in the loop.  The largest `top` of a piece: of the 64 maxima of what the threads of a lane number hold, the
 // top-th largest is a bound that at least `top` values reach and few more do; those are listed, and a value's place in the order is
 // the number of listed ones before it.  Where too many share the bound (all logits equal, say), they are taken one at a time.
-// Rows of several pieces are joined by a wave each.
+// Rows of several pieces are joined by a workgroup each.
 #include "types.hpp"
 
 namespace mpq {
 
-constexpr int kMostTop = 32, kPieceThreads = 256, kListed = 1024;
+constexpr int kMostTop = 32, kPieceThreads = 256, kWideThreads = 1024, kListed = 1024;
 constexpr int64_t kMostVocab = 1 << 22;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // 2^-200 is 0 in fp32: as the least exponent it leaves minus infinity a product of 0
@@ -64,8 +64,9 @@ __device__ __forceinline__ unsigned bound_of(unsigned largest, int top) {
 
 // The first `top` of n keys, in order, to out (those behind the last are 0): a key's place is the number of larger ones.  All threads;
 // keys are there and out is cleared already.
+template <int THREADS>
 __device__ __forceinline__ void place_keys(const Key* keys, int n, int top, Key* out) {
-  for (int k = threadIdx.x; k < n; k += kPieceThreads) {
+  for (int k = threadIdx.x; k < n; k += THREADS) {
     const Key mine = keys[k];
     int place = 0;
 #pragma unroll 8
@@ -95,12 +96,28 @@ __device__ __forceinline__ void store_top(const LogprobArgs& a, int64_t row, int
   a.top_index[row * a.top + i] = k ? index_of(k) : -1;
 }
 
+// over the waves, in a fixed order
+template <int NW>
+__device__ __forceinline__ float max_of(const float* v) {
+  float m = v[0];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) m = fmaxf(m, v[i]);
+  return m;
+}
+template <int NW>
+__device__ __forceinline__ float sum_of(const float* v) {
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NW; i += 4) s += (v[i] + v[i + 1]) + (v[i + 2] + v[i + 3]);
+  return s;
+}
+
 // V: vectors of eight values that a thread holds.  grid: row * pieces + piece
-template <int T, int V>
-__global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a) {
+template <int T, int V, int THREADS>
+__global__ __launch_bounds__(THREADS) void token_logprobs_k(LogprobArgs a) {
   using E = Elem<T>;
   typedef typename E::type El;
-  constexpr int NW = kPieceThreads / kWave;
+  constexpr int NW = THREADS / kWave;
   __shared__ float sm_m[NW], sm_l[NW], sm_w[NW], sm_log;
   __shared__ float lane_max[NW][kWave];
   __shared__ int count;
@@ -110,19 +127,19 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
   const int piece = (int)(b - row * a.pieces);
   if (row >= a.rows) return;
   const El* x = reinterpret_cast<const El*>(a.logits) + row * a.stride;
-  const int vocab = (int)a.vocab, first = piece * (kPieceThreads * 8 * V);
+  const int vocab = (int)a.vocab, first = piece * (THREADS * 8 * V);
   float v[V][8], most[V];  // most: of each vector
-  if (first + kPieceThreads * 8 * V <= vocab) {  // uniform
+  if (first + THREADS * 8 * V <= vocab) {  // uniform
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const f32x8 y = E::load8(x + first + (i * kPieceThreads + tid) * 8);
+      const f32x8 y = E::load8(x + first + (i * THREADS + tid) * 8);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] = y[e];
     }
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int at = first + (i * kPieceThreads + tid) * 8;
+      const int at = first + (i * THREADS + tid) * 8;
       f32x8 y;
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = -__builtin_inff();
@@ -151,7 +168,7 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
   if (tid == 0) count = 0;
   if (tid < kMostTop) out[tid] = 0;
   __syncthreads();
-  const float m = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
+  const float m = max_of<NW>(sm_m);
   const float m_use = m == -__builtin_inff() ? 0.0f : m, c = a.scale * kLog2e;
   float l = 0.0f, w = 0.0f;
 #pragma unroll
@@ -170,7 +187,10 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
   }
   float low = 0.0f;
   if (a.top > 0) {
-    low = value_of(bound_of(order_of(fmaxf(fmaxf(lane_max[0][lane], lane_max[1][lane]), fmaxf(lane_max[2][lane], lane_max[3][lane]))), a.top));
+    float of_lane = lane_max[0][lane];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) of_lane = fmaxf(of_lane, lane_max[i][lane]);
+    low = value_of(bound_of(order_of(of_lane), a.top));
     if (mine >= low) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -179,30 +199,30 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_k(LogprobArgs a)
         for (int e = 0; e < 8; ++e)
           if (v[i][e] >= low) {
             const int k = atomicAdd(&count, 1);  // (any order: places go by value and index)
-            if (k < kListed) listed[k] = key_of(v[i][e], first + (i * kPieceThreads + tid) * 8 + e);
+            if (k < kListed) listed[k] = key_of(v[i][e], first + (i * THREADS + tid) * 8 + e);
           }
       }
     }
   }
   __syncthreads();
   if (tid == 0) {
-    l = (sm_l[0] + sm_l[1]) + (sm_l[2] + sm_l[3]);
-    w = (sm_w[0] + sm_w[1]) + (sm_w[2] + sm_w[3]);
+    l = sum_of<NW>(sm_l);
+    w = sum_of<NW>(sm_w);
     if (a.pieces > 1) a.piece[b] = Piece{m, l, w};
     else sm_log = finish_row<T>(a, row, m, l, w);
   }
   if (a.top == 0) return;
   const int n = count;
   if (n <= kListed) {
-    place_keys(listed, n, a.top, out);
+    place_keys<THREADS>(listed, n, a.top, out);
   } else {
     // too many share the bound: one at a time, read again, the largest key below the last one taken
-    const int end = first + kPieceThreads * 8 * V < vocab ? first + kPieceThreads * 8 * V : vocab;
+    const int end = first + THREADS * 8 * V < vocab ? first + THREADS * 8 * V : vocab;
     Key last = ~(Key)0;
     for (int k = 0; k < a.top; ++k) {
       Key best = 0;
 #pragma unroll 1
-      for (int here = first + tid; here < end; here += kPieceThreads) {
+      for (int here = first + tid; here < end; here += THREADS) {
         const float z = (float)x[here];
         const Key key = z >= low ? key_of(z, here) : 0;
         if (key < last && key > best) best = key;
@@ -288,7 +308,7 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_join_k(LogprobAr
   if (a.top == 0) return;
   if (!all) n = count;
   if (n <= kListed) {
-    place_keys(listed, n, a.top, out);
+    place_keys<kPieceThreads>(listed, n, a.top, out);
   } else {
     // too many share the bound: one at a time, the largest key below the last one taken
     Key last = ~(Key)0;
@@ -315,33 +335,54 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_join_k(LogprobAr
 }
 
 struct LogprobPlan {
-  int vectors, pieces;
+  int vectors, threads, pieces;
   size_t ws_bytes;
 };
 static int plan_logprobs(int64_t rows, int64_t vocab, int type, int top, LogprobPlan& p) {
-  if (!known_type(type) || rows < 0 || vocab <= 0 || vocab > kMostVocab || top < 0 || top > kMostTop) return MPQ_ERR_SHAPE;
-  auto pieces = [&](int vectors) { return (vocab + kPieceThreads * 8 * vectors - 1) / (kPieceThreads * 8 * vectors); };
+  if (!known_type(type) || rows < 0 || vocab <= 0 || vocab > kMostVocab || top < 0 || top > kMostTop || mul_overflows(rows, vocab)) return MPQ_ERR_SHAPE;
+  auto pieces = [&](int vectors, int threads) { return (vocab + threads * 8 * vectors - 1) / (threads * 8 * vectors); };
   // One piece, the smallest that takes the row, spares the join's launch (us on the device, one piece | several; the host saves 4 more: 1 x
-  // 10000 6.1 | 6.6, 100 x 16000 fp32 7.0 | 9.1, 4000 x 10000 fp32 35 | 40).  Else eight vectors a thread where that makes many rounds of the
-  // chip, so that loads overlap with other workgroups' arithmetic, else fewer (2 | 4 | 8 vectors: 2500 x 65536 bf16 92 | 75 | 71, 190 x 100003
-  // fp32 24.2 | 23.1 | 24.0, 256 x 32768 12.8 | 12.6 | 12.8, 16 x 50000 fp32 8.0 | 8.7 | 9.4, 1 x 131072 9.1 | 9.6 | 10.4).
+  // 10000 6.1 | 6.6, 100 x 16000 fp32 7.0 | 9.1, 4000 x 10000 fp32 35 | 40).
   p.vectors = 1;
-  while (p.vectors < 8 && pieces(p.vectors) > 1) p.vectors *= 2;
-  if (pieces(8) > 1) p.vectors = rows * pieces(8) >= 8 * kNumCU ? 8 : rows * pieces(4) >= 4 * kNumCU ? 4 : 2;
-  p.pieces = (int)pieces(p.vectors);
+  p.threads = kPieceThreads;
+  while (p.vectors < 8 && pieces(p.vectors, p.threads) > 1) p.vectors *= 2;
+  if (pieces(8, kPieceThreads) > 1) {
+    // Up to 65536 values one workgroup of 16 waves still holds a row, which pays where all rows are on the chip at once: two workgroups to a
+    // CU at four vectors, one at eight (one wide piece | several, device: 1 x 32768 bf16 6.0 | 7.2, 256 x 32768 9.1 | 12.7, 512 x 32768
+    // 12.3 | 14.9, 1000 x 32768 22.1 | 21.7, 1 x 65536 8.0 | 7.3 but 11.9 | 15.9 from the host, 256 x 60000 fp32 18.7 | 19.7, 512 x 65536
+    // bf16 25 | 22).
+    const int vectors = pieces(4, kWideThreads) == 1 ? 4 : 8;
+    if (pieces(vectors, kWideThreads) == 1 && rows <= 8 * kNumCU / vectors) {
+      p.threads = kWideThreads;
+      p.vectors = vectors;
+    } else {
+      // Eight vectors a thread where that makes many rounds of the chip, so that loads overlap with other workgroups' arithmetic, else
+      // fewer (2 | 4 | 8 vectors: 2500 x 65536 bf16 92 | 75 | 71, 190 x 100003 fp32 24.2 | 23.1 | 24.0, 1 x 131072 9.1 | 9.6 | 10.4).
+      p.vectors = rows * pieces(8, kPieceThreads) >= 8 * kNumCU ? 8 : rows * pieces(4, kPieceThreads) >= 4 * kNumCU ? 4 : 2;
+    }
+  }
+  p.pieces = (int)pieces(p.vectors, p.threads);
   if (mul_overflows(rows, (int64_t)p.pieces * (kMostTop + 4))) return MPQ_ERR_SHAPE;
   p.ws_bytes = p.pieces > 1 ? (size_t)rows * p.pieces * (sizeof(Piece) + (size_t)top * 8) : 0;
-  if (rows > 0 && blocks_z(rows * p.pieces, kPieceThreads) > 65535u) return MPQ_ERR_SHAPE;
+  if (rows > 0 && blocks_z(rows * p.pieces, p.threads) > 65535u) return MPQ_ERR_SHAPE;
   return MPQ_OK;
 }
 
 template <int T>
 static int launch_logprobs(const LogprobArgs& a, const LogprobPlan& p, hipStream_t st) {
-  const dim3 grid = wide_grid(a.rows * a.pieces, kPieceThreads);
-  if (p.vectors == 1) token_logprobs_k<T, 1><<<grid, kPieceThreads, 0, st>>>(a);
-  else if (p.vectors == 2) token_logprobs_k<T, 2><<<grid, kPieceThreads, 0, st>>>(a);
-  else if (p.vectors == 4) token_logprobs_k<T, 4><<<grid, kPieceThreads, 0, st>>>(a);
-  else token_logprobs_k<T, 8><<<grid, kPieceThreads, 0, st>>>(a);
+  const dim3 grid = wide_grid(a.rows * a.pieces, p.threads);
+  if (p.threads == kWideThreads) {
+    if (p.vectors == 4) token_logprobs_k<T, 4, kWideThreads><<<grid, kWideThreads, 0, st>>>(a);
+    else token_logprobs_k<T, 8, kWideThreads><<<grid, kWideThreads, 0, st>>>(a);
+  } else if (p.vectors == 1) {
+    token_logprobs_k<T, 1, kPieceThreads><<<grid, kPieceThreads, 0, st>>>(a);
+  } else if (p.vectors == 2) {
+    token_logprobs_k<T, 2, kPieceThreads><<<grid, kPieceThreads, 0, st>>>(a);
+  } else if (p.vectors == 4) {
+    token_logprobs_k<T, 4, kPieceThreads><<<grid, kPieceThreads, 0, st>>>(a);
+  } else {
+    token_logprobs_k<T, 8, kPieceThreads><<<grid, kPieceThreads, 0, st>>>(a);
+  }
   const int rc = launch_status();
   if (rc != MPQ_OK || a.pieces == 1) return rc;
   token_logprobs_join_k<T><<<wide_grid(a.rows, kPieceThreads), kPieceThreads, 0, st>>>(a);

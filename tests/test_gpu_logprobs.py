@@ -62,6 +62,18 @@ def test_logprobs(dtype, n, vocab, top):
         check(got, full(x), tokens, top, scale)
 
 
+@pytest.mark.parametrize("n,vocab", [(1, 16384), (2, 16385), (3, 32768), (2, 32769), (3, 65535), (2, 65536), (2, 65537), (257, 33001), (513, 17001)])
+def test_where_a_row_is_cut(n, vocab):
+    """The sizes at which a row goes from one workgroup's hold to the next, and the rows at which it is cut after all."""
+    r = rng(n * vocab)
+    for dtype, top in (("float32", 32), ("bfloat16", 7)):
+        x = rows(r, n, vocab, dtype)
+        tokens = np.concatenate(([vocab - 1], r.integers(0, vocab, n - 1))).astype(np.int32)
+        check(mpq.token_logprobs(x, dev(tokens, "int32"), top), full(x), tokens, top, 1.0)
+    x = np.zeros((n, vocab), np.float32)
+    check(mpq.token_logprobs(dev(x), dev(tokens, "int32"), 32), x, tokens, 32, 1.0)
+
+
 @pytest.mark.parametrize("n,vocab", [(1, 5000), (600, 5000), (2, 70000)])
 def test_equal_logits(n, vocab):
     """All equal, two values, ties across pieces: the lowest index first."""
