@@ -59,7 +59,7 @@ int mpq_last_hip_error(void);
 /* Library version, major*100 + minor. */
 int mpq_version(void);
 /* Optional.  Configures, on the caller's current device, every kernel variant of the quantized-layer
- * calls, of mpq_kv_attention and of mpq_hutchinson_quad_signs that needs more than the default amount of on-chip memory (a
+ * calls, of mpq_kv_attention, mpq_kv_attention_tree and mpq_hutchinson_quad_signs that needs more than the default amount of on-chip memory (a
  * per-kernel runtime attribute, not a stream operation).  Without it the first call that selects a
  * variant does the same for that variant; code that records the calls into a HIP graph calls
  * mpq_init() before the capture begins, or runs each call once eagerly first.  Thread safe,
@@ -536,7 +536,7 @@ int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int t
  * w_q        two's-complement nibbles [N x K/2], the even channel in the low half (packed4_out of mpq_fake_quant; the weights seen as
  *            [N * K/group x group] with MPQ_PER_ROW give codes and maxima of such groups); any alignment.
  * group      32, 64 or 128; K a multiple of it.   w_scale  [N x K/group] of scale_type, dense.
- * y_out      [M x N] of y_type, dense.
+ * y_out      [M x N] of y_type, dense; it may not overlap the inputs.
  * Products are exact and sums in fp32 (a group's about -24 times the sum of its x, which is added in again: intermediate values are up
  * to 31 |x| summed); where such a value passes fp32's range, and for an x that is not finite, results are infinite or NaN.
  * Made for few rows, whose time is that of reading the weights; more go in blocks of 64, each of which reads the weights.
@@ -574,7 +574,7 @@ int mpq_rotate_heads(int type, int64_t rows, int dim, const void* q, int64_t q_t
  * tree       device int64 [rows][tree_words], 8-byte aligned, bits in words from the lowest.  tree_words at least 1 (else
  *            MPQ_ERR_SHAPE): drafted tokens behind the last word are not seen; bits behind a sequence's last drafted token do not matter.
  * Everything else, and what is rounded, as mpq_kv_attention without a window.  Tokens that are kept are appended again, in a row, behind
- * what the sequence held before. */
+ * what the sequence held before; a page's maximum stays that of all that was drafted onto it. */
 size_t mpq_kv_attention_tree_workspace_bytes(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, int q_heads);
 int mpq_kv_attention_tree(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, const void* q, int64_t q_token_stride,
                           int64_t q_head_stride, int q_heads, float softmax_scale, const int64_t* tree, int tree_words, void* out,

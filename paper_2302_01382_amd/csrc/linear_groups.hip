@@ -542,6 +542,8 @@ static int go(const GroupsArgs& p, hipStream_t st) {
   else linear_groups_k<T, WIDE, G, MT, 3><<<grid, kGroupThreads, 0, st>>>(p);
   return launch_status();
 }
+// of a workgroup
+static int most_rows(int x_type) { return x_type == MPQ_F32 ? 32 : 64; }
 template <int T, bool WIDE, int G>
 static int go_rows(const GroupsArgs& p, hipStream_t st) {
   constexpr int TERMS = Operand<T>::TERMS, SIZE = WIDE ? 4 : 2;
@@ -551,8 +553,10 @@ static int go_rows(const GroupsArgs& p, hipStream_t st) {
     return launch_status();
   }
   if (p.M <= 16) return go<T, WIDE, G, 1>(p, st);
-  if (p.M <= 32 || T == MPQ_F32) return go<T, WIDE, G, 2>(p, st);
-  return go<T, WIDE, G, T == MPQ_F32 ? 2 : 4>(p, st);
+  if constexpr (T != MPQ_F32) {
+    if (p.M > 32) return go<T, WIDE, G, 4>(p, st);
+  }
+  return go<T, WIDE, G, 2>(p, st);
 }
 template <int T, bool WIDE>
 static int go_group(const GroupsArgs& p, int group, hipStream_t st) {
@@ -574,7 +578,8 @@ extern "C" int mpq_linear_groups(const void* x, int x_type, int64_t M, int64_t N
   if (M < 0 || N <= 0 || K <= 0 || K % group || K > (1 << 30) || x_stride < K) return MPQ_ERR_SHAPE;
   if (mul_overflows(M, x_stride) || mul_overflows(N, K) || mul_overflows(M, N)) return MPQ_ERR_SHAPE;
   // (a grid counts 2^32 threads in x and 65535 blocks of rows in y)
-  if (N > (1 << 26) || (M + 63) / 64 > kMaxGridY) return MPQ_ERR_SHAPE;
+  const int64_t block = most_rows(x_type);
+  if (N > (1 << 26) || (M + block - 1) / block > kMaxGridY) return MPQ_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(x) & (uintptr_t)(type_size(x_type) - 1)) return MPQ_ERR_ALIGN;
   if (reinterpret_cast<uintptr_t>(w_scale) & (uintptr_t)(type_size(scale_type) - 1)) return MPQ_ERR_ALIGN;
   if (reinterpret_cast<uintptr_t>(y_out) & (uintptr_t)(type_size(y_type) - 1)) return MPQ_ERR_ALIGN;

@@ -3,8 +3,9 @@
 //
 // y = x / sqrt(mean x^2 + eps) * w, then pairs (a, b) -> (a cos t - b sin t, b cos t + a sin t), t = position * frequency.  A lane
 // holds eight channels of a head that make four whole pairs, so that the rotation needs no other lane, and the norm a sum over the
-// lanes of the head; a wave takes 64 / LPH heads of a row at a time.  Cosines and sines depend on the row alone: a lane makes its
-// four once per row.  The angle in turns is a product in 64 bits less its nearest whole number: a position of a million times a
+// lanes of the head; a wave takes 64 / LPH heads of a row at a time.  Cosines and sines depend on the row alone: a wave makes each
+// once, a pair to a lane, and hands them round.  Bytes bound it (12289 x 40 x 128 fp16: 252 MB in 55 us, 4.6 TB/s; a large copy reaches
+// 5.2), and with few rows the host.  The angle in turns is a product in 64 bits less its nearest whole number: a position of a million times a
 // frequency of one is 2e5 turns, of which fp32 would keep seven bits.
 #include "types.hpp"
 
@@ -177,7 +178,10 @@ extern "C" int mpq_rotate_heads(int type, int64_t rows, int dim, const void* q, 
                {q_out_token_stride, k_out_token_stride}, {q_out_head_stride, k_out_head_stride}, {q_weight, k_weight}, {q_heads, k_heads},
                positions, frequencies, rows, dim, pairs, 0, 0, eps};
   for (int i = 0; i < 2; ++i) {
-    if (a.heads[i] == 0) continue;
+    if (a.heads[i] == 0) {  // nothing of it is looked at
+      a.weight[i] = nullptr;
+      continue;
+    }
     if (a.in_ts[i] < 0 || a.in_hs[i] < 0 || a.out_ts[i] < 0 || a.out_hs[i] < 0) return MPQ_ERR_SHAPE;
     if (mul_overflows(rows, a.in_ts[i]) || mul_overflows(rows, a.out_ts[i]) || mul_overflows(a.heads[i], a.in_hs[i]) ||
         mul_overflows(a.heads[i], a.out_hs[i]))

@@ -40,6 +40,8 @@ def test_linear_groups_refuses():
     assert but(_4=2 ** 31, _5=2 ** 31) == mpq.ERR_SHAPE
     assert but(_2=2 ** 40, _5=2 ** 40) == mpq.ERR_SHAPE
     assert but(_3=2 ** 27) == mpq.ERR_SHAPE and but(_2=64 * 65535 + 1) == mpq.ERR_SHAPE  # grids that a launch cannot count
+    assert but(_1=0, _2=32 * 65535 + 1) == mpq.ERR_SHAPE and but(_1=0, _2=32 * 65535, _0=None) == mpq.ERR_NULL           # blocks of 32 rows
+    assert but(_2=64 * 65535, _0=None) == mpq.ERR_NULL
     assert but(_0=ODD) == mpq.ERR_ALIGN and but(_8=C.c_void_p(0x10002)) == mpq.ERR_ALIGN
     assert but(_8=ODD, _9=2) == mpq.ERR_ALIGN and but(_12=ODD) == mpq.ERR_ALIGN and but(_11=0, _12=C.c_void_p(0x10002)) == mpq.ERR_ALIGN
     assert but(_2=0, _0=None, _6=None, _8=None, _12=None) == mpq.OK        # no rows
@@ -121,7 +123,7 @@ def test_kv_attention_tree_refuses():
 def test_token_logprobs_refuses():
     L = mpq.lib()
     # logits, type, rows, vocab, stride, scale, tokens, logprob, entropy, top, top_logprob, top_index, ws, ws_bytes
-    but = caller(L.mpq_token_logprobs, [FAKE16, 1, 3, 50000, 50000, 1.0, FAKE, FAKE, FAKE, 5, FAKE, FAKE, FAKE16, BIG, None])
+    but = caller(L.mpq_token_logprobs, [FAKE16, 1, 3, 90000, 90000, 1.0, FAKE, FAKE, FAKE, 5, FAKE, FAKE, FAKE16, BIG, None])
     for i in (0, 6, 10, 11):
         assert but(**{"_%d" % i: None}) == mpq.ERR_NULL
     assert but(_7=None, _8=None, _9=0) == mpq.ERR_NULL                      # no output
@@ -130,18 +132,19 @@ def test_token_logprobs_refuses():
     assert but(_2=-1) == mpq.ERR_SHAPE and but(_2=2 ** 45) == mpq.ERR_SHAPE
     for vocab in (0, -5, 2 ** 22 + 1):
         assert but(_3=vocab, _4=2 ** 23) == mpq.ERR_SHAPE
-    assert but(_4=49999) == mpq.ERR_SHAPE
+    assert but(_4=89999) == mpq.ERR_SHAPE
     for scale in (0.0, -1.0, INF, NAN):
         assert but(_5=scale) == mpq.ERR_SHAPE
+    assert L.mpq_token_logprobs_workspace_bytes(2 ** 62, 50000, 1, 5) == 0 and but(_2=2 ** 62) == mpq.ERR_SHAPE
     for top in (-1, 33):
         assert but(_9=top) == mpq.ERR_SHAPE
     assert but(_0=ODD) == mpq.ERR_ALIGN
     for i in (6, 7, 8, 10, 11):
         assert but(**{"_%d" % i: C.c_void_p(0x1002)}) == mpq.ERR_ALIGN
-    need = L.mpq_token_logprobs_workspace_bytes(3, 50000, 1, 5)
+    need = L.mpq_token_logprobs_workspace_bytes(3, 90000, 1, 5)
     assert need > 0 and but(_13=need - 1) == mpq.ERR_WORKSPACE and but(_12=None) == mpq.ERR_WORKSPACE
     assert but(_12=C.c_void_p(0x10008)) == mpq.ERR_ALIGN
-    assert L.mpq_token_logprobs_workspace_bytes(3, 1000, 1, 5) == 0 and L.mpq_token_logprobs_workspace_bytes(3, 50000, 7, 5) == 0
+    assert L.mpq_token_logprobs_workspace_bytes(3, 1000, 1, 5) == 0 and L.mpq_token_logprobs_workspace_bytes(3, 90000, 7, 5) == 0
     assert but(_2=0, _0=None, _6=None, _10=None) == mpq.OK
 
 

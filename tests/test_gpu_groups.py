@@ -65,6 +65,42 @@ def test_rows_that_end_inside_a_step(group, K):
         check(full(mpq.linear_groups(x, w, steps_dev)), full(x), codes, steps, group, dtype)
 
 
+@pytest.mark.parametrize("group", (32, 64, 128))
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,N,K", [(9, 4200, 256), (40, 8300, 384), (64, 8333, 128), (100, 4111, 256), (1, 40, 131072), (8, 21, 14336), (5, 6, 65536)])
+def test_channel_tiles_and_long_rows(group, dtype, M, N, K):
+    """More channels than one tile to a workgroup fills the chip with; rows and steps that LDS holds no longer, or just."""
+    test_linear(group, dtype, M, N, K)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 2_200_000, 4096), (3, 140_000, 65536), (20, 140_000, 65536)])
+def test_offsets_past_32_bits(M, N, K):
+    """More than 2^32 bytes of codes: the last channels' are those of a small layer."""
+    import torch
+    r = rng(K)
+    codes, w, steps, steps_dev = layer(r, 70, K, 128, "bfloat16")
+    big_w = torch.zeros((N, K // 2), dtype=torch.uint8, device="cuda")
+    big_s = torch.zeros((N, K // 128), dtype=torch.bfloat16, device="cuda")
+    big_w[-70:] = w
+    big_s[-70:] = steps_dev
+    x = dev(r.standard_normal((M, K)), "bfloat16")
+    y = mpq.linear_groups(x, big_w, big_s)
+    check(full(y[:, -70:]), full(x), codes, steps, 128, "bfloat16")
+    assert not y[:, :-70].any()
+
+
+def test_offsets_past_32_bits_of_x():
+    import torch
+    r = rng(6)
+    codes, w, steps, steps_dev = layer(r, 20, 256, 64)
+    x = dev(r.standard_normal((30, 256)), "float16")
+    far = torch.empty(29 * (1 << 27) + 256, dtype=torch.float16, device="cuda").as_strided((30, 256), (1 << 27, 1))
+    far.copy_(x)
+    for rows in (30, 20, 5):   # (5: the last row at 2^30 bytes; its stride is a long one all the same)
+        assert torch.equal(mpq.linear_groups(far[:rows], w, steps_dev), mpq.linear_groups(x[:rows], w, steps_dev))
+    check(full(mpq.linear_groups(far, w, steps_dev)), full(x), codes, steps, 64, "float16")
+
+
 @pytest.mark.parametrize("steps_type", DTYPES)
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("act", (None, "relu", "gelu"))

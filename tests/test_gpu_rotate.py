@@ -112,6 +112,40 @@ def test_norm_alone_and_ends_of_the_range():
     np.testing.assert_array_equal(np.isnan(y).any(2), bad)
 
 
+def test_offsets_past_32_bits():
+    """Rows, and heads, that lie more than 2^32 bytes apart."""
+    import torch
+    r = rng(30)
+    q, k = heads(r, 34, 2, 64, "bfloat16"), heads(r, 34, 3, 64, "bfloat16")
+    far = torch.empty(34 << 26, dtype=torch.bfloat16, device="cuda")
+    wide = far.as_strided((34, 2, 64), (1 << 26, 100, 1))
+    wide.copy_(q)
+    tall = torch.empty(5 << 30, dtype=torch.bfloat16, device="cuda").as_strided((34, 3, 64), (64, 1 << 31, 1))
+    tall.copy_(k)
+    pos, f = dev(r.integers(0, 5000, 34), "int32"), dev(frequencies(32))
+    want = mpq.rotate_heads(q, k, pos, f)
+    for got, w in zip(mpq.rotate_heads(wide, tall, pos, f, q_out=wide, k_out=tall), want):
+        assert torch.equal(got, w)
+
+
+def test_nothing_is_looked_at_of_no_heads():
+    """In C: a weight, strides and pointers of the one that has no heads."""
+    import ctypes as C
+    import torch
+    r = rng(31)
+    x = heads(r, 9, 4, 64, "float32")
+    pos, f, out = dev(r.integers(0, 5000, 9), "int32"), dev(frequencies(32)), torch.empty_like(x)
+    odd = C.c_void_p(x.data_ptr() + 1)
+    want = mpq.rotate_heads(x, None, pos, f)[0]
+    for q, k in (((x.data_ptr(), 256, 64, 4), (odd, -1, -1, 0)), ((odd, -1, -1, 0), (x.data_ptr(), 256, 64, 4))):
+        out.zero_()
+        weights = (None, odd) if q[3] else (odd, None)
+        outs = [(out.data_ptr(), 256, 64) if n[3] else (odd, -1, -1) for n in (q, k)]
+        rc = mpq.lib().mpq_rotate_heads(0, 9, 64, *q, *k, pos.data_ptr(), f.data_ptr(), 32, 0, *weights, 1e-6, *outs[0], *outs[1],
+                                        C.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert rc == mpq.OK and torch.equal(out, want)
+
+
 def test_refusals_of_the_binding():
     import torch
     r = rng(7)

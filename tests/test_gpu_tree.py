@@ -226,6 +226,48 @@ def test_strides():
             assert torch.equal(out[:, :, 2:82].transpose(0, 1), want) and (out[:, :, :2] == 9).all() and (out[:, :, 82:] == 9).all()
 
 
+@pytest.mark.parametrize("new", ([3, 5], [40, 30], [130, 200]))
+def test_offsets_past_32_bits(new):
+    """A cache of more than 2^32 bytes of key codes: its last pages."""
+    import torch
+    r = rng(14)
+    heads, dim, page = 8, 128, 128
+    pages = (1 << 32) // (heads * dim * page) + 40
+    c = mpq.KvCache.empty(pages, heads, page, dim)
+    small = Pair(40, heads, page, dim, 8)
+    table = r.permutation(40)[:6].reshape(2, 3).astype(np.int32)
+    length = [300, 200]
+    b = small.batch(length, length, table)
+    far = mpq.KvBatch(b.starts, b.kv_len, b.table + (pages - 40), b.rows)
+    k, v = tokens(r, b.rows, heads, dim, "bfloat16")
+    small.append(b, k, v)
+    mpq.kv_append(c, far, k, v)
+    b = small.batch(new, length, table)
+    far = mpq.KvBatch(b.starts, b.kv_len, b.table + (pages - 40), b.rows)
+    seen, tree = bits_of([parents(r, n) for n in new])
+    q = dev(r.standard_normal((b.rows, heads, dim)), "bfloat16")
+    got = mpq.kv_attention_tree(c, far, q, tree)
+    assert torch.equal(got, mpq.kv_attention_tree(small.dev, b, q, tree))
+    check(small, full(got), full(q), seen, dim ** -0.5, "bfloat16")
+
+
+@pytest.mark.parametrize("new", (6, 70))
+def test_a_bound_of_rows_too_low(new):
+    """max_new below a sequence's rows: the others' rows are right, and those of every row within the bound."""
+    import torch
+    r = rng(15)
+    length = [2000, 900, 1500]
+    c, b = drafted(r, length, [new, 3, 2], 2, 64, 64, 8, "float16")
+    seen, tree = bits_of([parents(r, n) for n in (new, 3, 2)])
+    q = dev(r.standard_normal((b.rows, 4, 64)), "float16")
+    want = mpq.kv_attention_tree(c.dev, b, q, tree)
+    most = new - 2
+    low = mpq.KvBatch(b.starts, b.kv_len, b.table, b.rows, most, 2000)
+    got = mpq.kv_attention_tree(c.dev, low, q, tree)
+    near = lambda a, z: (full(a) - full(z)).__abs__().max() <= 2.0 ** -9 * abs(full(z)).max()  # noqa: E731  (two roundings of fp16, splits)
+    assert near(got[new:], want[new:]) and near(got[:most], want[:most])
+
+
 def test_graphs_streams_and_workspace():
     """Two captured graphs, each with scratch of its own, replayed in turn while lengths and bits change."""
     import torch
