@@ -108,11 +108,6 @@ struct Steps {
   typedef El RawAny __attribute__((ext_vector_type(COUNT), aligned(sizeof(El))));
   Raw v;
   __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const RawAny*>(reinterpret_cast<const El*>(p) + at); }
-  // the second half takes the first one's place
-  __device__ __forceinline__ void turn() {
-#pragma unroll
-    for (int i = 0; i < COUNT / 2; ++i) v[i] = v[i + COUNT / 2];
-  }
   // bf16: all bits set where the 2 bytes are one, else none (a choice in bits: at a branch the compiler would keep everything in registers)
   __device__ __forceinline__ float get(int i, unsigned bf16) const {
     if constexpr (WIDE) return v[i];
@@ -120,23 +115,25 @@ struct Steps {
   }
 };
 
-// A row tile's sums of the waves, in a fixed order, to y: lane (channel, rows 4 q .. 4 q + 3).
-template <int NT>
-__device__ __forceinline__ void store_tile(const GroupsArgs& p, f32x4 (*red)[NT][64], const f32x4 (&total)[NT], int64_t m0, int rows, int64_t n0) {
+// The waves' sums of MT row tiles, in a fixed order, to y: lane (channel, rows 4 q .. 4 q + 3).  m0, rows: of the first tile.
+template <int MT, int NT>
+__device__ __forceinline__ void store_tiles(const GroupsArgs& p, f32x4* red, const f32x4 (*total)[NT], int64_t m0, int rows, int64_t n0) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-  for (int j = 0; j < NT; ++j) red[wave][j][lane] = total[j];
-  __syncthreads();
-  for (int t = threadIdx.x; t < NT * 64; t += kGroupThreads) {
-    const int j = t >> 6, l = t & 63;
-    f32x4 sum = red[0][j][l];
+  for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int v = 1; v < kGroupWaves; ++v) sum += red[v][j][l];
+    for (int j = 0; j < NT; ++j) red[((wave * MT + i) * NT + j) * 64 + lane] = total[i][j];
+  __syncthreads();
+  for (int t = threadIdx.x; t < MT * NT * 64; t += kGroupThreads) {
+    const int tile = t >> 6, i = tile / NT, j = tile % NT, l = t & 63;
+    f32x4 sum = red[t];
+#pragma unroll
+    for (int v = 1; v < kGroupWaves; ++v) sum += red[v * (MT * NT * 64) + t];
     const int64_t n = n0 + j * 16 + (l & 15);
     if (n >= p.N) continue;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int m = 4 * (l >> 4) + e;
+      const int m = i * 16 + 4 * (l >> 4) + e;
       if (m >= rows) continue;
       const float y = apply_act(sum[e], p.act);
       const int64_t to = (m0 + m) * p.N + n;
@@ -240,7 +237,8 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
   constexpr int NW = kGroupWaves, TERMS = Operand<T>::TERMS, STEP = 128, OF_STEP = STEP / G;  // groups of a step
   constexpr int CH = 64 * (int)sizeof(El) / 16;            // chunks of 16 bytes of a row and 64 k
   constexpr int LOADS = MT * 16 * CH / 64;                 // a lane's
-  constexpr int STAGE = NW * MT * 16 * CH, RED = NW * NT * 64;
+  constexpr int PASS = MT < 2 ? 1 : 2;                     // row tiles whose sums meet in LDS together
+  constexpr int STAGE = NW * MT * 16 * CH, RED = NW * PASS * NT * 64;
   __shared__ v4i lds[STAGE > RED ? STAGE : RED];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int r = lane & 15, q = lane >> 4;
@@ -274,22 +272,36 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
   };
 
   // Whole steps of the wave, neighbours.  What comes next is requested while this is multiplied, without a branch: behind one the compiler
-  // does not know what is in flight, and waits for everything.
+  // does not know what is in flight, and waits for everything.  Loads arrive in the order of their requests, so that whatever was requested
+  // before something that is waited for has been waited for as well.
   const int whole = K / STEP, s0 = (int)((int64_t)whole * wave / NW), s1 = (int)((int64_t)whole * (wave + 1) / NW);
   f32x4 total[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) total[i][j] = f32x4{0, 0, 0, 0};
-  v4i x[LOADS], w[NT], w_next[NT];
-  Steps<WIDE, OF_STEP> sc[NT], sc_next[NT];
   HalfSums<T, MT, NT, G> sums;
   sums.clear();
-  auto request_x = [&](int k) {
+  auto request_x = [&](v4i (&to)[LOADS], int k) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) x[i] = *reinterpret_cast<const v4i_byte*>(x_row[i] + k);
+    for (int i = 0; i < LOADS; ++i) to[i] = *reinterpret_cast<const v4i_byte*>(x_row[i] + k);
   };
-  auto stage = [&]() {
+  struct Weights {
+    v4i w[NT];
+    Steps<WIDE, OF_STEP> sc[NT];
+  };
+  auto request_w = [&](Weights& to, int s) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      to.w[j] = *reinterpret_cast<const v4i_byte*>(w_row[j] + ((s * STEP + 32 * q) >> 1));
+      to.sc[j].load(p.scale, s_row[j] + s * OF_STEP);
+    }
+  };
+  auto arrange = [&](Weights& of) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) of.w[j] = exchange(of.w[j]);
+  };
+  auto stage = [&](const v4i (&x)[LOADS]) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) own[put[i]] = x[i];
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -308,73 +320,61 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
       }
     }
   };
-  auto w_of = [&](int j, int c) { return (unsigned)w[j][c]; };
-  auto step_of = [&](int j, int c) { return sc[j].get(G == 32 ? c : 0, bf16_steps); };
-  // the other half's codes and steps take the first one's place
-  auto turn = [&]() {
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      w[j] = v4i{w[j].z, w[j].w, 0, 0};
-      sc[j].turn();
-    }
+  auto multiply = [&](const Weights& of, int half, int there, bool last) {
+    sums.add(total, there, last, term_of, [&](int j, int c) { return (unsigned)of.w[j][2 * half + c]; },
+             [&](int j, int c) { return of.sc[j].get(G == 32 ? 2 * half + c : G == 64 ? half : 0, bf16_steps); });
   };
+  // rows a half step ahead, weights a step, behind the rows that are waited for first (all of one or two steps ahead, where rows are few enough for the
+  // registers, was no faster: 16 x 4096 x 11008, groups of 32: 14.0 us against 12.0)
   if (s0 < s1) {
-    request_x(s0 * STEP);
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      w[j] = *reinterpret_cast<const v4i_byte*>(w_row[j] + ((s0 * STEP + 32 * q) >> 1));
-      sc[j].load(p.scale, s_row[j] + s0 * OF_STEP);
-    }
+    v4i x[LOADS];
+    Weights now, next;
+    request_x(x, s0 * STEP);
+    request_w(now, s0);
 #pragma unroll 1
     for (int s = s0; s < s1; ++s) {
       const int then = s + 1 < s1 ? s + 1 : s;
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        w[j] = exchange(w[j]);
-        w_next[j] = *reinterpret_cast<const v4i_byte*>(w_row[j] + ((then * STEP + 32 * q) >> 1));
-        sc_next[j].load(p.scale, s_row[j] + then * OF_STEP);
-      }
-#pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        stage();
-        request_x(half == 0 ? s * STEP + 64 : then * STEP);
-        sums.add(total, 2, half == 1, term_of, w_of, step_of);
-        turn();
-      }
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        w[j] = w_next[j];
-        sc[j] = sc_next[j];
-      }
+      arrange(now);
+      stage(x);
+      request_x(x, s * STEP + 64);
+      request_w(next, then);
+      multiply(now, 0, 2, false);
+      stage(x);
+      request_x(x, then * STEP);
+      multiply(now, 1, 2, true);
+      now = next;
     }
   }
   if (G < 128 && whole * STEP < K && wave == NW - 1) {  // the rest of the row: one to three matrix steps
     // a lane's 32 codes, and its chunk of x, lie in the row or behind it, as a whole; those behind are not multiplied
     const int k = whole * STEP, there = (K - k) / 32, at = k + 32 * q;
+    v4i x[LOADS];
+    Weights rest;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      w[j] = exchange(*reinterpret_cast<const v4i_byte*>(w_row[j] + ((at < K ? at : K - 32) >> 1)));
+      rest.w[j] = *reinterpret_cast<const v4i_byte*>(w_row[j] + ((at < K ? at : K - 32) >> 1));
 #pragma unroll
       for (int g = 0; g < OF_STEP; ++g) {
         Steps<WIDE, 1> one;
         one.load(p.scale, s_row[j] + (whole * OF_STEP + g < groups ? whole * OF_STEP + g : groups - 1));
-        sc[j].v[g] = one.v[0];
+        rest.sc[j].v[g] = one.v[0];
       }
     }
-#pragma unroll 1
-    for (int half = 0; 2 * half < there; ++half) {
+    arrange(rest);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (2 * half >= there) break;  // uniform
       const int first = lane % CH * EL, here = k + 64 * half;
-      request_x(here + first < K ? here : K - EL - first);
-      stage();
-      sums.add(total, there - 2 * half, false, term_of, w_of, step_of);
-      turn();
+      request_x(x, here + first < K ? here : K - EL - first);
+      stage(x);
+      multiply(rest, half, there - 2 * half, false);
     }
   }
   __syncthreads();  // the waves' sums go where x was
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
+  for (int i = 0; i < MT; i += PASS) {
     if (i) __syncthreads();
-    store_tile<NT>(p, reinterpret_cast<f32x4(*)[NT][64]>(lds), total[i], m0 + 16 * i, rows - 16 * i, n0);
+    store_tiles<PASS, NT>(p, reinterpret_cast<f32x4*>(lds), total + i, m0 + 16 * i, rows - 16 * i, n0);
   }
 }
 
@@ -518,7 +518,7 @@ __global__ __launch_bounds__(kGroupThreads) void linear_groups_few_k(GroupsArgs 
     unit(w[0], whole, (K - whole * UNIT) / 32);
   }
   __syncthreads();  // the waves' sums go where x was
-  store_tile<NT>(p, reinterpret_cast<f32x4(*)[NT][64]>(few_lds), total[0], 0, rows, n0);
+  store_tiles<1, NT>(p, reinterpret_cast<f32x4*>(few_lds), total, 0, rows, n0);
 }
 
 // Channel tiles per workgroup: what makes the bytes that a CU loads smallest, its workgroups' weights and rows.
