@@ -3,8 +3,8 @@
 // y[m][n] = act(sum_g s[n][g] sum_{k in g} c[n][k] x[m][k]).  The weights are read once and meet at most 64 rows at a time, so that their bytes
 // bound it while there are few rows (1 x 4096 x 12288, fp16 steps: 26 MB in 8.4 us, of which a launch takes 2.6; a kernel that only reads
 // so many in the same way takes 5.3), and with many the rows, which every workgroup reads out of the L2 (61 x 4096 x 11008, groups of
-// 32: 21.6 us for 230 workgroups' 115 MB of x and 27 MB of weights).
-// A lane loads 16 bytes, 32 codes, of a weight row; the waves of a workgroup take an eighth of k each and their sums meet in LDS, in a
+// 32: 19.9 us; its loads alone 17, its arithmetic alone 16.7: 230 workgroups read 115 MB of x and 27 MB of weights, with two waves to a SIMD).
+// A lane loads 16 bytes, 32 codes, of a weight row; the waves of a workgroup share k out among them and their sums meet in LDS, in a
 // fixed order.
 //
 // The product runs on v_mfma_f32_16x16x32 in the rows' own 16-bit type (rows x times codes): bf16 and fp16 hold x and codes exactly.
@@ -226,7 +226,7 @@ struct HalfSums {
   }
 };
 
-// T: type of x, WIDE: steps of 4 bytes, G: group.  A workgroup takes NT x 16 output channels and MT x 16 rows, each wave an eighth of k.
+// T: type of x, WIDE: steps of 4 bytes, G: group.  A workgroup takes NT x 16 output channels and MT x 16 rows, its waves steps of 128 k.
 // A wave's rows of x come 64 k at a time, whole cache lines, through registers into LDS of its own, from where a lane reads its row's operands:
 // read straight as operands, 16 rows of 64 bytes a time, a line came twice (64 x 4096 x 11008, groups of 128: 55 us with a channel tile to a
 // workgroup, 30 so, 20 with three).
@@ -271,10 +271,11 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
     return own[row * CH + (chunk ^ (row >> 1 & 7))];
   };
 
-  // Whole steps of the wave, neighbours.  What comes next is requested while this is multiplied, without a branch: behind one the compiler
+  // Whole steps are dealt out to the waves in turn, so that neighbours read a line's two halves of codes, and the lines of their steps, at about the
+  // same time (a piece of k to each: 16 x 4096 x 11008, groups of 32: 11.8 us against 11.0, 64 rows alike).  What comes next is requested while this is multiplied, without a branch: behind one the compiler
   // does not know what is in flight, and waits for everything.  Loads arrive in the order of their requests, so that whatever was requested
   // before something that is waited for has been waited for as well.
-  const int whole = K / STEP, s0 = (int)((int64_t)whole * wave / NW), s1 = (int)((int64_t)whole * (wave + 1) / NW);
+  const int whole = K / STEP;
   f32x4 total[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -326,14 +327,14 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
   };
   // rows a half step ahead, weights a step, behind the rows that are waited for first (all of one or two steps ahead, where rows are few enough for the
   // registers, was no faster: 16 x 4096 x 11008, groups of 32: 14.0 us against 12.0)
-  if (s0 < s1) {
+  if (wave < whole) {
     v4i x[LOADS];
     Weights now, next;
-    request_x(x, s0 * STEP);
-    request_w(now, s0);
+    request_x(x, wave * STEP);
+    request_w(now, wave);
 #pragma unroll 1
-    for (int s = s0; s < s1; ++s) {
-      const int then = s + 1 < s1 ? s + 1 : s;
+    for (int s = wave; s < whole; s += NW) {
+      const int then = s + NW < whole ? s + NW : s;
       arrange(now);
       stage(x);
       request_x(x, s * STEP + 64);
