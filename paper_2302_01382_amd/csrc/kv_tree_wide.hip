@@ -1,5 +1,7 @@
 // kv_tree_wide.hip -- attention of a tree of drafted tokens where a sequence brings many rows: the prompt's kernel (kv_prompt.hpp)
-// with the tree's bits as its mask.
+// with the tree's bits as its mask.  24 sequences of up to 13 drafted tokens behind up to 8000, 32 / 8 heads of 128 in bf16: 77 us in pieces of
+// 64 rows, vector instructions 40 % and matrix steps 19 % of the cycles, 294 MB read; 61 behind 65500 in fp16: 113 in pieces of 128, 50 % and 37 %
+// (every probability has a second term there).
 #include "kv_prompt.hpp"
 
 namespace mpq {

@@ -7,6 +7,8 @@
 // top-th largest is a bound that at least `top` values reach and few more do; those are listed, and a value's place in the order is
 // the number of listed ones before it.  Where too many share the bound (all logits equal, say), they are taken one at a time.
 // Rows of several pieces are joined by a workgroup each.
+// Bytes and vector instructions bound it together where rows are many: 2500 x 65536 bf16, 328 MB, 62.7 us and 6.7 for the join, the vector ALUs
+// busy for 78 % of it, a third of that with the exponentials; 190 x 100003 fp32, 76 MB, 17.3 and 4.0; a single row is latency, 5.8.
 #include "types.hpp"
 
 namespace mpq {

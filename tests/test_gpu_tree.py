@@ -251,6 +251,28 @@ def test_offsets_past_32_bits(new):
     check(small, full(got), full(q), seen, dim ** -0.5, "bfloat16")
 
 
+@pytest.mark.parametrize("dtype,page,heads,group,dim,new", [("bfloat16", 64, 8, 2, 64, 5), ("float32", 16, 8, 1, 16, 20), ("float16", 32, 16, 2, 64, 30),
+                                                            ("bfloat16", 64, 16, 3, 16, 61), ("float32", 128, 4, 1, 128, 40), ("bfloat16", 16, 8, 2, 144, 9),
+                                                            ("float16", 64, 16, 1, 80, 150)])
+def test_sequences_of_many_lengths(dtype, page, heads, group, dim, new):
+    """One long one, some short, one of its drafted tokens alone, one that brings none."""
+    import torch
+    r = rng(16)
+    length = [5000, 200, 2600, 4999, 151, 3, 700, 64]
+    rows = [min(new, n) for n in length]
+    rows[4], rows[6] = min(151, new), 0
+    c, b = drafted(r, length, rows, heads, dim, page, 8, dtype)
+    seen, tree = bits_of([parents(r, n) for n in rows], (new + 63) // 64)
+    q = dev(r.standard_normal((b.rows, heads * group, dim)), dtype)
+    got = mpq.kv_attention_tree(c.dev, b, q, tree)
+    check(c, full(got), full(q), seen, dim ** -0.5, dtype)
+    # shorter than the bound that the call was planned for
+    b.kv_len.copy_(dev([max(n, m) for n, m in zip([900, 200, 1, 64, 151, 3, 700, 64], rows)], "int32"))
+    c.length = full(b.kv_len).astype(np.int32)
+    check(c, full(mpq.kv_attention_tree(c.dev, b, q, tree)), full(q), seen, dim ** -0.5, dtype)
+    assert torch.equal(mpq.kv_attention_tree(c.dev, b, q, tree), mpq.kv_attention_tree(c.dev, b, q, tree))
+
+
 @pytest.mark.parametrize("new", (6, 70))
 def test_a_bound_of_rows_too_low(new):
     """max_new below a sequence's rows: the others' rows are right, and those of every row within the bound."""
