@@ -1131,12 +1131,29 @@ def linear_groups(x, w_q, w_scale, act=ACT_NONE, dtype=None, y=None):
     return y
 
 
-def _heads(x, rows, dim, what):
-    """(heads, elements between rows, elements between heads) of a tensor [rows, heads, dim]."""
+_NO_HEADS = (None, 0, 0, 0, None, None, None, 0, 0)
+
+
+def _turned(x, out, weight, rows, dim, floats, what):
+    """Of q or k, [rows, heads, dim]: (address, elements between rows, between heads, heads, the weight's address, output, its address, elements
+    between its rows, between its heads)."""
+    if x is None:
+        if out is not None or weight is not None:
+            raise ValueError("%s_out and %s_weight go with %s" % (what, what, what))
+        return _NO_HEADS
     shape, stride = x.shape, x.stride()
     if len(shape) != 3 or shape[0] != rows or shape[2] != dim or stride[2] != 1:
         raise ValueError("%s: expected [%d, heads, %d] with contiguous channels" % (what, rows, dim))
-    return shape[1], stride[0], stride[1]
+    heads = shape[1]
+    if out is None:
+        out, o_ts, o_hs = x.new(rows, heads, dim), heads * dim, dim
+    else:
+        o_shape, o_stride = out.shape, out.stride()
+        if o_shape != shape or o_stride[2] != 1 or out.dtype != x.dtype:
+            raise ValueError("%s_out: expected %s's type and shape, with contiguous channels" % (what, what))
+        o_ts, o_hs = o_stride[0], o_stride[1]
+    w = None if weight is None else _dense(weight, floats, (dim,), "weight").data_ptr()
+    return x.data_ptr(), stride[0], stride[1], heads, w, out, out.data_ptr(), o_ts, o_hs
 
 
 def rotate_heads(q, k, positions, frequencies, q_weight=None, k_weight=None, eps=1e-6, layout=ROTATE_HALVES, q_out=None, k_out=None):
@@ -1147,40 +1164,22 @@ def rotate_heads(q, k, positions, frequencies, q_weight=None, k_weight=None, eps
     if some is None or some.dim() != 3:
         raise ValueError("expected q or k, [rows, heads, dim]")
     rows, _, dim = some.shape
-    dtype = some.dtype
-    t = _type(dtype)
+    t = _type(some.dtype)
     stream = _here(q, k, positions, frequencies, q_weight, k_weight, q_out, k_out)
+    if k is not None and k.dtype != some.dtype:
+        raise ValueError("q and k have one type")
     floats, ints = _empty(some)
-    inputs, outputs, outs = [], [], []
-    for x, out, weight, what in ((q, q_out, q_weight, "q"), (k, k_out, k_weight, "k")):
-        if x is None:
-            if out is not None or weight is not None:
-                raise ValueError("%s_out and %s_weight go with %s" % (what, what, what))
-            inputs.append((None, 0, 0, 0, None))
-            outputs.append((None, 0, 0))
-            outs.append(None)
-            continue
-        heads, ts, hs = _heads(x, rows, dim, what)
-        if out is None:
-            out, o_ts, o_hs = x.new(rows, heads, dim), heads * dim, dim
-        else:
-            out_heads, o_ts, o_hs = _heads(out, rows, dim, what + "_out")
-            if out_heads != heads or out.dtype != dtype:
-                raise ValueError("an output has its input's type and heads")
-        if x.dtype != dtype:
-            raise ValueError("q and k have one type")
-        inputs.append((x.data_ptr(), ts, hs, heads, None if weight is None else _dense(weight, floats.dtype, (dim,), "weight").data_ptr()))
-        outputs.append((out.data_ptr(), o_ts, o_hs))
-        outs.append(out)
-    pairs, pos, freq = 0, None, None
-    if frequencies is not None and frequencies.numel():
-        pairs = frequencies.numel()
-        freq = _dense(frequencies, floats.dtype, (pairs,), "frequencies").data_ptr()
+    floats = floats.dtype
+    qp, q_ts, q_hs, q_n, qw, q_out, qo, qo_ts, qo_hs = _turned(q, q_out, q_weight, rows, dim, floats, "q")
+    kp, k_ts, k_hs, k_n, kw, k_out, ko, ko_ts, ko_hs = _turned(k, k_out, k_weight, rows, dim, floats, "k")
+    pairs = 0 if frequencies is None else frequencies.numel()
+    pos = freq = None
+    if pairs:
+        freq = _dense(frequencies, floats, (pairs,), "frequencies").data_ptr()
         pos = _dense(positions, ints.dtype, (rows,), "positions").data_ptr()
-    (qp, q_ts, q_hs, q_n, qw), (kp, k_ts, k_hs, k_n, kw) = inputs
     _check(lib().mpq_rotate_heads(t, rows, dim, qp, q_ts, q_hs, q_n, kp, k_ts, k_hs, k_n, pos, freq, pairs, int(layout), qw, kw, float(eps),
-                                  *outputs[0], *outputs[1], stream), "mpq_rotate_heads")
-    return outs[0], outs[1]
+                                  qo, qo_ts, qo_hs, ko, ko_ts, ko_hs, stream), "mpq_rotate_heads")
+    return q_out, k_out
 
 
 def tree_bits(parents):
