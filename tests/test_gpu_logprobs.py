@@ -184,6 +184,44 @@ def test_strides_outputs_and_the_last_vocabulary():
     assert [t.shape for t in empty] == [(0,), (0,), (0, 3), (0, 3)]
 
 
+@pytest.mark.parametrize("vocab", (1000, 40000, 70000))
+def test_offsets_past_32_bits(vocab):
+    """Rows that lie 2^31 bytes apart."""
+    import torch
+    r = rng(8)
+    x = rows(r, 6, vocab, "bfloat16")
+    far = torch.empty((5 << 30) + vocab, dtype=torch.bfloat16, device="cuda").as_strided((6, vocab), (1 << 30, 1))
+    far.copy_(x)
+    t = dev(r.integers(0, vocab, 6), "int32")
+    for a, z in zip(mpq.token_logprobs(far, t, 9), mpq.token_logprobs(x, t, 9)):
+        assert torch.equal(a, z)
+
+
+def test_graphs_that_bring_scratch_of_their_own():
+    """Rows of several pieces: two captured graphs, and eager calls with one workspace, in turn."""
+    import torch
+    r = rng(9)
+    n, vocab = 5, 90001
+    x, t, ws = rows(r, n, vocab, "float16"), dev(r.integers(0, vocab, n), "int32"), mpq.Workspace()
+    assert mpq.token_logprobs_workspace_bytes(n, vocab, x.dtype, 6) > 0
+    graphs = []
+    mpq.token_logprobs(x, t, 6, ws=ws)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = mpq.token_logprobs(x, t, 6)
+        graphs.append((g, out))
+    for i in range(4):
+        x.copy_(rows(r, n, vocab, "float16"))
+        for g, _ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        want = mpq.token_logprobs(x, t, 6, ws=ws)
+        for _, out in graphs:
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
 def test_refusals_of_the_binding():
     r = rng(4)
     x = rows(r, 3, 100, "float32")
