@@ -79,17 +79,19 @@ __device__ __forceinline__ void place_keys(const Key* keys, int n, int top, Key*
 
 __device__ __forceinline__ float at_least(float d) { return __builtin_elementwise_maximum(d, kLeast); }  // (a NaN stays one)
 
-// what a row's outputs are made of, but for the alternatives: by one thread; ln l
+// The row's token, asked for before its logits, and that token's logit, asked for once they are there: at the row's end either would be a
+// latency to wait for.
+__device__ __forceinline__ int token_of(const LogprobArgs& a, int64_t row) { return a.logprob ? a.tokens[row] : -1; }
 template <int T>
-__device__ __forceinline__ float finish_row(const LogprobArgs& a, int64_t row, float m, float l, float w) {
+__device__ __forceinline__ float logit_of(const LogprobArgs& a, int64_t row, int token) {
+  if (token < 0 || token >= a.vocab) return -__builtin_inff();
+  return (float)reinterpret_cast<const typename Elem<T>::type*>(a.logits)[row * a.stride + token];
+}
+// what a row's outputs are made of, but for the alternatives: by one thread; ln l
+__device__ __forceinline__ float finish_row(const LogprobArgs& a, int64_t row, float logit, float m, float l, float w) {
   const float log_l = m == -__builtin_inff() ? __builtin_nanf("") : logf(l);
   if (a.entropy) a.entropy[row] = log_l - w / l * kLn2;
-  if (a.logprob) {
-    const int t = a.tokens[row];
-    float x = -__builtin_inff();
-    if (t >= 0 && t < a.vocab) x = (float)reinterpret_cast<const typename Elem<T>::type*>(a.logits)[row * a.stride + t];
-    a.logprob[row] = __builtin_fmaf(a.scale, x - m, -log_l);
-  }
+  if (a.logprob) a.logprob[row] = __builtin_fmaf(a.scale, logit - m, -log_l);
   return log_l;
 }
 
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_k(LogprobArgs a) {
   const int piece = (int)(b - row * a.pieces);
   if (row >= a.rows) return;
   const El* x = reinterpret_cast<const El*>(a.logits) + row * a.stride;
-  const int vocab = (int)a.vocab, first = piece * (THREADS * 8 * V);
+  const int vocab = (int)a.vocab, first = piece * (THREADS * 8 * V), token = a.pieces > 1 ? -1 : token_of(a, row);
   float v[V][8], most[V];  // most: of each vector
   if (first + THREADS * 8 * V <= vocab) {  // uniform
 #pragma unroll
@@ -164,6 +166,7 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_k(LogprobArgs a) {
     for (int e = 1; e < 8; ++e) most[i] = fmaxf(most[i], v[i][e]);
     mine = fmaxf(mine, most[i]);
   }
+  const float logit = logit_of<T>(a, row, token);
   lane_max[wave][lane] = mine;
   const float of_wave = wave_max(mine);
   if (lane == 0) sm_m[wave] = of_wave;
@@ -211,7 +214,7 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_k(LogprobArgs a) {
     l = sum_of<NW>(sm_l);
     w = sum_of<NW>(sm_w);
     if (a.pieces > 1) a.piece[b] = Piece{m, l, w};
-    else sm_log = finish_row<T>(a, row, m, l, w);
+    else sm_log = finish_row(a, row, logit, m, l, w);
   }
   if (a.top == 0) return;
   const int n = count;
@@ -261,6 +264,7 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_join_k(LogprobAr
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = block_index();
   if (row >= a.rows) return;
+  const int token = token_of(a, row);
   const Piece* piece = a.piece + row * a.pieces;
   const int entries = a.pieces * a.top;
   const Key* best = a.best + row * entries;
@@ -272,6 +276,7 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_join_k(LogprobAr
   for (int i = tid + kPieceThreads; i < a.pieces; i += kPieceThreads) m = fmaxf(m, piece[i].m);
   if (!all)
     for (int i = tid + kPieceThreads; i < entries; i += kPieceThreads) mine = max(mine, (unsigned)(best[i] >> 32));
+  const float logit = logit_of<T>(a, row, token);
   m = wave_max(m);
   if (lane == 0) sm_m[wave] = m;
   lane_max[wave][lane] = mine;
@@ -306,7 +311,7 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_join_k(LogprobAr
     }
   }
   __syncthreads();
-  if (tid == 0) sm_log = finish_row<T>(a, row, m, (sm_l[0] + sm_l[1]) + (sm_l[2] + sm_l[3]), (sm_w[0] + sm_w[1]) + (sm_w[2] + sm_w[3]));
+  if (tid == 0) sm_log = finish_row(a, row, logit, m, (sm_l[0] + sm_l[1]) + (sm_l[2] + sm_l[3]), (sm_w[0] + sm_w[1]) + (sm_w[2] + sm_w[3]));
   if (a.top == 0) return;
   if (!all) n = count;
   if (n <= kListed) {

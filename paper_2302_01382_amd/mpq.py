@@ -1175,6 +1175,8 @@ def rotate_heads(q, k, positions, frequencies, q_weight=None, k_weight=None, eps
     pairs = 0 if frequencies is None else frequencies.numel()
     pos = freq = None
     if pairs:
+        if positions is None:
+            raise ValueError("a rotation takes positions")
         freq = _dense(frequencies, floats, (pairs,), "frequencies").data_ptr()
         pos = _dense(positions, ints.dtype, (rows,), "positions").data_ptr()
     _check(lib().mpq_rotate_heads(t, rows, dim, qp, q_ts, q_hs, q_n, kp, k_ts, k_hs, k_n, pos, freq, pairs, int(layout), qw, kw, float(eps),

@@ -158,6 +158,8 @@ def test_refusals_of_the_binding():
             mpq.rotate_heads(*bad)
     with pytest.raises(ValueError):
         mpq.rotate_heads(q, k, pos, f, q_out=torch.empty_like(k))
+    with pytest.raises(ValueError):
+        mpq.rotate_heads(q, k, None, f)
     with pytest.raises(mpq.MpqError):
         mpq.rotate_heads(q, k, pos, dev(frequencies(30)))
     with pytest.raises(mpq.MpqError):
