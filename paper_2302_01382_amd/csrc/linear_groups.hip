@@ -229,7 +229,7 @@ struct HalfSums {
 // T: type of x, WIDE: steps of 4 bytes, G: group.  A workgroup takes NT x 16 output channels and MT x 16 rows, its waves steps of 128 k.
 // A wave's rows of x come 64 k at a time, whole cache lines, through registers into LDS of its own, from where a lane reads its row's operands:
 // read straight as operands, 16 rows of 64 bytes a time, a line came twice (64 x 4096 x 11008, groups of 128: 55 us with a channel tile to a
-// workgroup, 30 so, 20 with three).
+// workgroup, 30 so, 18 with three).
 // grid: x channels, y blocks of rows
 template <int T, bool WIDE, int G, int MT, int NT>
 __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p) {
