@@ -91,13 +91,14 @@ struct PromptCfg {
 // grid: pairs (sequence, head) fastest, a place further from one row tile to the next, so that each XCD has tiles of long and of
 // short sequences; then splits; row tiles last, the last ones -- under a causal mask the longest -- first.
 // ONE: a page holds at least a step's tokens, which then lie on one page.
-// TREE: of a sequence's own rows, its last tokens, a row sees those that its bits name.
+// TREE: of a sequence's own rows, its last tokens, a row sees those that its bits name.  Its probabilities have both terms in every type: drafts
+// are kept or dropped by what comes of them, and a call of few rows (kv_tree.hip) has both.
 template <int T, int DH, int NQ, bool ONE, bool TREE, bool SINGLE = false>
 __device__ __forceinline__ void prompt_rows_body(const AttnArgs& a, int64_t wg_tiles, const TreeMask& tree) {
   using C = PromptCfg<T, DH, NQ, SINGLE>;
   using E = Elem<T>;
   typedef typename E::type El;
-  constexpr int QT = C::QT, PT = C::PT, TT = 64;
+  constexpr int QT = C::QT, PT = TREE ? 2 : C::PT, TT = 64;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, quarter = lane >> 4;

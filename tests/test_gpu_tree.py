@@ -4,6 +4,7 @@ import pytest
 
 from oracle import drafts
 from test_gpu_kv import DTYPES, NAN, Pair, tables, tokens
+from test_gpu_kv_edges import half_step
 from test_gpu_parity import host, mpq
 from test_gpu_tokens import dev, full, rng
 
@@ -288,6 +289,45 @@ def test_a_bound_of_rows_too_low(new):
     got = mpq.kv_attention_tree(c.dev, low, q, tree)
     near = lambda a, z: (full(a) - full(z)).__abs__().max() <= 2.0 ** -9 * abs(full(z)).max()  # noqa: E731  (two roundings of fp16, splits)
     assert near(got[new:], want[new:]) and near(got[:most], want[:most])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("page", (16, 64))
+@pytest.mark.parametrize("new,group,dim", [(2, 1, 64), (5, 4, 64), (5, 6, 128), (3, 5, 256), (40, 1, 64), (33, 2, 128), (40, 1, 256), (64, 3, 64),
+                                           (64, 4, 128), (64, 3, 256)])
+def test_probabilities_keep_their_bits(dtype, page, new, group, dim):
+    """With a value of its own channel for each of 64 tokens an output is a token's probability.  Products of whole numbers are exact
+    here, so that a logit below 9 is off by its scalings alone (9 * 4 * 2^-24 = 1.125 * 2^-19) and a probability by that, its exponential
+    and the value factor that it takes along (2^-20), its two fp16 terms and the sum (2^-21, 64 * 2^-24): 1.94 * 2^-18 together.
+    The terms end at 2^-25 of a scale that holds the largest one at 2^8 or more: 2^-33, of values below 2.  Beyond that an output is off by
+    the half step that it is rounded by, however many rows the call has."""
+    import torch
+    r = rng(page + new + dim)
+    heads = 4
+    pages, table = tables(r, 1, 900 // page)          # (places for more than short sequences, so that many rows go to the kernel for many)
+    c = Pair(pages, heads, page, dim, 8)
+    scale = 1 / 128 / dim ** 0.5
+    for seed in range(4):
+        k = r.integers(-127, 128, (64, heads, dim)).astype(np.float64)
+        k[::page] = 127.0                              # a page's maximum, so that codes are the numbers
+        v = np.broadcast_to(np.eye(64, dim)[:, None, :] * (1 + seed / 16), (64, heads, dim))
+        mpq.kv_append(c.dev, c.batch([64], [64], table), dev(k, dtype), dev(v, dtype))
+        b = c.batch([new], [64], table, new, 900)
+        bits = r.integers(0, 2 ** 63, new, dtype=np.int64) | 1 << np.arange(new, dtype=np.int64) % 63
+        tree = torch.from_numpy(bits[:, None]).cuda()
+        q = r.integers(-3, 4, (new, heads * group, dim)).astype(np.float64)
+        got = full(mpq.kv_attention_tree(c.dev, b, dev(q, dtype), tree, softmax_scale=scale)).astype(np.float64)
+        x = np.einsum("jhd,rhgd->rhgj", k, q.reshape(new, heads, group, dim)).reshape(new, heads * group, 64) * scale
+        j = np.arange(64)
+        sees = (j < 64 - new) | (bits[:, None] >> np.maximum(j - (64 - new), 0) & 1 != 0)
+        assert np.abs(x).max() < 9 and sees.any(1).all()
+        x = np.where(sees[:, None, :], x, -np.inf)
+        e = np.exp(x - x.max(2, keepdims=True))
+        p = e / e.sum(2, keepdims=True) * (1 + seed / 16)
+        off = p * 2.0 ** -17 + 2.0 ** -32
+        assert np.isfinite(got).all() and not got[..., 64:].any()
+        over = np.abs(got[..., :64] - p) - off - half_step(p + off, dtype)
+        assert (over <= 0).all(), (over.max(), (over > 0).sum())
 
 
 def test_graphs_streams_and_workspace():
