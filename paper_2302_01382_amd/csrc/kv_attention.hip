@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kBlock) void kv_attention_join_k(AttnArgs a) {
   if (s >= a.b.seqs) return;
   const Sequence sq = sequence(a.b, a.c.page, (int)s);
   const int64_t at = tile * 16 + row;
-  if (at >= (int64_t)sq.n * a.group) return;
+  if (at >= joined_rows(a, sq)) return;
   const int D = a.c.dim, quads = D >> 2, parts = kBlock / quads;
   const int d = ((int)threadIdx.x % quads) * 4, part = (int)threadIdx.x / quads;
   const Partial* of = a.part + slot * 16 + row;  // the row's in the first split; 16 to the next

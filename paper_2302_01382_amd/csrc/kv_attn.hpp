@@ -50,6 +50,13 @@ int launch_tree_wide(int type, const AttnArgs& a, const TreeMask& tree, int64_t 
 
 #if defined(__HIPCC__)
 
+// Pairs (row, query head) of a sequence and a key head that splits are joined of: of a sequence with more rows than the call was told of only
+// that many have partial results in every kernel, and what the scratch holds for the others is whatever was there.
+__device__ __forceinline__ int64_t joined_rows(const AttnArgs& a, const Sequence& sq) {
+  const int64_t most = a.b.max_new < a.b.rows ? a.b.max_new : a.b.rows;
+  return (sq.n < most ? sq.n : most) * a.group;
+}
+
 // 64 bits of a row of a tree from bit `at` on: ones before its first drafted token, zeros behind its words
 __device__ __forceinline__ uint64_t tree_bits(const TreeMask& tree, int64_t row, int64_t at) {
   const uint64_t* words = tree.bits + row * tree.words;

@@ -183,6 +183,36 @@ def test_more_rows_than_the_call_was_told_of_stay_inside():
     check_attention(c, full(out), full(q), True, 0, 0.125, "bfloat16")
 
 
+@pytest.mark.parametrize("most", (149, 146))
+def test_rows_behind_a_low_bound_are_nobodys(most):
+    """Rows behind max_new of a split prompt: left as they were or what the full call gives, whatever the scratch held."""
+    import torch
+    r = rng(78)
+    new, length, group = 150, 16000, 2
+    c = mpq.KvCache.empty(length // 64 + 1, 2, 64, 64)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for t in (c.k_codes, c.v_codes):
+        t.copy_(torch.randint(-127, 128, t.shape, dtype=torch.int8, device="cuda", generator=g))
+    c.k_absmax.fill_(0.3)
+    c.v_absmax.fill_(1.0)
+    arrays = dev([0, new], "int32"), dev([length], "int32"), dev(np.arange(251)[None], "int32")
+    q = queries(r, new, 2 * group, 64, "bfloat16")
+    want = mpq.kv_attention(c, mpq.KvBatch(*arrays, new, new, length), q)
+    low = mpq.KvBatch(*arrays, new, most, length)
+    need = mpq.kv_attention_workspace_bytes(c, low, torch.bfloat16, 2 * group)
+    assert need > 0
+    ws = mpq.Workspace()
+    ws.get(need)
+    ws.buf.fill_(255)
+    out = torch.full_like(q, 9.0)
+    mpq.kv_attention(c, low, q, out=out, ws=ws)
+    left = (full(out) == 9).all((1, 2))
+    assert not left[:most].any()
+    # (both are off by 2 V (2^-12 + n / 4 2^-24 + ...) < 2^-9 V and a rounding of 2^-8 of themselves, V = 1)
+    got, want = full(out)[~left], full(want)[~left]
+    assert (np.abs(got - want) <= 2.0 ** -8 + 2.0 ** -7 * np.abs(want)).all()
+
+
 def test_offsets_past_32_bits_of_a_prompt():
     """Pages behind the first 4 GiB of codes."""
     import torch

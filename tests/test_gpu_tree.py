@@ -330,6 +330,29 @@ def test_probabilities_keep_their_bits(dtype, page, new, group, dim):
         assert (over <= 0).all(), (over.max(), (over > 0).sum())
 
 
+@pytest.mark.parametrize("new", (6, 70, 75))
+def test_rows_behind_a_low_bound_are_nobodys(new):
+    """max_new below a sequence's rows: those behind it are left as they were or are what the full call gives, whatever the scratch held."""
+    import torch
+    r = rng(17)
+    length = [2000, 900, 1500]
+    c, b = drafted(r, length, [new, 3, 2], 2, 64, 64, 8, "float16")
+    seen, tree = bits_of([parents(r, n) for n in (new, 3, 2)])
+    q = dev(r.standard_normal((b.rows, 4, 64)), "float16")
+    for most in (new - 1, new - 2, new - 5):
+        low = mpq.KvBatch(b.starts, b.kv_len, b.table, b.rows, most, 2000)
+        need = mpq.kv_attention_tree_workspace_bytes(c.dev, low, q.dtype, 4)
+        assert need > 0
+        ws = mpq.Workspace()
+        ws.get(need)
+        ws.buf.fill_(255)
+        out = torch.full((b.rows, 4, 64), 9.0, dtype=torch.float16, device="cuda")
+        mpq.kv_attention_tree(c.dev, low, q, tree, out=out, ws=ws)
+        left = (full(out) == 9).all((1, 2))
+        assert not left[:most].any() and not left[new:new + min(most, 3)].any() and not left[new + 3:new + 3 + min(most, 2)].any()
+        check(c, np.where(left[:, None, None], full(mpq.kv_attention_tree(c.dev, b, q, tree)), full(out)), full(q), seen, 0.125, "float16")
+
+
 def test_graphs_streams_and_workspace():
     """Two captured graphs, each with scratch of its own, replayed in turn while lengths and bits change."""
     import torch
