@@ -589,7 +589,7 @@ int mpq_kv_attention_tree(const mpq_kv_cache* cache, const mpq_kv_batch* batch, 
  * A row of nothing but minus infinity has no distribution: NaN, as a row with a NaN or with plus infinity has (whose indices are of
  * the logits that are not NaN).
  * logits     [rows x vocab] of `type`, vocab contiguous, rows row_stride elements apart (row_stride >= vocab); vocab at most 2^22.
- * scale      of the logits (1 / temperature): positive, finite.
+ * scale      of the logits (1 / temperature): positive, scale * log2(e) finite.
  * tokens     device int32[rows].  Outputs float [rows], float [rows], float and int32 [rows x top].  Nullable: logprob_out (then tokens
  *            too) and entropy_out; with top = 0 the last two.  top 0 .. 32, at least one output.
  * Sums in fp32 of exponentials relative to the row's maximum; logits are not rounded.

@@ -2,6 +2,8 @@
 //
 // With m the row's largest logit, d = scale log2(e) (x - m), l = sum 2^d and w = sum d 2^d:
 //   ln p_t = scale (x_t - m) - ln l,   entropy = ln l - ln 2 w / l.
+// A scale below 1 is split into its power of two, unit, and a factor of 1 to 2: d = factor log2(e) (unit x - unit m), the difference in one fused
+// step, so that logits further apart than fp32's range lose nothing, and no factor its bits, however small the scale is.
 // A workgroup holds a piece of a row in registers, so that the maximum is known before the first exponential and nothing is
 // rescaled in the loop.  The largest `top` of a piece: of the 64 maxima of what the threads of a lane number hold, the
 // top-th largest is a bound that at least `top` values reach and few more do; those are listed, and a value's place in the order is
@@ -10,6 +12,8 @@
 // Bytes and vector instructions bound it together where rows are many: 2500 x 65536 bf16, 328 MB, 62.7 us and 6.7 for the join, the vector ALUs
 // busy for 78 % of it, a third of that with the exponentials; 190 x 100003 fp32, 76 MB, 17.3 and 4.0; a single row is latency, 5.8.
 #include "types.hpp"
+
+#include <cmath>
 
 namespace mpq {
 
@@ -27,7 +31,7 @@ struct Piece {
 struct LogprobArgs {
   const void* logits;
   int64_t rows, vocab, stride;
-  float scale;
+  float unit, factor;  // scale: their product; unit: a power of two, at most 1
   const int32_t* tokens;
   float* logprob;
   float* entropy;
@@ -87,16 +91,18 @@ __device__ __forceinline__ float logit_of(const LogprobArgs& a, int64_t row, int
   if (token < 0 || token >= a.vocab) return -__builtin_inff();
   return (float)reinterpret_cast<const typename Elem<T>::type*>(a.logits)[row * a.stride + token];
 }
+// unit (x - m), of unit m
+__device__ __forceinline__ float below(const LogprobArgs& a, float x, float unit_m) { return __builtin_fmaf(x, a.unit, -unit_m); }
 // what a row's outputs are made of, but for the alternatives: by one thread; ln l
 __device__ __forceinline__ float finish_row(const LogprobArgs& a, int64_t row, float logit, float m, float l, float w) {
   const float log_l = m == -__builtin_inff() ? __builtin_nanf("") : logf(l);
   if (a.entropy) a.entropy[row] = log_l - w / l * kLn2;
-  if (a.logprob) a.logprob[row] = __builtin_fmaf(a.scale, logit - m, -log_l);
+  if (a.logprob) a.logprob[row] = __builtin_fmaf(a.factor, below(a, logit, a.unit * m), -log_l);
   return log_l;
 }
 
 __device__ __forceinline__ void store_top(const LogprobArgs& a, int64_t row, int i, Key k, float m, float log_l) {
-  a.top_logprob[row * a.top + i] = k ? __builtin_fmaf(a.scale, value_of(k) - m, -log_l) : -__builtin_inff();
+  a.top_logprob[row * a.top + i] = k ? __builtin_fmaf(a.factor, below(a, value_of(k), a.unit * m), -log_l) : -__builtin_inff();
   a.top_index[row * a.top + i] = k ? index_of(k) : -1;
 }
 
@@ -174,13 +180,13 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_k(LogprobArgs a) {
   if (tid < kMostTop) out[tid] = 0;
   __syncthreads();
   const float m = max_of<NW>(sm_m);
-  const float m_use = m == -__builtin_inff() ? 0.0f : m, c = a.scale * kLog2e;
+  const float m_use = m == -__builtin_inff() ? 0.0f : a.unit * m, c = a.factor * kLog2e;
   float l = 0.0f, w = 0.0f;
 #pragma unroll
   for (int i = 0; i < V; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float d = at_least((v[i][e] - m_use) * c), p = __builtin_amdgcn_exp2f(d);
+      const float d = at_least(below(a, v[i][e], m_use) * c), p = __builtin_amdgcn_exp2f(d);
       l += p;
       w = __builtin_fmaf(p, d, w);
     }
@@ -285,12 +291,12 @@ __global__ __launch_bounds__(kPieceThreads) void token_logprobs_join_k(LogprobAr
   if (all && tid < kWave) listed[tid] = first;
   __syncthreads();
   m = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
-  const float m_use = m == -__builtin_inff() ? 0.0f : m, c = a.scale * kLog2e;
+  const float m_use = m == -__builtin_inff() ? 0.0f : a.unit * m, c = a.factor * kLog2e;
   float l = 0.0f, w = 0.0f;
   for (int i = tid; i < a.pieces; i += kPieceThreads) {
     // 2^(d + d') = 2^d 2^d', and (d + d') 2^(d + d') likewise; a piece of nothing has l of 0, or of NaN
     if (i != tid) p = piece[i];
-    const float d = at_least((p.m - m_use) * c), f = __builtin_amdgcn_exp2f(d);
+    const float d = at_least(below(a, p.m, m_use) * c), f = __builtin_amdgcn_exp2f(d);
     l = __builtin_fmaf(p.l, f, l);
     w = __builtin_fmaf(f, __builtin_fmaf(p.l, d, p.w), w);
   }
@@ -411,7 +417,7 @@ extern "C" int mpq_token_logprobs(const void* logits, int type, int64_t rows, in
   LogprobPlan p;
   const int rc = plan_logprobs(rows, vocab, type, top, p);
   if (rc != MPQ_OK) return rc;
-  if (row_stride < vocab || mul_overflows(rows, row_stride) || !(scale > 0.0f) || __builtin_isinf(scale)) return MPQ_ERR_SHAPE;
+  if (row_stride < vocab || mul_overflows(rows, row_stride) || !(scale > 0.0f) || __builtin_isinf(scale * kLog2e)) return MPQ_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(logits) & (uintptr_t)(type_size(type) - 1)) return MPQ_ERR_ALIGN;
   if ((reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(logprob_out) | reinterpret_cast<uintptr_t>(entropy_out)) & 3u)
     return MPQ_ERR_ALIGN;
@@ -421,7 +427,10 @@ extern "C" int mpq_token_logprobs(const void* logits, int type, int64_t rows, in
   if (!logprob_out && !entropy_out && top == 0) return MPQ_ERR_NULL;
   if (p.ws_bytes > 0 && (!ws || ws_bytes < p.ws_bytes)) return MPQ_ERR_WORKSPACE;
   if (p.ws_bytes > 0 && !aligned16(ws)) return MPQ_ERR_ALIGN;
-  LogprobArgs a{logits, rows, vocab, row_stride, scale, tokens, logprob_out, entropy_out, top, top_logprob_out, top_index_out, p.pieces,
+  int exponent = 0;
+  const float half_factor = frexpf(scale, &exponent), unit = scale < 1.0f ? ldexpf(1.0f, exponent - 1) : 1.0f;
+  const float factor = scale < 1.0f ? 2.0f * half_factor : scale;
+  LogprobArgs a{logits, rows, vocab, row_stride, unit, factor, tokens, logprob_out, entropy_out, top, top_logprob_out, top_index_out, p.pieces,
                 nullptr, nullptr};
   if (p.pieces > 1) {
     a.best = reinterpret_cast<Key*>(ws);

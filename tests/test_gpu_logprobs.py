@@ -146,6 +146,34 @@ def test_large_values_and_scales():
         check(mpq.token_logprobs(dev(y), dev(tokens, "int32"), 4, scale), y, tokens, 4, scale)
 
 
+@pytest.mark.parametrize("dtype", ("float32", "bfloat16"))
+@pytest.mark.parametrize("vocab", (3000, 40000, 90000))
+def test_logits_of_the_whole_range(dtype, vocab):
+    """Logits up to twice the type's largest apart, and scales that bring them together, down to the least ones that there are."""
+    r = rng(vocab + 1)
+    top = 3.3e38
+    x = dev(np.clip(r.standard_normal((4, vocab)) * 2e38, -top, top), dtype)
+    x[1, ::2], x[1, 1::2] = top, -top
+    x[2, 5] = -INF
+    tokens = r.integers(0, vocab, 4).astype(np.int32)
+    for scale in (1e-38, 3e-38, 2.0 ** -126, 1e-40, 2.0 ** -149, 0.7e-37, 0.3):
+        check(mpq.token_logprobs(x, dev(tokens, "int32"), 7, scale), full(x), tokens, 7, scale)
+
+
+def test_the_largest_scale():
+    """Up to the one whose product with log2 e is the last finite number; the rest is refused."""
+    r = rng(12)
+    for size in (1e-38, 1e-3):
+        x = (r.standard_normal((3, 5000)) * size).astype(np.float32)
+        x[2] = 0
+        tokens = r.integers(0, 5000, 3).astype(np.int32)
+        for scale in (1e38, 2.35e38):
+            check(mpq.token_logprobs(dev(x), dev(tokens, "int32"), 4, scale), x, tokens, 4, scale)
+    for scale in (2.4e38, 3.4e38):
+        with pytest.raises(mpq.MpqError):
+            mpq.token_logprobs(dev(x), dev(tokens, "int32"), 4, scale)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("vocab", (700, 30000))
 def test_rows_of_the_lowest_value(dtype, vocab):
