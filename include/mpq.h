@@ -537,8 +537,8 @@ int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int t
  *            [N * K/group x group] with MPQ_PER_ROW give codes and maxima of such groups); any alignment.
  * group      32, 64 or 128; K a multiple of it.   w_scale  [N x K/group] of scale_type, dense.
  * y_out      [M x N] of y_type, dense; it may not overlap the inputs.
- * Products are exact and sums in fp32 (a group's about -24 times the sum of its x, which is added in again: intermediate values are up
- * to 31 |x| summed); where such a value passes fp32's range, and for an x that is not finite, results are infinite or NaN.
+ * Products are exact and sums in fp32; where one of x's products or sums passes fp32's range, and for an x that is not finite (fp32: that
+ * bf16 would round to infinity), results are infinite or NaN.
  * Made for few rows, whose time is that of reading the weights; more go in blocks of 64, each of which reads the weights.
  * Errors: MPQ_ERR_NULL, MPQ_ERR_SHAPE (dims, stride, group, an unknown type or act), MPQ_ERR_ALIGN (elements).  M = 0: nothing is
  * launched. */

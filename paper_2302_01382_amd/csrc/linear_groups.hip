@@ -8,10 +8,11 @@
 // fixed order.
 //
 // The product runs on v_mfma_f32_16x16x32 in the rows' own 16-bit type (rows x times codes): bf16 and fp16 hold x and codes exactly.
-// fp32 rows go in as three bf16 terms, 24 bits.  Both types take a code's four bits as they are: u = code + 8 in the mantissa of 16,
-// which makes 16 + u = code + 24, one shift and one three-operand logic instruction for two codes.  The 24 comes off again in the same sums:
-// -24 times the sum of the group's x is a matrix step with a constant operand, which all channels share.  A sum's rounding is that of terms up to
-// 24 / 4 times as large as without it, 2^-21 of them.
+// fp32 rows go in as three bf16 terms, 24 bits.  Operands are the codes themselves, so that a sum holds nothing but the products.  (Cheaper to make is
+// code + 24, the code's bits in the mantissa of 16, and -24 times the group's sum of x added in again: rows of one sign then lose four bits of
+// fp32 -- K = 4096, rows behind a ReLU, groups of 128: 5e-6 of the outputs' norm -- for times within 4 % of these, but for one row of bf16 with fp32
+// steps, 1 x 4096 x 12288 in groups of 64, 8.5 us against 9.3.)  fp16: that form, less 24 in one packed instruction for two codes.  bf16, which
+// has no such instruction: v_cvt_off_f32_i4 makes code / 16 of four bits, whose upper half is the operand; the 16 is multiplied in at the end.
 //
 // A group's sum has to hold that group alone, and a matrix step adds up the k of four quarters of the wave.  A lane's 16 bytes are
 // 32 neighbouring codes: the quarters exchange their dwords, four swaps for four dwords, after which dword c has 32 neighbouring k.
@@ -33,38 +34,48 @@ struct GroupsArgs {
 
 constexpr int kGroupWaves = 8, kGroupThreads = kGroupWaves * 64;
 
+// UNIT: what operands of codes are counted in
 template <int T>
 struct Operand {  // bf16, also for the terms of fp32
-  static constexpr int TERMS = T == MPQ_F32 ? 3 : 1, SHIFT = 3;
-  static constexpr unsigned MASK = 0x00780078u, FORM = 0x41804180u ^ 0x00400040u;  // 16, and the codes' sign bits turned: u = code + 8
-  static constexpr unsigned MINUS = 0xC1C0C1C0u;                                   // -24
+  static constexpr int TERMS = T == MPQ_F32 ? 3 : 1;
+  static constexpr float UNIT = 16.0f;
   static __device__ __forceinline__ f32x4 mfma(v4i a, v4i b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  // eight codes as an operand: its dword i holds codes i and i + 4
+  static __device__ __forceinline__ v4i codes(unsigned w) {
+    const unsigned odd = w >> 4;
+    v4i r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned of = i & 1 ? odd : w;
+      const float low = __builtin_amdgcn_cvt_off_f32_i4(of >> 8 * (i >> 1)), high = __builtin_amdgcn_cvt_off_f32_i4(of >> (8 * (i >> 1) + 16));
+      r[i] = (int)__builtin_amdgcn_perm((unsigned)bits_from_f(high), (unsigned)bits_from_f(low), 0x07060302u);
+    }
+    return r;
   }
 };
 template <>
 struct Operand<MPQ_F16> {
-  static constexpr int TERMS = 1, SHIFT = 6;
-  static constexpr unsigned MASK = 0x03C003C0u, FORM = 0x4C004C00u ^ 0x02000200u, MINUS = 0xCE00CE00u;
+  static constexpr int TERMS = 1;
+  static constexpr float UNIT = 1.0f;
   static __device__ __forceinline__ f32x4 mfma(v4i a, v4i b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
-};
-
-// Eight codes as an operand: its dword i holds codes i and i + 4.
-template <int T>
-__device__ __forceinline__ v4i codes_operand(unsigned w) {
-  using O = Operand<T>;
-  v4i r;
+  // 16, and the code's sign bit turned in the mantissa behind it: code + 24, less that
+  static __device__ __forceinline__ v4i codes(unsigned w) {
+    v4i r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int left = O::SHIFT - 4 * i;
-    const unsigned v = left >= 0 ? w << (left & 31) : w >> (-left & 31);
-    r[i] = (int)((v & O::MASK) ^ O::FORM);
+    for (int i = 0; i < 4; ++i) {
+      const int left = 6 - 4 * i;
+      const unsigned v = left >= 0 ? w << (left & 31) : w >> (-left & 31);
+      const f16x2 with = __builtin_bit_cast(f16x2, (v & 0x03C003C0u) ^ (0x4C004C00u ^ 0x02000200u));
+      r[i] = __builtin_bit_cast(int, with - f16x2{(_Float16)24, (_Float16)24});
+    }
+    return r;
   }
-  return r;
-}
-// eight 16-bit values in their order -> the order of codes_operand
+};
+// eight 16-bit values in their order -> the order of Operand::codes
 __device__ __forceinline__ v4i pair_up(v4i v) {
   return v4i{(int)__builtin_amdgcn_perm((unsigned)v.z, (unsigned)v.x, 0x05040100u), (int)__builtin_amdgcn_perm((unsigned)v.z, (unsigned)v.x, 0x07060302u),
              (int)__builtin_amdgcn_perm((unsigned)v.w, (unsigned)v.y, 0x05040100u), (int)__builtin_amdgcn_perm((unsigned)v.w, (unsigned)v.y, 0x07060302u)};
@@ -115,9 +126,9 @@ struct Steps {
   }
 };
 
-// The waves' sums of MT row tiles, in a fixed order, to y: lane (channel, rows 4 q .. 4 q + 3).  m0, rows: of the first tile.
+// The waves' sums of MT row tiles, in a fixed order, times unit to y: lane (channel, rows 4 q .. 4 q + 3).  m0, rows: of the first tile.
 template <int MT, int NT>
-__device__ __forceinline__ void store_tiles(const GroupsArgs& p, f32x4* red, const f32x4 (*total)[NT], int64_t m0, int rows, int64_t n0) {
+__device__ __forceinline__ void store_tiles(const GroupsArgs& p, f32x4* red, const f32x4 (*total)[NT], int64_t m0, int rows, int64_t n0, float unit) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -135,7 +146,7 @@ __device__ __forceinline__ void store_tiles(const GroupsArgs& p, f32x4* red, con
     for (int e = 0; e < 4; ++e) {
       const int m = i * 16 + 4 * (l >> 4) + e;
       if (m >= rows) continue;
-      const float y = apply_act(sum[e], p.act);
+      const float y = apply_act(sum[e] * unit, p.act);
       const int64_t to = (m0 + m) * p.N + n;
       if (p.y_type == MPQ_F32) reinterpret_cast<float*>(p.y)[to] = y;
       else reinterpret_cast<unsigned short*>(p.y)[to] = to_half(y, p.y_type == MPQ_BF16);
@@ -144,53 +155,31 @@ __device__ __forceinline__ void store_tiles(const GroupsArgs& p, f32x4* red, con
 }
 
 // What the two kernels share: the sums of 64 k, `half` of a step of 128, times their groups' steps to the totals.  `term` holds x of 32 k as
-// operands, of MT row tiles; from: -24 times the sums of its x.  Groups of 128 are summed over both halves.
+// operands, of MT row tiles.  Groups of 128 are summed over both halves.
 template <int T, int MT, int NT, int G>
 struct HalfSums {
   using O = Operand<T>;
   static constexpr int PER = G / 32;
-  f32x4 from[MT], part[PER > 1 ? NT : 1][MT];
+  f32x4 part[PER > 1 ? NT : 1][MT];
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      from[i] = f32x4{0, 0, 0, 0};
+    for (int j = 0; j < (PER > 1 ? NT : 1); ++j)
 #pragma unroll
-      for (int j = 0; j < (PER > 1 ? NT : 1); ++j) part[j][i] = f32x4{0, 0, 0, 0};
-    }
+      for (int i = 0; i < MT; ++i) part[j][i] = f32x4{0, 0, 0, 0};
   }
-  // c: 0 or 1, of the half
-  __device__ __forceinline__ void add32(const v4i (&term)[MT][O::TERMS], const unsigned (&w)[NT], int c) {
-    const v4i minus = {(int)O::MINUS, (int)O::MINUS, (int)O::MINUS, (int)O::MINUS};
-    const bool fresh = PER == 1 || (PER == 2 && c == 0);
+  // to part j, or its first: 32 k
+  __device__ __forceinline__ void product(const v4i (&term)[MT][O::TERMS], unsigned w, int j, bool first) {
+    const v4i codes = O::codes(w);
 #pragma unroll
     for (int t = 0; t < O::TERMS; ++t)
 #pragma unroll
-      for (int i = 0; i < MT; ++i) from[i] = O::mfma(term[i][t], minus, fresh && t == 0 ? f32x4{0, 0, 0, 0} : from[i]);
-    if constexpr (PER > 1) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const v4i codes = codes_operand<T>(w[j]);
-#pragma unroll
-        for (int t = 0; t < O::TERMS; ++t)
-#pragma unroll
-          for (int i = 0; i < MT; ++i) part[j][i] = O::mfma(term[i][t], codes, fresh && t == 0 ? f32x4{0, 0, 0, 0} : part[j][i]);
-      }
-    }
-  }
-  // groups of 32: the product itself, from `from` on
-  __device__ __forceinline__ void product(const v4i (&term)[MT][O::TERMS], unsigned w) {
-    const v4i codes = codes_operand<T>(w);
-#pragma unroll
-    for (int t = 0; t < O::TERMS; ++t)
-#pragma unroll
-      for (int i = 0; i < MT; ++i) part[0][i] = O::mfma(term[i][t], codes, t == 0 ? from[i] : part[0][i]);
+      for (int i = 0; i < MT; ++i) part[j][i] = O::mfma(term[i][t], codes, first && t == 0 ? f32x4{0, 0, 0, 0} : part[j][i]);
   }
   __device__ __forceinline__ void scale(f32x4 (&total)[MT][NT], int j, float step) {
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        total[i][j][e] = __builtin_fmaf(PER > 1 ? part[PER > 1 ? j : 0][i][e] + from[i][e] : part[0][i][e], step, total[i][j][e]);
+      for (int e = 0; e < 4; ++e) total[i][j][e] = __builtin_fmaf(part[PER > 1 ? j : 0][i][e], step, total[i][j][e]);
   }
   // term_of(c, term), dword c of a half's codes w[j][c], step_of(j, c): of tile j, of the group that ends with c; there: matrix steps of
   // the half, 1 or 2; last: whether a group of 128 ends
@@ -205,13 +194,10 @@ struct HalfSums {
       unsigned w[NT];
 #pragma unroll
       for (int j = 0; j < NT; ++j) w[j] = w_of(j, c);
-      add32(term, w, c);
-      if constexpr (PER == 1) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          product(term, w[j]);
-          scale(total, j, step_of(j, c));
-        }
+      for (int j = 0; j < NT; ++j) {
+        product(term, w[j], PER > 1 ? j : 0, PER == 1 || (PER == 2 && c == 0));
+        if (PER == 1) scale(total, j, step_of(j, c));
       }
       if (PER == 2 && c == 1) {
 #pragma unroll
@@ -375,7 +361,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
 #pragma unroll
   for (int i = 0; i < MT; i += PASS) {
     if (i) __syncthreads();
-    store_tiles<PASS, NT>(p, reinterpret_cast<f32x4*>(lds), total + i, m0 + 16 * i, rows - 16 * i, n0);
+    store_tiles<PASS, NT>(p, reinterpret_cast<f32x4*>(lds), total + i, m0 + 16 * i, rows - 16 * i, n0, Operand<T>::UNIT);
   }
 }
 
@@ -519,7 +505,7 @@ __global__ __launch_bounds__(kGroupThreads) void linear_groups_few_k(GroupsArgs 
     unit(w[0], whole, (K - whole * UNIT) / 32);
   }
   __syncthreads();  // the waves' sums go where x was
-  store_tiles<1, NT>(p, reinterpret_cast<f32x4*>(few_lds), total, 0, rows, n0);
+  store_tiles<1, NT>(p, reinterpret_cast<f32x4*>(few_lds), total, 0, rows, n0, Operand<T>::UNIT);
 }
 
 // Channel tiles per workgroup: what makes the bytes that a CU loads smallest, its workgroups' weights and rows.

@@ -171,6 +171,56 @@ def test_rows_do_not_depend_on_their_neighbours():
     assert torch.equal(again, y)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("group", (32, 64, 128))
+@pytest.mark.parametrize("M", (2, 8, 40))
+def test_one_sided_rows(dtype, group, M):
+    """Rows behind a ReLU, or all positive, steps of either sign, fp32 outputs: relative to the outputs' norm as near to 64 bits as products of the
+    codes themselves.  Roundings are independent, u / sqrt(3) of a partial sum each.  32 k in three terms bring at most 24 (one per four products),
+    a group of 128 then 96, of partial sums whose mean square is half of the group's at most: u sqrt(96 / 6) = 4 u of a group's sum, and of the outputs'
+    norm, since groups' sums are independent as well.  The 32 to 128 groups and 8 waves bring u sqrt(136 / 6) = 4.8 u.  Together 6.3 u = 3.7e-7."""
+    r = rng(group + M)
+    K, N = 4096, 96
+    import torch
+    codes, w, steps, _ = layer(r, N, K, group)
+    steps = steps * r.choice([-1, 1], steps.shape).astype(np.float32)
+    steps_dev = dev(steps)
+    for x in (np.maximum(r.standard_normal((M, K)), 0), r.random((M, K)) + 0.5):
+        x = dev(x, dtype)
+        y = host(mpq.linear_groups(x, w, steps_dev, dtype=torch.float32)).astype(np.float64)
+        want = drafts.linear_groups(full(x), codes, steps, group)
+        assert np.linalg.norm(y - want) <= 1e-6 * np.linalg.norm(want), np.linalg.norm(y - want) / np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("group", (32, 64, 128))
+@pytest.mark.parametrize("steps_type", ("float32", "float16"))
+def test_every_channel_and_code_in_few_rows(dtype, group, steps_type):
+    """One channel of x at a time, in calls of up to 8 rows: each product by itself, 24 bits of x.  x's terms times a code are exact, their sum is
+    rounded at most twice and its product with the step once: 3 u of |x c step|, and u of it for the bits that three terms leave."""
+    import torch
+    r = rng(group + 7)
+    K, N = 256, 21
+    codes, w, steps, steps_dev = layer(r, N, K, group, steps_type)
+    value = (r.random(K) + 1) * np.exp2(r.integers(-12, 12, K)) * r.choice([-1, 1], K)
+    x = dev(np.diag(value), dtype)
+    v = np.diag(full(x)).astype(np.float64)
+    wide = np.repeat(steps.astype(np.float64), group, 1)
+    at = 0
+    for rows in [1, 2, 3, 5, 7, 8] * 12:
+        if at >= K:
+            break
+        m = slice(at, min(at + rows, K))
+        y = host(mpq.linear_groups(x[m], w, steps_dev, dtype=torch.float32))
+        want = v[m, None] * (codes * wide)[:, m].T
+        assert (np.abs(y - want) <= 4 * U * np.abs(want)).all(), (at, np.abs(y - want).max())
+        at += rows
+    assert at >= K
+    y = host(mpq.linear_groups(x, w, steps_dev, dtype=torch.float32))
+    want = v[:, None] * (codes * wide).T
+    assert (np.abs(y - want) <= 4 * U * np.abs(want)).all()
+
+
 def test_group_quant_and_its_layer():
     import torch
     r = rng(10)
