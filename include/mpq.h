@@ -539,7 +539,8 @@ int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int t
  * y_out      [M x N] of y_type, dense; it may not overlap the inputs.
  * Products are exact and sums in fp32; where one of x's products or sums passes fp32's range, and for an x that is not finite (fp32: that
  * bf16 would round to infinity), results are infinite or NaN.
- * Made for few rows, whose time is that of reading the weights; more go in blocks of 64, each of which reads the weights.
+ * Made for few rows, whose time is that of reading the weights; more go in blocks of 64, each of which reads the weights.  A row's result
+ * is the same, bit for bit, in a call of any number of rows.
  * Errors: MPQ_ERR_NULL, MPQ_ERR_SHAPE (dims, stride, group, an unknown type or act), MPQ_ERR_ALIGN (elements).  M = 0: nothing is
  * launched. */
 int mpq_linear_groups(const void* x, int x_type, int64_t M, int64_t N, int64_t K, int64_t x_stride, const uint8_t* w_q, int group,

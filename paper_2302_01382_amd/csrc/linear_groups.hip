@@ -422,17 +422,18 @@ __global__ __launch_bounds__(kGroupThreads) void linear_groups_few_k(GroupsArgs 
   const uint8_t* w_row[NT];
 #pragma unroll
   for (int j = 0; j < NT; ++j) w_row[j] = p.w + (n0 + (j * 16 + r < channels ? j * 16 + r : channels - 1)) * (K >> 1) + 16 * q;
-  const int whole = K / UNIT, s0 = (int)((int64_t)whole * wave / NW), s1 = (int)((int64_t)whole * (wave + 1) / NW);
+  // units are dealt out to the waves as linear_groups_k deals its steps: a row's sums are the same, bit for bit, in both kernels
+  const int whole = K / UNIT;
   v4i w[kUnits][NT], w_next[kUnits][NT];
   auto request = [&](v4i (&to)[kUnits][NT], int s) {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-      const int at = s + u < s1 ? s + u : s1 - 1;
+      const int at = s + u * NW < whole ? s + u * NW : whole - 1;
 #pragma unroll
       for (int j = 0; j < NT; ++j) to[u][j] = *reinterpret_cast<const v4i_byte*>(w_row[j] + at * (UNIT / 2));
     }
   };
-  if (s0 < s1) request(w, s0);
+  if (wave < whole) request(w, wave);
   if (tid < chunks) store_x(x_first, x_to);
   const int row_length = step_row_length(groups, sizeof(StepEl));
   auto store_steps = [&](v4i v, int i) {
@@ -477,16 +478,16 @@ __global__ __launch_bounds__(kGroupThreads) void linear_groups_few_k(GroupsArgs 
     }
   };
   // (the last units apart, so that the loop needs no branch around its requests)
-  int s = s0;
+  int s = wave;
 #pragma unroll 1
-  for (; s + kUnits < s1; s += kUnits) {
+  for (; s + kUnits * NW < whole; s += kUnits * NW) {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u)
 #pragma unroll
       for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(w[u][j]));  // here they have arrived: a wait further down would be one for the next as well
-    request(w_next, s + kUnits);
+    request(w_next, s + kUnits * NW);
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) unit(w[u], s + u, 4);
+    for (int u = 0; u < kUnits; ++u) unit(w[u], s + u * NW, 4);
 #pragma unroll
     for (int u = 0; u < kUnits; ++u)
 #pragma unroll
@@ -494,8 +495,8 @@ __global__ __launch_bounds__(kGroupThreads) void linear_groups_few_k(GroupsArgs 
   }
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
-    if (s + u >= s1) break;  // uniform
-    unit(w[u], s + u, 4);
+    if (s + u * NW >= whole) break;  // uniform
+    unit(w[u], s + u * NW, 4);
   }
   if (G < 128 && whole * UNIT < K && wave == NW - 1) {  // the rest of the row: one to three matrix steps
     // a lane's 32 codes lie in the row or behind it, as a whole; those behind are not multiplied

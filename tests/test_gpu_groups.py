@@ -221,6 +221,20 @@ def test_every_channel_and_code_in_few_rows(dtype, group, steps_type):
     assert (np.abs(y - want) <= 4 * U * np.abs(want)).all()
 
 
+@pytest.mark.parametrize("group,K", [(32, 4096), (64, 4224), (128, 11008), (32, 1120), (64, 8256)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_row_alone_and_in_a_batch(dtype, group, K):
+    """The same bits, in fp32, however many rows there are: one order of k for all of them."""
+    import torch
+    r = rng(K)
+    codes, w, steps, steps_dev = layer(r, 70, K, group)
+    x = dev(r.standard_normal((70, K)), dtype)
+    y = mpq.linear_groups(x, w, steps_dev, dtype=torch.float32)
+    for rows in (1, 2, 8, 9, 16, 17, 33, 64, 65):
+        for at in (0, 70 - rows):
+            assert torch.equal(mpq.linear_groups(x[at:at + rows], w, steps_dev, dtype=torch.float32), y[at:at + rows]), rows
+
+
 def test_group_quant_and_its_layer():
     import torch
     r = rng(10)
