@@ -536,7 +536,7 @@ int mpq_kv_attention(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int t
  * w_q        two's-complement nibbles [N x K/2], the even channel in the low half (packed4_out of mpq_fake_quant; the weights seen as
  *            [N * K/group x group] with MPQ_PER_ROW give codes and maxima of such groups); any alignment.
  * group      32, 64 or 128; K a multiple of it.   w_scale  [N x K/group] of scale_type, dense.
- * y_out      [M x N] of y_type, dense; it may not overlap the inputs.
+ * y_out      [M x N] of y_type, dense; it may not overlap the inputs (MPQ_ERR_SHAPE).
  * Products are exact and sums in fp32; where one of x's products or sums passes fp32's range, and for an x that is not finite (fp32: that
  * bf16 would round to infinity), results are infinite or NaN.
  * Made for few rows, whose time is that of reading the weights; more go in blocks of 64, each of which reads the weights.  A row's result

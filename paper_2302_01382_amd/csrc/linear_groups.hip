@@ -573,6 +573,19 @@ extern "C" int mpq_linear_groups(const void* x, int x_type, int64_t M, int64_t N
   if (reinterpret_cast<uintptr_t>(y_out) & (uintptr_t)(type_size(y_type) - 1)) return MPQ_ERR_ALIGN;
   if (M == 0) return MPQ_OK;
   if (!x || !w_q || !w_scale || !y_out) return MPQ_ERR_NULL;
+  // an output where others still read
+  const int x_el = (int)type_size(x_type), y_el = (int)type_size(y_type);
+  const char* to = reinterpret_cast<const char*>(y_out);
+  const int64_t to_bytes = M * N * y_el;
+  auto meets = [&](const void* from, int64_t bytes) {
+    const char* at = reinterpret_cast<const char*>(from);
+    return to < at + bytes && at < to + to_bytes;
+  };
+  if (meets(w_q, N * (K / 2)) || meets(w_scale, N * (K / group) * (int64_t)type_size(scale_type))) return MPQ_ERR_SHAPE;
+  if (meets(x, ((M - 1) * x_stride + K) * x_el)) {  // between two rows of x is no place of x
+    const int64_t row = x_stride * x_el, behind = to - reinterpret_cast<const char*>(x);
+    if (behind < 0 || behind % row < K * x_el || behind % row + to_bytes > row) return MPQ_ERR_SHAPE;
+  }
   const GroupsArgs p{x, x_stride, w_q, w_scale, M, N, (int)K, scale_type, act, y_type, y_out};
   hipStream_t st = (hipStream_t)stream;
   if (x_type == MPQ_F32) return go_type<MPQ_F32>(p, group, st);

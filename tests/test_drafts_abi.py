@@ -148,6 +148,20 @@ def test_token_logprobs_refuses():
     assert but(_2=0, _0=None, _6=None, _10=None) == mpq.OK
 
 
+@needs_no_gpu
+def test_an_output_of_the_layer_in_a_place_that_is_read_is_refused():
+    """Workgroups would read what others have written: found on the host (nothing here reaches a launch)."""
+    L = mpq.lib()
+    P = lambda a: C.c_void_p(0x1000000 + 2 * a)  # noqa: E731  (element a of one buffer of 2-byte values)
+    # x, type, M, N, K, stride, w, group, steps, their type, act, y type, y, stream
+    far = C.c_void_p(0x8000000)
+    but = caller(L.mpq_linear_groups, [P(0), 1, 4, 8, 256, 512, far, 64, C.c_void_p(0x9000000), 0, 0, 1, P(256), None])
+    assert but(_12=P(0)) == mpq.ERR_SHAPE and but(_12=P(255)) == mpq.ERR_SHAPE and but(_12=P(3 * 512 + 255)) == mpq.ERR_SHAPE
+    assert but(_12=P(512 - 31)) == mpq.ERR_SHAPE                                          # the last of 32 elements
+    assert but(_12=far) == mpq.ERR_SHAPE and but(_12=C.c_void_p(0x8000000 + 8 * 128 - 2)) == mpq.ERR_SHAPE   # the codes
+    assert but(_12=C.c_void_p(0x9000000 + 8 * 4 * 4 - 4)) == mpq.ERR_SHAPE                 # the steps
+
+
 def test_tree_bits():
     # 0 and 1 continue the sequence, 2 and 3 continue 0, 4 continues 3
     assert mpq.tree_bits([-1, -1, 0, 0, 3]).tolist() == [[0b1], [0b10], [0b101], [0b1001], [0b11001]]

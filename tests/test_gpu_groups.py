@@ -235,6 +235,24 @@ def test_a_row_alone_and_in_a_batch(dtype, group, K):
             assert torch.equal(mpq.linear_groups(x[at:at + rows], w, steps_dev, dtype=torch.float32), y[at:at + rows]), rows
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_an_output_in_the_inputs_place(dtype):
+    """Refused: workgroups would read what others have written.  An output between x's rows is none of them."""
+    import torch
+    r = rng(14)
+    K = N = 128
+    codes, w, steps, steps_dev = layer(r, N, K, 32, dtype)
+    x = dev(r.standard_normal((4, K)), dtype)
+    with pytest.raises(mpq.MpqError):
+        mpq.linear_groups(x, w, steps_dev, y=x)
+    both = torch.zeros(2, 2 * K, dtype=x.dtype, device="cuda")
+    both[:, :K] = x[:2]
+    got = mpq.linear_groups(both[:, :K], w[:64], steps_dev[:64], y=both[0, K:].view(2, 64))
+    assert torch.equal(got, mpq.linear_groups(x[:2], w[:64], steps_dev[:64]))
+    with pytest.raises(mpq.MpqError):
+        mpq.linear_groups(both[:, :K], w[:64], steps_dev[:64], y=both.view(-1)[K + 1:K + 129].view(2, 64))
+
+
 def test_group_quant_and_its_layer():
     import torch
     r = rng(10)
