@@ -554,7 +554,8 @@ int mpq_linear_groups(const void* x, int x_type, int64_t M, int64_t N, int64_t K
  * Whole turns of t are dropped in 64 bits, so that far positions keep their angle; everything else is fp32, rounded once.
  * q, k       [rows][q_heads][dim], [rows][k_heads][dim] of `type`, dim contiguous, strides in elements; outputs likewise, their rows and
  *            heads may not overlap.  An output may be its input (the same address and strides: in place), else it may not overlap
- *            any input.  q_heads or k_heads may be 0 (pointers are not looked at then).
+ *            any input, nor the other output (MPQ_ERR_SHAPE, as for two whose ranges overlap without being views of one tensor, of equal
+ *            token strides).  q_heads or k_heads may be 0 (pointers are not looked at then).
  * dim        a multiple of 16, at most 256.   pairs  a multiple of 4, 0 .. dim / 2 (0: positions and frequencies may be NULL).
  * positions  device int32[rows] (negative: backwards).   frequencies  device float[pairs], radians per position.
  * weights    device float[dim], 4-byte aligned, nullable.   eps  at least FLT_MIN, finite.

@@ -97,6 +97,41 @@ inline bool pieces_overlap(int64_t rows, int64_t row_stride, int64_t heads, int6
   return false;
 }
 
+// rows x heads pieces of dim elements each, strides in elements
+struct Pieces {
+  const void* at;
+  int64_t row_stride, heads, head_stride;
+};
+// Whether one of x's pieces and one of y's share an element of `size` bytes.  Strides are not negative, and their products with rows and heads were
+// looked at.  Only what is certain counts as apart where the two lie among one another: rows of equal length, or a single one, as views of
+// one tensor have.
+inline bool pieces_meet(Pieces x, Pieces y, int64_t rows, int dim, int size) {
+  if (rows <= 0 || x.heads <= 0 || y.heads <= 0) return false;
+  const int64_t from = (int64_t)(reinterpret_cast<uintptr_t>(y.at) - reinterpret_cast<uintptr_t>(x.at)) / size;
+  const int64_t x_row = (x.heads - 1) * x.head_stride + dim, y_row = (y.heads - 1) * y.head_stride + dim;
+  if (from >= (rows - 1) * x.row_stride + x_row || -from >= (rows - 1) * y.row_stride + y_row) return false;
+  const int64_t rs = x.row_stride;
+  if (rows > 1) {
+    if (rs != y.row_stride || rs <= 0) return true;
+    const int64_t in_row = (from % rs + rs) % rs;  // where y's first row begins, counted from the row of x that it begins in
+    if (x_row <= in_row && in_row + y_row <= rs) return false;
+  }
+  // every distance of two heads, and of it the nearest rows
+  const bool same = x.head_stride == y.head_stride;
+  const int64_t nx = same ? x.heads + y.heads - 1 : x.heads, ny = same ? 1 : y.heads, first = same ? from + (y.heads - 1) * y.head_stride : from;
+  if (nx > 65536 / ny) return true;
+  for (int64_t i = 0; i < nx; ++i)
+    for (int64_t j = 0; j < ny; ++j) {
+      const int64_t apart = first + j * y.head_stride - i * x.head_stride;  // of y's piece from x's, in one row
+      const int64_t near = rows == 1 ? 0 : apart / rs;
+      for (int64_t r = near - 1; r <= near + 1; ++r) {
+        const int64_t over = apart - r * rs;
+        if (r > -rows && r < rows && over < dim && -over < dim) return true;
+      }
+    }
+  return false;
+}
+
 inline int64_t channels(int gran, int64_t rows, int64_t cols) {
   return gran == MPQ_PER_ROW ? rows : gran == MPQ_PER_COL ? cols : 1;
 }

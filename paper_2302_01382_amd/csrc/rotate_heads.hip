@@ -198,6 +198,14 @@ extern "C" int mpq_rotate_heads(int type, int64_t rows, int dim, const void* q, 
   if (pairs > 0 && (!positions || !frequencies)) return MPQ_ERR_NULL;
   for (int i = 0; i < 2; ++i)
     if (a.heads[i] > 0 && (!a.in[i] || !a.out[i])) return MPQ_ERR_NULL;
+  // an output in the other's place, or in an input's but its own: waves would write the same elements, or read what others have written
+  const Pieces in[2] = {{q, q_token_stride, q_heads, q_head_stride}, {k, k_token_stride, k_heads, k_head_stride}};
+  const Pieces out[2] = {{q_out, q_out_token_stride, q_heads, q_out_head_stride}, {k_out, k_out_token_stride, k_heads, k_out_head_stride}};
+  const int el = (int)type_size(type);
+  if (pieces_meet(out[0], out[1], rows, dim, el)) return MPQ_ERR_SHAPE;
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j)
+      if (!(i == j && in[i].at == out[i].at) && pieces_meet(out[i], in[j], rows, dim, el)) return MPQ_ERR_SHAPE;
   if (blocks_z(rows * ((int64_t)q_heads + k_heads), kBlock) > 65535u) return MPQ_ERR_SHAPE;
   hipStream_t st = (hipStream_t)stream;
   if (type == MPQ_F32) return launch<MPQ_F32>(a, layout, st);

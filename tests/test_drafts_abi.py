@@ -1,5 +1,6 @@
 """Refusals of the calls of a step of drafted tokens, found on the host before anything is launched, and the tree's bits."""
 import ctypes as C
+import random
 
 import pytest
 
@@ -160,6 +161,59 @@ def test_an_output_of_the_layer_in_a_place_that_is_read_is_refused():
     assert but(_12=P(512 - 31)) == mpq.ERR_SHAPE                                          # the last of 32 elements
     assert but(_12=far) == mpq.ERR_SHAPE and but(_12=C.c_void_p(0x8000000 + 8 * 128 - 2)) == mpq.ERR_SHAPE   # the codes
     assert but(_12=C.c_void_p(0x9000000 + 8 * 4 * 4 - 4)) == mpq.ERR_SHAPE                 # the steps
+
+
+@needs_no_gpu
+def test_rotated_heads_in_a_place_that_is_read_or_written_are_refused():
+    L = mpq.lib()
+    P = lambda a: C.c_void_p(0x1000000 + 2 * a)  # noqa: E731
+    # type, rows, dim, q, ts, hs, heads, k, ts, hs, heads, positions, frequencies, pairs, layout, weights, eps, q_out, ts, hs, k_out, ts, hs
+    R = 8 * 64                                                                             # a row of eight heads
+    q, k, out = 0, 4 * 64, 100000
+    but = caller(L.mpq_rotate_heads, [1, 5, 64, P(q), R, 64, 4, P(k), R, 64, 2, FAKE, FAKE, 32, 0, FAKE, FAKE, 1e-6,
+                                      P(out), R, 64, P(out + k), R, 64, None])
+    assert but(_21=P(out)) == mpq.ERR_SHAPE and but(_21=P(out + k - 1)) == mpq.ERR_SHAPE    # both outputs in one place, or one element too near
+    assert but(_21=P(out + R - 2 * 64 + 1)) == mpq.ERR_SHAPE                               # into the next row's
+    assert but(_21=P(out + 4 * R + 3 * 64 + 63)) == mpq.ERR_SHAPE                          # q's last element
+    assert but(_21=P(out - 5 * R + 7 * 64 + 1)) == mpq.ERR_SHAPE
+    assert but(_19=R, _20=128, _21=P(out + 63), _22=R, _23=128) == mpq.ERR_SHAPE           # heads in turn
+    assert but(_21=P(out + 1024), _22=R + 64) == mpq.ERR_SHAPE                             # rows of another length among them
+    assert but(_18=P(q + 16)) == mpq.ERR_SHAPE and but(_18=P(k), _21=P(out)) == mpq.ERR_SHAPE and but(_21=P(q)) == mpq.ERR_SHAPE
+    assert but(_18=P(q), _21=P(k - 1)) == mpq.ERR_SHAPE and but(_18=P(q + R), _19=R) == mpq.ERR_SHAPE
+
+
+@needs_no_gpu
+def test_places_of_queries_and_keys():
+    """Patterns of few rows and heads of two outputs in one buffer against the elements that they cover, and of an output and the other's input.  A
+    call that is taken ends at its launch, without a GPU.  (Rows of two lengths among one another count as one place.)"""
+    r = random.Random(5)
+    L, dim, seen = mpq.lib(), 16, {}
+    far = [C.c_void_p(0x8000000 * i) for i in range(1, 5)]
+    for trial in range(30000):
+        rows, qh, kh = r.choice((1, 2, 3, 4)), r.choice((1, 2, 3, 5)), r.choice((1, 2, 4))
+        strides = (16, 17, 24, 32, 33, 48, 64, 80, 96, 112, 128, 160, 200)
+        q_ts, q_hs, k_hs = r.choice(strides), r.choice(strides), r.choice(strides)
+        k_ts = q_ts if r.random() < 0.8 else r.choice(strides)
+        at = r.choice((0, 1, 15, 16, 17, 32, 48, 64, 80, -16, -15, -40, -64, 100, 200, 300, 500, -200, -300))
+        cells = lambda at, heads, ts, hs: [at + i * ts + h * hs + d for i in range(rows) for h in range(heads) for d in range(dim)]  # noqa: E731
+        a, b = cells(0, qh, q_ts, q_hs), cells(at, kh, k_ts, k_hs)
+        if len(set(a)) < len(a) or len(set(b)) < len(b):
+            continue   # (each alone is looked at elsewhere)
+        place = C.c_void_p(0x1000000), C.c_void_p(0x1000000 + 2 * at)
+        if trial % 2:
+            ins, outs = (far[0], far[1]), place
+        else:
+            ins, outs = (far[0], place[1]), (place[0], far[2])
+        rc = L.mpq_rotate_heads(1, rows, dim, ins[0], 0, 16, qh, ins[1], k_ts, k_hs, kh, None, None, 0, 0, None, None, 1e-6,
+                                outs[0], q_ts, q_hs, outs[1], k_ts, k_hs, None)
+        meet = bool(set(a) & set(b))
+        among = min(b) <= max(a) and min(a) <= max(b)
+        if meet or not among or rows == 1 or q_ts == k_ts:
+            assert rc == (mpq.ERR_SHAPE if meet else mpq.ERR_HIP), (rows, qh, kh, q_ts, q_hs, k_ts, k_hs, at, rc)
+            seen[meet, among] = seen.get((meet, among), 0) + 1
+        else:
+            assert rc == mpq.ERR_SHAPE
+    assert min(seen.get(x, 0) for x in ((True, True), (False, True), (False, False))) > 200, seen
 
 
 def test_tree_bits():

@@ -146,6 +146,24 @@ def test_nothing_is_looked_at_of_no_heads():
         assert rc == mpq.OK and torch.equal(out, want)
 
 
+def test_outputs_in_one_place_are_refused():
+    """Both outputs, or an output and the other's input; heads in turn in one buffer are neither."""
+    import torch
+    r = rng(32)
+    q, k = heads(r, 6, 4, 64, "bfloat16"), heads(r, 6, 4, 64, "bfloat16")
+    pos, f = dev(r.integers(0, 900, 6), "int32"), dev(frequencies(32))
+    want = mpq.rotate_heads(q, k, pos, f)
+    out = torch.zeros((6, 8, 64), dtype=q.dtype, device="cuda")
+    for qo, ko in ((out[:, :4], out[:, :4]), (out[:, :4], out[:, 3:7]), (k, None), (None, q), (q, q)):
+        with pytest.raises(mpq.MpqError):
+            mpq.rotate_heads(q, k, pos, f, q_out=qo, k_out=ko)
+    for qo, ko in ((out[:, ::2], out[:, 1::2]), (out[:, 4:], out[:, :4]), (out.view(12, 4, 64)[:6], out.view(12, 4, 64)[6:]),
+                   (out.view(8, 6, 64)[:4].transpose(0, 1), out.view(8, 6, 64)[4:].transpose(0, 1))):
+        out.zero_()
+        mpq.rotate_heads(q, k, pos, f, q_out=qo, k_out=ko)
+        assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
+
+
 def test_refusals_of_the_binding():
     import torch
     r = rng(7)
