@@ -353,6 +353,44 @@ def test_rows_behind_a_low_bound_are_nobodys(new):
         check(c, np.where(left[:, None, None], full(mpq.kv_attention_tree(c.dev, b, q, tree)), full(out)), full(q), seen, 0.125, "float16")
 
 
+def splits_of(c, b, dtype, q_heads, most):
+    """Of a call, from the scratch that it asks for: partial results of 16 rows x (dim + 3) floats per tile and split."""
+    import torch
+    rows = most * q_heads // c.dev.heads
+    tiles = (rows + 15) // 16 * c.dev.heads * len(c.length)
+    return mpq.kv_attention_tree_workspace_bytes(c.dev, b, getattr(torch, dtype), q_heads) / (tiles * 16 * (c.dev.dim + 3) * 4)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,group,dim,new,length", [(1, 2, 64, 5, 9100), (2, 4, 64, 5, 9100), (1, 3, 256, 5, 9100), (2, 1, 64, 40, 12100),
+                                                        (1, 1, 128, 150, 12100), (1, 1, 64, 150, 12100), (1, 2, 256, 30, 12100)])
+def test_many_splits(dtype, heads, group, dim, new, length):
+    """One long sequence in more than 16 pieces, in every kernel: one and two tiles of 16 rows, pieces of 64 and of 128."""
+    r = rng(dim + new)
+    c, b = drafted(r, [length], [new], heads, dim, 64, 8, dtype)
+    b = mpq.KvBatch(b.starts, b.kv_len, b.table, new, new, length)
+    assert splits_of(c, b, dtype, heads * group, new) > 16
+    seen, tree = bits_of([parents(r, new)])
+    q = dev(r.standard_normal((new, heads * group, dim)), dtype)
+    check(c, full(mpq.kv_attention_tree(c.dev, b, q, tree)), full(q), seen, dim ** -0.5, dtype)
+
+
+@pytest.mark.parametrize("dtype,page,heads,group,dim,new", [("bfloat16", 64, 8, 2, 64, 5), ("float32", 16, 2, 1, 16, 20), ("float16", 32, 4, 2, 64, 14),
+                                                            ("bfloat16", 64, 2, 3, 128, 10), ("float32", 128, 4, 1, 128, 4), ("bfloat16", 16, 2, 2, 144, 9)])
+def test_few_rows_of_many_lengths(dtype, page, heads, group, dim, new):
+    """The bounds that a serving program knows: the most rows of a sequence, and the longest."""
+    r = rng(18)
+    length = [5000, 200, 2600, 4999, 151, 3, 700, 64]
+    rows = [min(new, n) for n in length]
+    rows[6] = 0
+    c, b = drafted(r, length, rows, heads, dim, page, 8, dtype)
+    b = mpq.KvBatch(b.starts, b.kv_len, b.table, b.rows, max(rows), max(length))
+    assert new * group <= 32 and splits_of(c, b, dtype, heads * group, max(rows)) >= 1
+    seen, tree = bits_of([parents(r, n) for n in rows], 1)
+    q = dev(r.standard_normal((b.rows, heads * group, dim)), dtype)
+    check(c, full(mpq.kv_attention_tree(c.dev, b, q, tree)), full(q), seen, dim ** -0.5, dtype)
+
+
 def test_graphs_streams_and_workspace():
     """Two captured graphs, each with scratch of its own, replayed in turn while lengths and bits change."""
     import torch
