@@ -407,12 +407,12 @@ __global__ __launch_bounds__(kBlock) void kv_tree_join_k(AttnArgs a) {
 // that fill the chip once; more in the wide kernel, in pieces of 64 rows of which three workgroups share a CU, of 128 from 129 rows on; few
 // rows over short sequences here, where a workgroup's latency counts.  us on the device, bf16, pages of 64 (sequences x drafted
 // tokens behind held, key heads x group, dim; one tile | two tiles | pieces of 64 | of 128, each with its best number of splits):
-// 1 x 3 behind 60000 8x4 128 fp16 33 | 35 | 44 | 69, 32 x 5 behind 4000 8x4 128 74 | 59 | 65 | -, 1 x 5 behind 32000 28 | 27 | 30 | 39, 8 x 7 behind 8000 43 |
-// 39 | 40 | -, 32 x 30 behind 1000 12x1 64 28 | 26 | 24 | 33 -- 4 x 16 behind 8000 8x4 128 41 | 38 | 31 | 36, 24 x 13 behind 8000 171 | 149 | 88 | 138, the
-// same behind 4000 in fp32 - | 91 | 73 | -, 4 x 30 behind 8000 62 | 59 | 42 | 43, 16 x 60 behind 2000 8x8 128 - | - | 84 | 87, 1 x 61 behind 65500 8x4 128 fp16
-// 434 | 349 | 147 | 126, 2 x 10 behind 16000 2x7 256 41 | 48 | - | 35 -- 1 x 60 behind 400 12x1 64 6.9 | 9.8 | 10.3 | -, 2 x 100 behind 300 8x4 128 18.5 |
-// 14.6 | 17.2 | 23.  (Four tiles here, which need 480 registers: 24 x 13 behind 8000 196.)  Splits: 4 x 16 behind 8000 in pieces of 64, 8 | 16 | 32:
-// 33 | 31 | 38; 24 x 13 behind 8000, 2 | 4 | 8: 118 | 88 | 110.
+// 1 x 3 behind 60000 8x4 128 fp16 33 | 34 | 42 | 56, 32 x 5 behind 4000 8x4 128 74 | 56 | 69 | 101, 1 x 5 behind 32000 29 | 27 | 29 | 39, 8 x 7 behind 8000 44 |
+// 39 | 43 | 59, 32 x 30 behind 1000 12x1 64 29 | 26 | 28 | 39 -- 4 x 16 behind 8000 8x4 128 41 | 38 | 31 | 39, 24 x 13 behind 8000 173 | 145 | 95 | 142, the
+// same behind 4000 in fp32 102 | 92 | 71 | -, 4 x 30 behind 8000 61 | 59 | 46 | 46, 16 x 60 behind 2000 8x8 128 249 | 174 | 94 | 103, 1 x 61 behind 65500 8x4 128
+// fp16 235 | 185 | 140 | 121, 2 x 10 behind 16000 2x7 256 45 | - | - | 33 -- 1 x 60 behind 400 12x1 64 7.7 | 10.6 | 14 | 18, 2 x 100 behind 300 8x4 128 18.8 |
+// 15.0 | 18.9 | 26.  (16 x 60 would be better off with pieces of 64.  Four tiles here, which need 480 registers: 24 x 13 behind 8000 196.)  Splits: 4 x 16
+// behind 8000 in pieces of 64, 8 | 16 | 32: 34 | 31 | 38; 24 x 13 behind 8000, 2 | 4 | 8: 123 | 95 | 97.
 struct TreePlan {
   int64_t row_tiles, tiles, wg_tiles;
   int mt, splits, tile_rows;

@@ -1,7 +1,7 @@
 // kv_tree_wide.hip -- attention of a tree of drafted tokens where a sequence brings many rows: the prompt's kernel (kv_prompt.hpp)
-// with the tree's bits as its mask.  24 sequences of up to 13 drafted tokens behind up to 8000, 32 / 8 heads of 128 in bf16: 77 us in pieces of
-// 64 rows, vector instructions 40 % and matrix steps 19 % of the cycles, 294 MB read; 61 behind 65500 in fp16: 113 in pieces of 128, 50 % and 37 %
-// (every probability has a second term there).
+// with the tree's bits as its mask.  24 sequences of up to 13 drafted tokens behind up to 8000, 32 / 8 heads of 128 in bf16: 88 us in pieces of
+// 64 rows, vector instructions 44 % and matrix steps 26 % of the cycles, 294 MB read (77 with one term of a probability, which leaves outputs
+// 8.9e-4 of their norm from fp32 products in place of 8e-5); 61 behind 65500 in fp16: 117 in pieces of 128, 50 % and 37 %.
 #include "kv_prompt.hpp"
 
 namespace mpq {

@@ -2,8 +2,9 @@
 //
 // y[m][n] = act(sum_g s[n][g] sum_{k in g} c[n][k] x[m][k]).  The weights are read once and meet at most 64 rows at a time, so that their bytes
 // bound it while there are few rows (1 x 4096 x 12288, fp16 steps: 26 MB in 8.4 us, of which a launch takes 2.6; a kernel that only reads
-// so many in the same way takes 5.3), and with many the rows, which every workgroup reads out of the L2 (61 x 4096 x 11008, groups of
-// 32: 19.9 us; its loads alone 17, its arithmetic alone 16.7: 230 workgroups read 115 MB of x and 27 MB of weights, with two waves to a SIMD).
+// so many in the same way takes 5.3).  With many rows it is latency: 61 x 4096 x 11008, groups of 32, takes 19.7 us, of whose cycles vector instructions
+// fill 34 % and matrix steps 9 %.  One to two waves to a SIMD wait for a chain -- a matrix step's rows from LDS, the product, the product times the
+// steps -- that a scheduling barrier keeps apart from the next one's, and 230 workgroups read 115 MB of x out of the L2 (the loads alone: 17 us).
 // A lane loads 16 bytes, 32 codes, of a weight row; the waves of a workgroup share k out among them and their sums meet in LDS, in a
 // fixed order.
 //
@@ -258,7 +259,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
   };
 
   // Whole steps are dealt out to the waves in turn, so that neighbours read a line's two halves of codes, and the lines of their steps, at about the
-  // same time (a piece of k to each: 16 x 4096 x 11008, groups of 32: 11.8 us against 11.0, 64 rows alike).  What comes next is requested while this is multiplied, without a branch: behind one the compiler
+  // same time (a piece of k to each: 16 x 4096 x 11008, groups of 32, takes 7 % more, 64 rows alike).  What comes next is requested while this is multiplied, without a branch: behind one the compiler
   // does not know what is in flight, and waits for everything.  Loads arrive in the order of their requests, so that whatever was requested
   // before something that is waited for has been waited for as well.
   const int whole = K / STEP;
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
              [&](int j, int c) { return of.sc[j].get(G == 32 ? 2 * half + c : G == 64 ? half : 0, bf16_steps); });
   };
   // rows a half step ahead, weights a step, behind the rows that are waited for first (all of one or two steps ahead, where rows are few enough for the
-  // registers, was no faster: 16 x 4096 x 11008, groups of 32: 14.0 us against 12.0)
+  // registers, was no faster: 16 x 4096 x 11008, groups of 32, takes 17 % more)
   if (wave < whole) {
     v4i x[LOADS];
     Weights now, next;
