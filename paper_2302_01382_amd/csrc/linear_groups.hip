@@ -290,6 +290,8 @@ __global__ __launch_bounds__(kGroupThreads, 2) void linear_groups_k(GroupsArgs p
     for (int j = 0; j < NT; ++j) of.w[j] = exchange(of.w[j]);
   };
   auto stage = [&](const v4i (&x)[LOADS]) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // what the lanes read of the last one has been read
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) own[put[i]] = x[i];
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
