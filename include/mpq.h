@@ -575,8 +575,8 @@ int mpq_rotate_heads(int type, int64_t rows, int dim, const void* q, int64_t q_t
  * branches; rotations are the caller's, mpq_rotate_heads).
  * tree       device int64 [rows][tree_words], 8-byte aligned, bits in words from the lowest.  tree_words at least 1 (else
  *            MPQ_ERR_SHAPE): drafted tokens behind the last word are not seen; bits behind a sequence's last drafted token do not matter.
- * Everything else, and what is rounded, as mpq_kv_attention without a window.  Tokens that are kept are appended again, in a row, behind
- * what the sequence held before; a page's maximum stays that of all that was drafted onto it. */
+ * Everything else, and what is rounded, as mpq_kv_attention without a window, but that probabilities have both terms in every type.  Tokens
+ * that are kept are appended again, in a row, behind what the sequence held before; a page's maximum stays that of all that was drafted onto it. */
 size_t mpq_kv_attention_tree_workspace_bytes(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, int q_heads);
 int mpq_kv_attention_tree(const mpq_kv_cache* cache, const mpq_kv_batch* batch, int type, const void* q, int64_t q_token_stride,
                           int64_t q_head_stride, int q_heads, float softmax_scale, const int64_t* tree, int tree_words, void* out,

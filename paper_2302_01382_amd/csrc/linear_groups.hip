@@ -13,7 +13,8 @@
 // code + 24, the code's bits in the mantissa of 16, and -24 times the group's sum of x added in again: rows of one sign then lose four bits of
 // fp32 -- K = 4096, rows behind a ReLU, groups of 128: 5e-6 of the outputs' norm -- for times within 4 % of these, but for one row of bf16 with fp32
 // steps, 1 x 4096 x 12288 in groups of 64, 8.5 us against 9.3.)  fp16: that form, less 24 in one packed instruction for two codes.  bf16, which
-// has no such instruction: v_cvt_off_f32_i4 makes code / 16 of four bits, whose upper half is the operand; the 16 is multiplied in at the end.
+// has no such instruction: v_cvt_off_f32_i4 makes code / 16 of four bits, whose upper half is the operand; the 16 is
+// multiplied in at the end, so that outputs within 2^4 of the least normal number may lose as many bits.
 //
 // A group's sum has to hold that group alone, and a matrix step adds up the k of four quarters of the wave.  A lane's 16 bytes are
 // 32 neighbouring codes: the quarters exchange their dwords, four swaps for four dwords, after which dword c has 32 neighbouring k.
